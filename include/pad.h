@@ -484,6 +484,143 @@ pad_status pad_prefill_attn(const pad_problem* prob, int32_t prefix_len, int32_t
  * (a bounded wait that gave up: PAD_ERR_DEVICE_TIMEOUT); PAD_OK otherwise. */
 pad_status pad_prefill_status(pad_stream_t stream);
 
+/* ---------------------------------------------------------------------------
+ * Steps of several tokens per branch: drafted tokens to be verified, chunks of a prompt, or
+ * single tokens over a cache held in 8 bits.  The paper's step (Eq. 3) is the case of one
+ * token per branch; the mask is its own (Sec. 3.4) applied to every chunk token: token t of
+ * event e attends to the shared prefix of its video and to its own branch's tokens up to and
+ * including itself.  A step is, in stream order,
+ *   pad_chunk_plan    host: validate, allocate pages, build the work lists and copy them to
+ *                     the workspace; one plan serves every layer of the model;
+ *   pad_chunk_append  write the new tokens' K/V into the branches' pages (quantised where the
+ *                     cache is held in 8 bits) and the new page-table entries;
+ *   pad_chunk_attn    attention of the new tokens;
+ *   pad_draft_verify  accept or reject the drafted tokens and draw the next one;
+ *   pad_chunk_commit  host: the branches' new lengths; pages past them go back.
+ * pad_chunk_read copies the branches' cached tokens out as contiguous bf16 (the layout of
+ * k_prefix / v_prefix).  All device work is asynchronous on the stream given; calls on
+ * another stream than the plan's must be ordered after it by the caller.
+ *
+ * Layouts (row-major, bf16 unless stated); N = sum of n_new, tokens packed event by event:
+ *   q      [N, h_q, head_dim]   k_new / v_new [N, h_kv, head_dim]   (token strides may be larger)
+ *   out    [N, h_q, head_dim]   fp32 or bf16 (out_dtype), lse [N, h_q] fp32, natural log
+ *   pools  kv_format PAD_KV_BF16: as above, bf16 [n_pages, h_kv, page_size, head_dim]
+ *          kv_format PAD_KV_FP8:  codes uint8 [n_pages, h_kv, page_size, head_dim] and scales
+ *          uint8 [n_pages, h_kv, page_size], one scale for the head_dim codes of a token and head
+ *
+ * 8-bit groups: with a = max|x| over the head_dim values, k is the smallest integer with
+ * a <= 448 * 2^k, kept in [-120, 7]; a code is x / 2^k in e4m3, rounded to nearest even, values
+ * beyond +-448 (a > 57344) saturated; the scale byte is k + 127, or 0 for a group of zeros, or
+ * 255 for a group that holds a NaN or an infinity, which reads back as NaN throughout.  A power
+ * of two costs e4m3 no accuracy (its relative spacing is the same everywhere) and makes code
+ * times scale exact in bf16: what the attention multiplies is what pad_chunk_read returns.
+ * --------------------------------------------------------------------------- */
+typedef struct pad_chunk_t pad_chunk_t;
+#define PAD_KV_BF16 0
+#define PAD_KV_FP8 1
+
+/* Bytes of device workspace pad_chunk_plan needs (host arrays, same meaning as there); 0 on
+ * invalid arguments.  A caller that keeps one workspace for many steps takes the largest. */
+size_t pad_chunk_workspace_size(const pad_problem* prob, int32_t kv_format, int32_t n_videos,
+                                const int32_t* prefix_len, int32_t n_events, const int32_t* event_video,
+                                const int32_t* event_len, const int32_t* n_new);
+
+/* Plan one step.
+ *   prob           layer shape; flags: PAD_FLAG_PREFIX_MMA forces the warp-level kernel for
+ *                  everything, PAD_FLAG_PREFIX_TC the tcgen05 kernel, other prefix flags are refused
+ *   kv_format      PAD_KV_BF16 or PAD_KV_FP8 (the prefix is bf16 either way)
+ *   cache          page bookkeeping: every page that the new tokens start is taken from it, the
+ *                  lowest-numbered free ones, events in ascending order; NULL: page_table already
+ *                  lists the pages of all event_len + n_new tokens
+ *   n_videos, prefix_len, prefix_offset   as in pad_plan; n_videos 0: no event has a prefix
+ *   n_events, event_video                 as in pad_plan; event_video NULL when n_videos is 0
+ *   event_len      [n_events] host: private tokens of each branch before this step
+ *   n_new          [n_events] host: its new tokens, >= 0 (0: the branch only takes part in
+ *                  pad_chunk_read); event_len + n_new <= 2^30
+ *   page_table     [n_events * max_pages] device int32; may be NULL for a plan that is used for
+ *                  pad_draft_verify only
+ *   n_pages        pages of the pools; with a cache, 0 or its size
+ *   workspace      device, 256-byte aligned, zero-filled when allocated; holds the plan's work
+ *                  lists, its status word and the split-KV partial states, so plans that share one
+ *                  run one after the other
+ *   stream         the work lists are copied to the workspace on it, asynchronously, from a
+ *                  page-locked buffer of the library
+ * On any error nothing changes: no page is taken. */
+pad_status pad_chunk_plan(const pad_problem* prob, int32_t kv_format, pad_cache_state* cache, int32_t n_videos,
+                          const int32_t* prefix_len, const int64_t* prefix_offset, int32_t n_events,
+                          const int32_t* event_video, const int32_t* event_len, const int32_t* n_new,
+                          int32_t* page_table, int32_t max_pages, int32_t n_pages, void* workspace,
+                          size_t workspace_bytes, pad_stream_t stream, pad_chunk_t** out);
+
+typedef struct {
+  int64_t n_tokens;        /* N, the step's new tokens */
+  int64_t n_cached;        /* tokens that pad_chunk_read returns: sum of event_len + n_new */
+  int64_t n_drafts;        /* drafted tokens: sum of max(n_new - 1, 0) */
+  int64_t workspace_bytes; /* bytes of workspace this plan uses */
+  int64_t partial_rows;    /* split-KV partial rows among them (0: every row is finished in one piece) */
+  int32_t n_new_pages;
+  int32_t prefix_splits;   /* most key ranges that a video's prefix is split into */
+  int32_t page_splits;     /* most key ranges that a branch's own tokens are split into */
+  int32_t tc_items;        /* work items of the tcgen05 kernel, */
+  int32_t mma_items;       /* and of the warp-level kernel (times h_kv CTAs each) */
+} pad_chunk_info;
+pad_status pad_chunk_get_info(const pad_chunk_t* chunk, pad_chunk_info* info);
+/* The pages taken: for i < n_new_pages, page[i] became column column[i] of event[i]'s row of the
+ * page table (host arrays of n_new_pages entries). */
+pad_status pad_chunk_new_pages(const pad_chunk_t* chunk, int32_t* event, int32_t* column, int32_t* page);
+pad_status pad_chunk_destroy(pad_chunk_t* chunk);
+
+/* Write the new tokens into the pools, token i of event e at position event_len[e] + i, and the
+ * new page-table entries.  k_scale / v_scale: the scale pools, NULL for PAD_KV_BF16.  new_stride:
+ * elements from one token of k_new / v_new to the next, a multiple of 8, 0 = h_kv * head_dim.
+ * A page id outside the pool is skipped and recorded (pad_chunk_status). */
+pad_status pad_chunk_append(const pad_chunk_t* chunk, const void* k_new, const void* v_new, int64_t new_stride,
+                            void* k_pool, void* v_pool, uint8_t* k_scale, uint8_t* v_scale, pad_stream_t stream);
+
+/* Copy the cached tokens of every event, positions 0 .. event_len + n_new - 1, event after event,
+ * into k_out / v_out [n_cached, h_kv, head_dim] bf16 (exact in either format). */
+pad_status pad_chunk_read(const pad_chunk_t* chunk, const void* k_pool, const void* v_pool, const uint8_t* k_scale,
+                          const uint8_t* v_scale, void* k_out, void* v_out, pad_stream_t stream);
+
+/* Attention of the new tokens; their K/V are read from the pools (pad_chunk_append first).
+ * k_prefix / v_prefix may be NULL when no video has a prefix; lse may be NULL.  q_stride: elements
+ * from one token of q to the next, a multiple of 8, 0 = h_q * head_dim.  A page id outside the pool
+ * hides its tokens and is recorded; a row that then sees nothing gets 0 and an lse of -infinity.  What
+ * lies in cache slots past a branch's last token is never used in arithmetic. */
+pad_status pad_chunk_attn(const pad_chunk_t* chunk, const void* q, int64_t q_stride, const void* k_prefix,
+                          const void* v_prefix, const void* k_pool, const void* v_pool, const uint8_t* k_scale,
+                          const uint8_t* v_scale, void* out, float* lse, pad_stream_t stream);
+
+/* Verify drafted tokens: event e has n_new[e] - 1 drafted tokens (none where n_new is 0 or 1), its chunk
+ * being its last accepted token followed by them.
+ *   dtype     0 = fp32, 1 = bf16 probabilities
+ *   p         [N, vocab] the target's probabilities after each chunk token, row stride p_stride elements
+ *             (0 = vocab)
+ *   q         [n_drafts, vocab] the probabilities each drafted token was drawn from, q_stride likewise
+ *   draft     [n_drafts] int32; u_accept [n_drafts], u_pick [n_events] fp32 in [0, 1)
+ *   accepted  [n_events] int32: how many drafted tokens are kept: token i while u_i * q_i(x_i) < p_i(x_i)
+ *             (a product rounded to fp32), none after the first that fails
+ *   token     [n_events] int32: the token after them, drawn with u_pick from max(p - q, 0) at the rejected
+ *             position, or from p after a whole accepted draft (or where that difference has no
+ *             weight left); -1 where p has none, and for an event without new tokens
+ * Weights are floor(2^38 min(r, 1)) as integers, a NaN counting as 0, and the token is the first whose
+ * running sum exceeds floor(m S / 2^24), S the sum of the weights, m = floor(2^24 u_pick): integer sums, so
+ * that the result does not depend on the order they are formed in.  A drafted token outside
+ * [0, vocab) is rejected and recorded (pad_chunk_status).  vocab <= 2^24. */
+pad_status pad_draft_verify(const pad_chunk_t* chunk, int32_t vocab, int32_t dtype, const void* p, int64_t p_stride,
+                            const void* q, int64_t q_stride, const int32_t* draft, const float* u_accept,
+                            const float* u_pick, int32_t* accepted, int32_t* token, pad_stream_t stream);
+
+/* After verification (host): event_len[e] becomes the planned length + min(accepted[e] + 1, n_new[e]),
+ * and the pages this plan took that hold none of those tokens go back to `cache` (which may be NULL
+ * for a plan without one).  accepted [n_events] host, each >= 0; NULL keeps every new token.  The device page
+ * table keeps its entries; they are written again when the pages are next taken.
+ * PAD_ERR_INVALID_ARG, changing nothing, for a bad count or a page that is not in use. */
+pad_status pad_chunk_commit(pad_chunk_t* chunk, pad_cache_state* cache, const int32_t* accepted, int32_t* event_len);
+
+/* Synchronise the stream and read the plan's device status word, as pad_device_status does. */
+pad_status pad_chunk_status(const pad_chunk_t* chunk, pad_stream_t stream);
+
 /* Synchronise the stream and read the plan's device status word:
  * PAD_OK, PAD_ERR_DEVICE_BOUNDS or PAD_ERR_DEVICE_TIMEOUT.  For a plan without a workspace
  * the word is the static scratch array's (pad_event_decode_attn_static); PAD_OK if no call

@@ -30,6 +30,8 @@ G_ALL = 0
 G_SELF = 1
 BRANCH_OWN = 0
 BRANCH_CAUSAL = 1
+KV_BF16 = 0
+KV_FP8 = 1
 
 
 class PadError(RuntimeError):
@@ -51,6 +53,12 @@ class PlanInfo(ctypes.Structure):
                 ("param_descriptor_bytes", c_int32), ("fused_tail", c_int32),
                 ("generation", ctypes.c_uint64), ("prefix_ctas", c_int32), ("max_split_tiles", c_int32),
                 ("merge_first", c_int32)]
+
+
+class ChunkInfo(ctypes.Structure):
+    _fields_ = [("n_tokens", c_int64), ("n_cached", c_int64), ("n_drafts", c_int64), ("workspace_bytes", c_int64),
+                ("partial_rows", c_int64), ("n_new_pages", c_int32), ("prefix_splits", c_int32),
+                ("page_splits", c_int32), ("tc_items", c_int32), ("mma_items", c_int32)]
 
 
 _I32P = POINTER(c_int32)
@@ -101,6 +109,19 @@ _SIGNATURES = {
     "pad_attn_aggregate": (c_int32, [c_void_p, c_int64, c_int32, c_void_p, c_void_p, c_int32, c_void_p, c_int32,
                                      c_void_p, c_void_p, ctypes.c_size_t, c_void_p, c_void_p]),
     "pad_attn_aggregate_workspace_size": (ctypes.c_size_t, [c_int64, c_int32, c_int32]),
+    "pad_chunk_workspace_size": (c_size_t, [POINTER(Problem), c_int32, c_int32, _I32P, c_int32, _I32P, _I32P, _I32P]),
+    "pad_chunk_plan": (c_int32, [POINTER(Problem), c_int32, c_void_p, c_int32, _I32P, _I64P, c_int32, _I32P, _I32P, _I32P,
+                                 c_void_p, c_int32, c_int32, c_void_p, c_size_t, c_void_p, POINTER(c_void_p)]),
+    "pad_chunk_get_info": (c_int32, [c_void_p, POINTER(ChunkInfo)]),
+    "pad_chunk_new_pages": (c_int32, [c_void_p, _I32P, _I32P, _I32P]),
+    "pad_chunk_destroy": (c_int32, [c_void_p]),
+    "pad_chunk_append": (c_int32, [c_void_p, c_void_p, c_void_p, c_int64, c_void_p, c_void_p, c_void_p, c_void_p,
+                                   c_void_p]),
+    "pad_chunk_read": (c_int32, [c_void_p] * 8),
+    "pad_chunk_attn": (c_int32, [c_void_p, c_void_p, c_int64] + [c_void_p] * 9),
+    "pad_draft_verify": (c_int32, [c_void_p, c_int32, c_int32, c_void_p, c_int64, c_void_p, c_int64] + [c_void_p] * 6),
+    "pad_chunk_commit": (c_int32, [c_void_p, c_void_p, _I32P, _I32P]),
+    "pad_chunk_status": (c_int32, [c_void_p, c_void_p]),
     "pad_device_status": (c_int32, [c_void_p, c_void_p]),
     "pad_last_error": (ctypes.c_char_p, []),
     "pad_status_string": (ctypes.c_char_p, [c_int32]),
@@ -398,6 +419,199 @@ def pad_event_decode_attn_static(plan: Plan, q, k_prefix, v_prefix, k_pool, v_po
 
 def pad_device_status(plan: Plan, stream=None):
     _check(lib().pad_device_status(plan.handle, _stream(stream)))
+
+
+def _rows(t):
+    """Device pointer and row stride (elements) of a tensor whose rows are contiguous (None -> NULL, packed)."""
+    if t is None:
+        return None, 0
+    want = 1
+    for n, st in zip(reversed(t.shape[1:]), reversed(t.stride()[1:])):
+        if n != 1 and st != want:
+            raise ValueError("the rows of tensors passed to libpad must be contiguous")
+        want *= n
+    return c_void_p(t.data_ptr()), (int(t.stride(0)) if t.shape[0] > 1 else 0)
+
+
+def _shaped(t, name, shape, dtype):
+    """A tensor's shape and type checked against what the plan says."""
+    if t is not None and (tuple(t.shape) != tuple(shape) or t.dtype != dtype):
+        raise ValueError(f"{name}: {tuple(t.shape)} {t.dtype}, expected {tuple(shape)} {dtype}")
+
+
+class ChunkPlan:
+    """A planned step of several tokens per branch (pad_chunk_t)."""
+
+    def __init__(self, handle, problem, n_events, kv_format, n_pages, keep):
+        self._h = handle
+        self.problem = problem
+        self.n_events = n_events
+        self.kv_format = kv_format
+        self.n_pages = n_pages
+        self._keep = keep  # device memory that the plan points to
+        i = self.info()
+        self.n_tokens, self.n_cached, self.n_drafts = i["n_tokens"], i["n_cached"], i["n_drafts"]
+
+    @property
+    def handle(self):
+        return self._h
+
+    def info(self) -> dict:
+        i = ChunkInfo()
+        _check(lib().pad_chunk_get_info(self._h, ctypes.byref(i)))
+        return {f: getattr(i, f) for f, _ in ChunkInfo._fields_}
+
+    def new_pages(self):
+        """(event, column, page) of every page the plan took."""
+        n = self.info()["n_new_pages"]
+        out = np.zeros((3, n), dtype=np.int32)
+        _check(lib().pad_chunk_new_pages(self._h, *(row.ctypes.data_as(_I32P) for row in out)))
+        return out[0], out[1], out[2]
+
+    def commit(self, cache, accepted=None) -> np.ndarray:
+        """The branches' lengths after verification (pad_chunk_commit); pages past them go back to ``cache``."""
+        out = np.zeros(self.n_events, dtype=np.int32)
+        acc = accp = None
+        if accepted is not None:
+            acc, accp = _i32(accepted)
+            if acc.size != self.n_events:
+                raise ValueError(f"accepted has {acc.size} entries, the plan {self.n_events} events")
+        _check(lib().pad_chunk_commit(self._h, None if cache is None else cache.handle, accp,
+                                      out.ctypes.data_as(_I32P)))
+        return out
+
+    def check_pools(self, k_pool, v_pool, k_scale, v_scale):
+        import torch
+        p = self.problem
+        shape = (self.n_pages, p.h_kv, p.page_size, p.head_dim)
+        dt = torch.uint8 if self.kv_format == KV_FP8 else torch.bfloat16
+        for name, pool, scale in (("k", k_pool, k_scale), ("v", v_pool, v_scale)):
+            _shaped(pool, name + "_pool", shape, dt)
+            _shaped(scale, name + "_scale", shape[:3], torch.uint8)
+
+    def destroy(self):
+        if self._h is not None and _lib is not None:
+            _lib.pad_chunk_destroy(self._h)
+            self._h = None
+
+    def __del__(self):
+        self.destroy()
+
+
+def _batch(prefix_len, event_video, event_len, n_new):
+    el, elp = _i32(event_len)
+    nn, nnp = _i32(n_new)
+    if el.size != nn.size:
+        raise ValueError(f"event_len has {el.size} entries, n_new {nn.size}")
+    if prefix_len is None:
+        return 0, None, None, el.size, elp, nnp, (el, nn)
+    pl, plp = _i32(prefix_len)
+    ev, evp = _i32(event_video)
+    if ev.size != el.size:
+        raise ValueError(f"event_video has {ev.size} entries, event_len {el.size}")
+    return int(pl.size), plp, evp, int(el.size), elp, nnp, (el, nn, pl, ev)
+
+
+def pad_chunk_workspace_size(problem: Problem, prefix_len, event_video, event_len, n_new, kv_format=KV_BF16) -> int:
+    nv, plp, evp, ne, elp, nnp, _keep = _batch(prefix_len, event_video, event_len, n_new)
+    n = int(lib().pad_chunk_workspace_size(ctypes.byref(problem), int(kv_format), nv, plp, ne, evp, elp, nnp))
+    if n == 0:
+        raise PadError(1, lib().pad_last_error().decode(errors="replace"))
+    return n
+
+
+def pad_chunk_plan(problem: Problem, cache, prefix_len, event_video, event_len, n_new, page_table=None,
+                   n_pages: int = 0, kv_format=KV_BF16, workspace=None, prefix_offset=None, stream=None) -> ChunkPlan:
+    """Plan a step of n_new[e] tokens per branch (host, and one copy of the work lists to the workspace).
+    ``cache`` None: page_table already lists every page.  ``prefix_len`` None: no prefixes.  workspace=None
+    plans on the host only."""
+    nv, plp, evp, ne, elp, nnp, _keep = _batch(prefix_len, event_video, event_len, n_new)
+    po = None
+    if prefix_offset is not None:
+        po_arr = np.ascontiguousarray(prefix_offset, dtype=np.int64)
+        po = po_arr.ctypes.data_as(_I64P)
+    max_pages = 0
+    if page_table is not None:
+        import torch
+        if page_table.dim() != 2 or page_table.shape[0] != ne or page_table.dtype != torch.int32:
+            raise ValueError(f"page_table: {tuple(page_table.shape)} {page_table.dtype}, expected [{ne}, max_pages] int32")
+        max_pages = int(page_table.shape[1])
+    if cache is not None and n_pages == 0:
+        n_pages = cache.n_pages
+    ws_bytes = int(workspace.numel() * workspace.element_size()) if workspace is not None else 0
+    strm = _stream(stream) if workspace is not None else c_void_p(0)
+    h = c_void_p()
+    _check(lib().pad_chunk_plan(ctypes.byref(problem), int(kv_format), None if cache is None else cache.handle, nv, plp,
+                                po, ne, evp, elp, nnp, _ptr(page_table), max_pages, int(n_pages), _ptr(workspace),
+                                ws_bytes, strm, ctypes.byref(h)))
+    return ChunkPlan(h, problem, ne, int(kv_format), int(n_pages), (page_table, workspace))
+
+
+def pad_chunk_append(plan: ChunkPlan, k_new, v_new, k_pool, v_pool, k_scale=None, v_scale=None, stream=None):
+    """Write the new tokens' K/V into the branches' pages (quantised in an 8-bit cache)."""
+    import torch
+    p = plan.problem
+    shape = (plan.n_tokens, p.h_kv, p.head_dim)
+    _shaped(k_new, "k_new", shape, torch.bfloat16)
+    _shaped(v_new, "v_new", shape, torch.bfloat16)
+    plan.check_pools(k_pool, v_pool, k_scale, v_scale)
+    kp, ks = _rows(k_new)
+    vp, vs = _rows(v_new)
+    if ks != vs:
+        raise ValueError("k_new and v_new must have the same token stride")
+    _check(lib().pad_chunk_append(plan.handle, kp, vp, ks, _ptr(k_pool), _ptr(v_pool), _ptr(k_scale), _ptr(v_scale),
+                                  _stream(stream)))
+
+
+def pad_chunk_read(plan: ChunkPlan, k_pool, v_pool, k_out, v_out, k_scale=None, v_scale=None, stream=None):
+    """Copy every branch's cached tokens out as contiguous bf16 [n_cached, h_kv, head_dim]."""
+    import torch
+    p = plan.problem
+    plan.check_pools(k_pool, v_pool, k_scale, v_scale)
+    shape = (plan.n_cached, p.h_kv, p.head_dim)
+    _shaped(k_out, "k_out", shape, torch.bfloat16)
+    _shaped(v_out, "v_out", shape, torch.bfloat16)
+    _check(lib().pad_chunk_read(plan.handle, _ptr(k_pool), _ptr(v_pool), _ptr(k_scale), _ptr(v_scale), _ptr(k_out),
+                                _ptr(v_out), _stream(stream)))
+
+
+def pad_chunk_attn(plan: ChunkPlan, q, k_prefix, v_prefix, k_pool, v_pool, out, lse=None, k_scale=None, v_scale=None,
+                   stream=None):
+    """Attention of the step's new tokens over their video's prefix and their branch's cached tokens."""
+    import torch
+    p = plan.problem
+    shape = (plan.n_tokens, p.h_q, p.head_dim)
+    _shaped(q, "q", shape, torch.bfloat16)
+    _shaped(out, "out", shape, torch.bfloat16 if p.out_dtype == 1 else torch.float32)
+    _shaped(lse, "lse", shape[:2], torch.float32)
+    plan.check_pools(k_pool, v_pool, k_scale, v_scale)
+    qp, qs = _rows(q)
+    _check(lib().pad_chunk_attn(plan.handle, qp, qs, _ptr(k_prefix), _ptr(v_prefix), _ptr(k_pool), _ptr(v_pool),
+                                _ptr(k_scale), _ptr(v_scale), _ptr(out), _ptr(lse), _stream(stream)))
+
+
+def pad_draft_verify(plan: ChunkPlan, p, q, draft, u_accept, u_pick, accepted, token, stream=None):
+    """Accept or reject the step's drafted tokens against the target's probabilities p [n_tokens, vocab] and
+    the draft's q [n_drafts, vocab] (fp32 or bf16), and draw each branch's next token."""
+    import torch
+    if p.dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError(f"p: {p.dtype}, expected float32 or bfloat16")
+    vocab = int(p.shape[1])
+    _shaped(p, "p", (plan.n_tokens, vocab), p.dtype)
+    _shaped(q, "q", (plan.n_drafts, vocab), p.dtype)
+    _shaped(draft, "draft", (plan.n_drafts,), torch.int32)
+    _shaped(u_accept, "u_accept", (plan.n_drafts,), torch.float32)
+    _shaped(u_pick, "u_pick", (plan.n_events,), torch.float32)
+    _shaped(accepted, "accepted", (plan.n_events,), torch.int32)
+    _shaped(token, "token", (plan.n_events,), torch.int32)
+    pp, ps = _rows(p)
+    qp, qs = _rows(q)
+    _check(lib().pad_draft_verify(plan.handle, vocab, 1 if p.dtype == torch.bfloat16 else 0, pp, ps, qp, qs, _ptr(draft),
+                                  _ptr(u_accept), _ptr(u_pick), _ptr(accepted), _ptr(token), _stream(stream)))
+
+
+def pad_chunk_status(plan: ChunkPlan, stream=None):
+    _check(lib().pad_chunk_status(plan.handle, _stream(stream)))
 
 
 def pad_timing_enable(max_launches: int):

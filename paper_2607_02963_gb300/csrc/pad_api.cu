@@ -664,6 +664,40 @@ struct pad_plan_t {
   ~pad_plan_t() { image_release(image); }
 };
 
+namespace pad {
+pad_status api_fail(pad_status st, const char* fmt, ...) {
+  char buf[512];
+  va_list ap;
+  va_start(ap, fmt);
+  vsnprintf(buf, sizeof(buf), fmt, ap);
+  va_end(ap);
+  return fail(st, "%s", buf);
+}
+pad_status api_check_problem(const pad_problem* prob) { return check_problem(prob); }
+int api_num_sms() { return query_num_sms(); }
+uint64_t api_next_generation() { return next_generation(); }
+int32_t api_next_free_page(const pad_cache_state* cache, int32_t from) { return cache->next_free(from); }
+void api_take_page(pad_cache_state* cache, int32_t page) {
+  cache->set(page, true);
+  --cache->free_count;
+}
+// (a copy from pageable memory would wait for all that the stream holds)
+cudaError_t api_copy_in(void* dst, const void* src, size_t n, cudaStream_t s) {
+  PlanImage* img = nullptr;
+  cudaError_t e = image_acquire(n, &img);
+  if (e != cudaSuccess) return e;
+  memcpy(img->host, src, n);
+  e = cudaMemcpyAsync(dst, img->host, n, cudaMemcpyHostToDevice, s);
+  if (e == cudaSuccess) {
+    e = cudaEventRecord(img->done, s);
+    img->recorded = e == cudaSuccess;
+    if (e != cudaSuccess) cudaStreamSynchronize(s);
+  }
+  image_release(img);
+  return e;
+}
+}  // namespace pad
+
 extern "C" {
 
 const char* pad_last_error(void) { return g_last_error.c_str(); }

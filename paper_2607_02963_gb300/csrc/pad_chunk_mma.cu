@@ -1,0 +1,566 @@
+// Attention of a step's chunk tokens on the warp-level tensor-core path (mma.sync): for few query rows
+// per (event, kv-head), and the join of split key ranges for both paths.
+//
+// o_t = sum_j softmax_j(scale q_t . k_j) v_j over the keys j that token t sees.  An item is a range of
+// keys for up to 32 rows (chunk tokens x the G query heads of a kv-head); a CTA of four warps takes an
+// item and a kv-head.  Each warp takes every fourth block of 16 keys with rows of its own running
+// maximum, sum and O (no meeting inside the loop), brought in by cp.async through a ring of its own;
+// the four states are joined through shared memory at the end, and written to out, or to the partial
+// states that chunk_merge_kernel joins, when the item is one of several of its rows.
+//
+// 8-bit caches: the codes are staged as they are (half the bytes in flight buys twice the keys) and
+// widened to bf16 in the fragments: a K word holds four dimensions of a key (which Q's fragments follow:
+// the order of a sum's terms is free), a V word four columns of a key, so that words of two keys give the
+// pairs P.V wants without a transpose.  Code times scale is exact in bf16, so the products are those
+// of the values that pad_chunk_read returns.
+//
+// P goes into P.V rounded to bf16 (2^-8 of each weight at most, as in every kernel of this library); the row sum is that of the unrounded fp32 weights, and all states are fp32.
+#include <cuda_bf16.h>
+#include <algorithm>
+#include <cstdint>
+
+#include "pad_chunk.h"
+#include "pad_tc_common.cuh"
+
+namespace pad {
+
+namespace {
+
+using tc::ex2;
+using tc::pack_bf16;
+using tc::smem_u32;
+
+constexpr int kWarps = 4;
+constexpr int kThreads = 32 * kWarps;
+constexpr int kBlk = 16;  // keys of a block
+constexpr float kNegInf = -__builtin_huge_valf();
+constexpr float kLn2 = 0.69314718055994531f;
+
+template <int D, bool FP8>
+struct Ring {
+  static constexpr int kRow = FP8 ? D : 2 * D;            // bytes of a key
+  static constexpr int kPitch = FP8 ? D + 16 : 2 * D;     // (8 bits: rows 4 banks apart; bf16: swizzled)
+  static constexpr int kScale = 2 * kBlk * kPitch;        // scale bytes: 16 of K, 16 of V
+  static constexpr int kMask = kScale + 32;               // which keys are there
+  static constexpr int kStage = kScale + 48;
+  static constexpr int kStages = FP8 ? 4 : 3;
+  static constexpr int kWarpBytes = kStages * kStage;
+};
+
+template <int D, bool FP8, int MT>
+constexpr int smem_bytes() {
+  constexpr int ring = kWarps * Ring<D, FP8>::kWarpBytes;
+  constexpr int join = kWarps * 16 * MT * (D + 2) * 4;
+  return ring > join ? ring : join;
+}
+
+__device__ __forceinline__ void cp16(uint32_t dst, const void* src, uint32_t n) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
+}
+__device__ __forceinline__ void cp4(uint32_t dst, const void* src, uint32_t n) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
+}
+__device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t a) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(a) : "memory");
+}
+__device__ __forceinline__ void ldsm4t(uint32_t (&r)[4], uint32_t a) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(a) : "memory");
+}
+__device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t lds32(uint32_t a) {
+  uint32_t v;
+  asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
+  return v;
+}
+__device__ __forceinline__ uint32_t lds8(uint32_t a) {
+  uint32_t v;
+  asm volatile("ld.shared.u8 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
+  return v;
+}
+__device__ __forceinline__ bool not_finite2(uint32_t v) {  // either half's exponent is all ones
+  return (v & 0x7f80u) == 0x7f80u || (v & 0x7f800000u) == 0x7f800000u;
+}
+
+// FP8: of paged items; items of the prefix take the bf16 instance.
+template <int D, bool FP8, int MT>
+__global__ void __launch_bounds__(kThreads) chunk_mma_kernel(const __grid_constant__ ChunkParams p,
+                                                             const ChunkItem* __restrict__ items) {
+  using R = Ring<D, FP8>;
+  constexpr int kRows = 16 * MT;
+  extern __shared__ __align__(128) uint8_t smem[];
+  const ChunkItem it = items[blockIdx.x / p.h_kv];
+  const int h = (int)blockIdx.x % p.h_kv, G = p.group;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t4 = lane & 3;
+  const uint32_t ring = smem_u32(smem) + warp * R::kWarpBytes;
+  const uint8_t* ring_ptr = smem + warp * R::kWarpBytes;
+  const int n_rows = it.ntok * G;
+
+  const int n_blocks = it.key1 > it.key0 ? (it.key1 - it.key0 + kBlk - 1) / kBlk : 0;
+  const int mine = n_blocks > warp ? (n_blocks - warp + kWarps - 1) / kWarps : 0;
+  const int32_t* table = p.page_table + (it.paged ? it.src * p.max_pages : 0);
+  const uint8_t* kb = static_cast<const uint8_t*>(it.paged ? p.k_pool : p.k_prefix);
+  const uint8_t* vb = static_cast<const uint8_t*>(it.paged ? p.v_pool : p.v_prefix);
+
+  // page of this lane's key (lanes 0-15, one key each) of the warp's i-th block
+  auto page_of = [&](int i) -> int {
+    const int key = it.key0 + (warp + kWarps * i) * kBlk + lane;
+    return it.paged && i < mine && lane < kBlk && key < it.key1 ? __ldg(table + (key >> p.page_shift)) : 0;
+  };
+  auto issue = [&](int i, int page) {
+    if (i >= mine) return;
+    const uint32_t st = ring + (i % R::kStages) * R::kStage;
+    const int k0 = it.key0 + (warp + kWarps * i) * kBlk, key = k0 + (lane & 15);
+    bool ok = key < it.key1;
+    if (it.paged && ok && lane < kBlk && (unsigned)page >= (unsigned)p.n_pages) {
+      ok = false;
+      pad_set_error(p.header, p.gen, PAD_ERR_DEVICE_BOUNDS, (int)it.src, key >> p.page_shift, page);
+    }
+    const uint32_t there = __ballot_sync(0xffffffffu, ok) & 0xffffu;
+    // first slot (token and head) of the lane's key
+    const int64_t slot = !ok ? 0 : it.paged ? ((int64_t)page * p.h_kv + h) * p.page_size + (key & (p.page_size - 1))
+                                            : (it.src + key) * p.h_kv + h;
+    constexpr int CH = R::kRow / 16, kIter = kBlk * CH / 32;
+#pragma unroll
+    for (int j = 0; j < kIter; ++j) {
+      const int row = (j * 32 + lane) / CH, c = (j * 32 + lane) % CH;
+      const int64_t off = __shfl_sync(0xffffffffu, slot, row) * R::kRow + 16 * c;
+      const uint32_t n = (there >> row) & 1u ? 16u : 0u;
+      const uint32_t dst = st + row * R::kPitch + 16 * (FP8 ? c : c ^ (row & 7));
+      cp16(dst, kb + off, n);
+      cp16(dst + kBlk * R::kPitch, vb + off, n);
+    }
+    if (FP8) {  // four keys' scale bytes each (they share a page)
+      const int64_t s4 = __shfl_sync(0xffffffffu, slot, 4 * (lane & 3));
+      if (lane < 8) cp4(st + R::kScale + 4 * lane, (lane < 4 ? p.k_scale : p.v_scale) + (s4 & ~(int64_t)3), (there >> (4 * (lane & 3))) & 1u ? 4u : 0u);
+    }
+    if (lane == 0) *reinterpret_cast<uint32_t*>(smem + (st - smem_u32(smem)) + R::kMask) = there;
+  };
+
+  int page = page_of(0);
+#pragma unroll
+  for (int i = 0; i < R::kStages - 1; ++i) {
+    const int next = page_of(i + 1);
+    issue(i, page);
+    asm volatile("cp.async.commit_group;" ::: "memory");
+    page = next;
+  }
+
+  // Q fragments (rows g and g + 8 of each 16-row group), in the order of K's
+  uint32_t qf[MT][D / 16][4];
+#pragma unroll
+  for (int m = 0; m < MT; ++m)
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int r = 16 * m + 8 * u + g;
+      const bool on = r < n_rows;
+      const __nv_bfloat16* src = p.q + (on ? (it.tok0 + r / G) * p.q_stride + (int64_t)(h * G + r % G) * D : 0);
+#pragma unroll
+      for (int j = 0; j < D / 16; ++j) {
+        uint32_t a = 0u, b = 0u;
+        if (on) {
+          if (FP8) {
+            const uint2 x = __ldg(reinterpret_cast<const uint2*>(src + 16 * j + 4 * t4));
+            a = __byte_perm(x.x, x.y, 0x5410);
+            b = __byte_perm(x.x, x.y, 0x7632);
+          } else {
+            a = __ldg(reinterpret_cast<const uint32_t*>(src + 16 * j + 2 * t4));
+            b = __ldg(reinterpret_cast<const uint32_t*>(src + 16 * j + 2 * t4 + 8));
+          }
+        }
+        qf[m][j][u] = a;
+        qf[m][j][2 + u] = b;
+      }
+    }
+  // keys that each of the thread's rows sees
+  int lim[MT][2];
+#pragma unroll
+  for (int m = 0; m < MT; ++m)
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int r = 16 * m + 8 * u + g;
+      lim[m][u] = r < n_rows ? min(it.lim0 + (it.paged ? r / G : 0), it.key1) : 0;
+    }
+
+  float o[MT][D / 8][4], mx[MT][2], l[MT][2];
+#pragma unroll
+  for (int m = 0; m < MT; ++m) {
+#pragma unroll
+    for (int i = 0; i < D / 8; ++i)
+#pragma unroll
+      for (int u = 0; u < 4; ++u) o[m][i][u] = 0.f;
+    mx[m][0] = mx[m][1] = kNegInf;
+    l[m][0] = l[m][1] = 0.f;
+  }
+
+#pragma unroll 1
+  for (int i = 0; i < mine; ++i) {
+    {
+      const int next = page_of(i + R::kStages);
+      issue(i + R::kStages - 1, page);
+      asm volatile("cp.async.commit_group;" ::: "memory");
+      page = next;
+    }
+    asm volatile("cp.async.wait_group %0;" ::"n"(R::kStages - 1) : "memory");
+    __syncwarp();
+    const uint32_t st = ring + (i % R::kStages) * R::kStage;
+    const uint32_t sv = st + kBlk * R::kPitch;
+    const uint32_t there = *reinterpret_cast<const uint32_t*>(ring_ptr + (i % R::kStages) * R::kStage + R::kMask);
+    const int k0 = it.key0 + (warp + kWarps * i) * kBlk;
+
+    float s[MT][2][4];
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int u = 0; u < 4; ++u) s[m][b][u] = 0.f;
+    if (FP8) {
+      uint32_t mult[2];
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        const int key = 8 * b + g;
+        const uint32_t x = (there >> key) & 1u ? scale_mult(lds8(st + R::kScale + key)) : 0u;
+        mult[b] = x | (x << 16);
+      }
+#pragma unroll
+      for (int j = 0; j < D / 16; ++j)
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+          const uint32_t w = lds32(st + (8 * b + g) * R::kPitch + 16 * j + 4 * t4);
+          const uint32_t b0 = e4m3_pair(w << 8, mult[b]), b1 = e4m3_pair(w, mult[b]);
+#pragma unroll
+          for (int m = 0; m < MT; ++m) mma(s[m][b], qf[m][j], b0, b1);
+        }
+    } else {
+#pragma unroll
+      for (int j = 0; j < D / 16; ++j) {
+        uint32_t kf[4];
+        const int row = (lane & 7) + ((lane >> 4) << 3), c = 2 * j + ((lane >> 3) & 1);
+        ldsm4(kf, st + row * R::kPitch + 16 * (c ^ (row & 7)));
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+          mma(s[m][0], qf[m][j], kf[0], kf[1]);
+          mma(s[m][1], qf[m][j], kf[2], kf[3]);
+        }
+      }
+    }
+
+    uint32_t pf[MT][4];
+    bool hidden = false;  // some row here does not see some key of the block
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const int n = lim[m][u] - k0;  // keys of the block that the row sees, if they are there
+        uint32_t see = n >= kBlk ? 0xffffu : n <= 0 ? 0u : (1u << n) - 1u;
+        hidden |= see != 0xffffu && 16 * m + 8 * u + g < n_rows;
+        see &= there;
+        float top = kNegInf;
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int v = 0; v < 2; ++v) {
+            float& x = s[m][b][2 * u + v];
+            x = (see >> (8 * b + 2 * t4 + v)) & 1u ? x * p.scale_log2 : kNegInf;
+            top = fmaxf(top, x);
+          }
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+        const float m_new = fmaxf(mx[m][u], top), base = m_new == kNegInf ? 0.f : m_new;
+        const float alpha = ex2(mx[m][u] - base);
+        mx[m][u] = m_new;
+        float sum = 0.f;
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+          const float a = ex2(s[m][b][2 * u] - base), c = ex2(s[m][b][2 * u + 1] - base);
+          sum += a + c;
+          pf[m][2 * b + u] = pack_bf16(a, c);
+        }
+        l[m][u] = l[m][u] * alpha + sum;
+#pragma unroll
+        for (int c = 0; c < D / 8; ++c) {
+          o[m][c][2 * u] *= alpha;
+          o[m][c][2 * u + 1] *= alpha;
+        }
+      }
+
+    // P.V.  A weight of 0 times a NaN or an infinity is not 0: where a row does not see all of the block
+    // and its values are not all finite, the products are formed one by one instead.
+    const bool any_hidden = __any_sync(0xffffffffu, hidden);
+    if (FP8) {
+      uint32_t mult[2];
+      bool bad = false;
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        const int key = 8 * b + 2 * t4;
+        const uint32_t x = (there >> key) & 1u ? scale_mult(lds8(st + R::kScale + 16 + key)) : 0u;
+        const uint32_t y = (there >> (key + 1)) & 1u ? scale_mult(lds8(st + R::kScale + 17 + key)) : 0u;
+        mult[b] = x | (y << 16);
+        bad |= not_finite2(mult[b]);
+      }
+      if (!(any_hidden && __any_sync(0xffffffffu, bad))) {
+#pragma unroll
+        for (int q = 0; q < D / 32; ++q) {
+          const uint32_t a = sv + 2 * t4 * R::kPitch + 32 * q + 4 * g;
+          const uint32_t w0 = lds32(a), w1 = lds32(a + R::kPitch), w2 = lds32(a + 8 * R::kPitch), w3 = lds32(a + 9 * R::kPitch);
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {  // column 32 q + 4 g + r: column g of O tile 4 q + r
+            const uint32_t sel = (uint32_t)(r << 4) | ((uint32_t)(4 + r) << 12);  // (the low bytes are masked out)
+            const uint32_t b0 = e4m3_pair(__byte_perm(w0, w1, sel), mult[0]), b1 = e4m3_pair(__byte_perm(w2, w3, sel), mult[1]);
+#pragma unroll
+            for (int m = 0; m < MT; ++m) mma(o[m][4 * q + r], pf[m], b0, b1);
+          }
+        }
+      } else {
+        // (only whole groups are NaN: every column of such a key)
+#pragma unroll 1
+        for (int key = 0; key < kBlk; ++key) {
+          const uint32_t x = (there >> key) & 1u ? scale_mult(lds8(st + R::kScale + 16 + key)) : 0u;
+          const int src = 4 * g + ((key & 7) >> 1);
+#pragma unroll
+          for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+              const uint32_t w = __shfl_sync(0xffffffffu, key < 8 ? pf[m][u] : pf[m][2 + u], src);
+              const float pw = __uint_as_float(key & 1 ? w & 0xffff0000u : w << 16);
+              if (k0 + key >= lim[m][u] || !((there >> key) & 1u)) continue;
+#pragma unroll
+              for (int c = 0; c < D / 8; ++c)
+#pragma unroll
+                for (int v = 0; v < 2; ++v) {
+                  // accumulator column 2 t + v of tile c: column 32 (c / 4) + 4 (2 t + v) + c % 4
+                  const uint32_t code = lds8(sv + key * R::kPitch + 32 * (c / 4) + 4 * (2 * t4 + v) + c % 4);
+                  o[m][c][2 * u + v] = fmaf(pw, __uint_as_float(e4m3_pair(code << 8, x) << 16), o[m][c][2 * u + v]);
+                }
+            }
+        }
+      }
+    } else {
+      auto load_v = [&](uint32_t (&vf)[4], int c) {  // O tiles c and c + 1
+        const int row = (lane & 7) + (((lane >> 3) & 1) << 3), ch = c + (lane >> 4);
+        ldsm4t(vf, sv + row * R::kPitch + 16 * (ch ^ (row & 7)));
+      };
+      bool bad = false;
+      if (any_hidden) {
+#pragma unroll
+        for (int c = 0; c < D / 8; c += 2) {
+          uint32_t vf[4];
+          load_v(vf, c);
+          bad |= not_finite2(vf[0]) | not_finite2(vf[1]) | not_finite2(vf[2]) | not_finite2(vf[3]);
+        }
+        bad = __any_sync(0xffffffffu, bad);
+      }
+      if (!bad) {
+#pragma unroll
+        for (int c = 0; c < D / 8; c += 2) {
+          uint32_t vf[4];
+          load_v(vf, c);
+#pragma unroll
+          for (int m = 0; m < MT; ++m) {
+            mma(o[m][c], pf[m], vf[0], vf[1]);
+            mma(o[m][c + 1], pf[m], vf[2], vf[3]);
+          }
+        }
+      } else {
+#pragma unroll 1
+        for (int key = 0; key < kBlk; ++key) {
+          const int src = 4 * g + ((key & 7) >> 1);
+#pragma unroll
+          for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+              const uint32_t w = __shfl_sync(0xffffffffu, key < 8 ? pf[m][u] : pf[m][2 + u], src);
+              const float pw = __uint_as_float(key & 1 ? w & 0xffff0000u : w << 16);
+              if (k0 + key >= lim[m][u] || !((there >> key) & 1u)) continue;
+#pragma unroll
+              for (int c = 0; c < D / 8; ++c) {
+                const uint32_t v2 = lds32(sv + key * R::kPitch + 16 * (c ^ (key & 7)) + 4 * t4);
+                o[m][c][2 * u] = fmaf(pw, __uint_as_float(v2 << 16), o[m][c][2 * u]);
+                o[m][c][2 * u + 1] = fmaf(pw, __uint_as_float(v2 & 0xffff0000u), o[m][c][2 * u + 1]);
+              }
+            }
+        }
+      }
+    }
+    __syncwarp();
+  }
+  asm volatile("cp.async.wait_all;" ::: "memory");
+
+  // The four warps' states through shared memory: O rows, then (m, l).
+#pragma unroll
+  for (int m = 0; m < MT; ++m)
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      l[m][u] += __shfl_xor_sync(0xffffffffu, l[m][u], 1);
+      l[m][u] += __shfl_xor_sync(0xffffffffu, l[m][u], 2);
+    }
+  __syncthreads();
+  float* so = reinterpret_cast<float*>(smem);
+  float2* sml = reinterpret_cast<float2*>(so + kWarps * kRows * D);
+#pragma unroll
+  for (int m = 0; m < MT; ++m)
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int r = 16 * m + 8 * u + g;
+      float* dst = so + (warp * kRows + r) * D;
+#pragma unroll
+      for (int c = 0; c < D / 8; ++c)
+#pragma unroll
+        for (int v = 0; v < 2; ++v) {
+          const int n = 2 * t4 + v, col = FP8 ? 32 * (c / 4) + 4 * n + c % 4 : 8 * c + n;
+          dst[col ^ (4 * (r & 7))] = o[m][c][2 * u + v];  // (rows 8 apart in a warp's store: other banks)
+        }
+      if (t4 == 0) sml[warp * kRows + r] = make_float2(mx[m][u], l[m][u]);
+    }
+  __syncthreads();
+  constexpr int C4 = D / 4;  // float4 columns
+  for (int i = threadIdx.x; i < n_rows * C4; i += kThreads) {
+    const int r = i / C4, c = i % C4;
+    float m_all = kNegInf, w[kWarps], l_all = 0.f;
+#pragma unroll
+    for (int k = 0; k < kWarps; ++k) m_all = fmaxf(m_all, sml[k * kRows + r].x);
+#pragma unroll
+    for (int k = 0; k < kWarps; ++k) {
+      const float2 ml = sml[k * kRows + r];
+      w[k] = ml.y == 0.f ? 0.f : ex2(ml.x - m_all);  // (l = 0: it saw nothing; a NaN passes)
+      l_all += w[k] * ml.y;
+    }
+    float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int k = 0; k < kWarps; ++k) {
+      if (sml[k * kRows + r].y == 0.f) continue;
+      const float4 x = *reinterpret_cast<const float4*>(so + (k * kRows + r) * D + ((4 * c) ^ (4 * (r & 7))));
+      a.x += w[k] * x.x;
+      a.y += w[k] * x.y;
+      a.z += w[k] * x.z;
+      a.w += w[k] * x.w;
+    }
+    const int tok = r / G, head = h * G + r % G;
+    if (it.part_row >= 0) {
+      const int64_t row = it.part_row + (int64_t)tok * p.h_q + head;
+      *reinterpret_cast<float4*>(p.part_o + row * D + 4 * c) = a;
+      if (c == 0) p.part_ml[row] = make_float2(m_all, l_all);
+    } else {
+      const int64_t row = (int64_t)(it.tok0 + tok) * p.h_q + head;
+      const float inv = l_all == 0.f ? 0.f : 1.f / l_all;
+      if (p.out_bf16)
+        *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(p.out) + row * D + 4 * c) =
+            make_uint2(pack_bf16(a.x * inv, a.y * inv), pack_bf16(a.z * inv, a.w * inv));
+      else
+        *reinterpret_cast<float4*>(static_cast<float*>(p.out) + row * D + 4 * c) =
+            make_float4(a.x * inv, a.y * inv, a.z * inv, a.w * inv);
+      if (c == 0 && p.lse != nullptr) p.lse[row] = l_all == 0.f ? kNegInf : (m_all + log2f(l_all)) * kLn2;
+    }
+  }
+}
+
+// The split key ranges of one (token, query head) joined, a warp each: weights 2^(m_s - max m), O and l
+// added up in the order of the splits.
+template <int D>
+__global__ void __launch_bounds__(256) chunk_merge_kernel(const __grid_constant__ ChunkParams p,
+                                                          const ChunkMerge* __restrict__ work) {
+  const ChunkMerge w = work[blockIdx.x];
+  const int head = blockIdx.y * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+  if (head >= p.h_q) return;
+  const int n = w.pre_n + w.page_n;
+  auto row_of = [&](int s) {
+    return (s < w.pre_n ? w.pre_row + s * w.pre_stride : w.page_row + (s - w.pre_n) * w.page_stride) + head;
+  };
+  float m_all = kNegInf;
+  for (int s = lane; s < n; s += 32) m_all = fmaxf(m_all, p.part_ml[row_of(s)].x);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) m_all = fmaxf(m_all, __shfl_xor_sync(0xffffffffu, m_all, o));
+  constexpr int V = D / 32;  // columns of a lane
+  float acc[V], l = 0.f;
+#pragma unroll
+  for (int v = 0; v < V; ++v) acc[v] = 0.f;
+  for (int s0 = 0; s0 < n; s0 += 32) {
+    float wt = 0.f;
+    int64_t row = 0;
+    if (s0 + lane < n) {
+      row = row_of(s0 + lane);
+      const float2 ml = p.part_ml[row];
+      wt = ml.y == 0.f ? 0.f : ex2(ml.x - m_all);  // (l = 0: nothing was visible there; a NaN passes)
+      l += wt * ml.y;
+    }
+    const int k = min(32, n - s0);
+#pragma unroll 4
+    for (int s = 0; s < k; ++s) {
+      const float ws = __shfl_sync(0xffffffffu, wt, s);
+      const float* src = p.part_o + __shfl_sync(0xffffffffu, row, s) * D + V * lane;
+      if (ws == 0.f) continue;  // (its O, then, may not have been written)
+      if constexpr (V == 4) {
+        const float4 x = *reinterpret_cast<const float4*>(src);
+        acc[0] += ws * x.x;
+        acc[1] += ws * x.y;
+        acc[2] += ws * x.z;
+        acc[3] += ws * x.w;
+      } else {
+        const float2 x = *reinterpret_cast<const float2*>(src);
+        acc[0] += ws * x.x;
+        acc[1] += ws * x.y;
+      }
+    }
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  const int64_t row = (int64_t)w.tok * p.h_q + head;
+  if (p.out_bf16) {
+    uint32_t* dst = reinterpret_cast<uint32_t*>(static_cast<__nv_bfloat16*>(p.out) + row * D) + (V / 2) * lane;
+    if constexpr (V == 4)
+      *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16(acc[0] * inv, acc[1] * inv), pack_bf16(acc[2] * inv, acc[3] * inv));
+    else
+      *dst = pack_bf16(acc[0] * inv, acc[1] * inv);
+  } else {
+    float* dst = static_cast<float*>(p.out) + row * D + V * lane;
+    if constexpr (V == 4)
+      *reinterpret_cast<float4*>(dst) = make_float4(acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv);
+    else
+      *reinterpret_cast<float2*>(dst) = make_float2(acc[0] * inv, acc[1] * inv);
+  }
+  if (lane == 0 && p.lse != nullptr) p.lse[row] = l == 0.f ? kNegInf : (m_all + log2f(l)) * kLn2;
+}
+
+template <int D, bool FP8, int MT>
+cudaError_t launch(const ChunkParams& p, const ChunkItem* items, int n, cudaStream_t s) {
+  static bool configured[64] = {};
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (dev < 0 || dev >= 64 || !configured[dev]) {
+    e = cudaFuncSetAttribute(chunk_mma_kernel<D, FP8, MT>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_bytes<D, FP8, MT>());
+    if (e != cudaSuccess) return e;
+    if (dev >= 0 && dev < 64) configured[dev] = true;
+  }
+  if ((int64_t)n * p.h_kv > INT32_MAX) return cudaErrorInvalidValue;
+  chunk_mma_kernel<D, FP8, MT><<<n * p.h_kv, kThreads, smem_bytes<D, FP8, MT>(), s>>>(p, items);
+  return cudaGetLastError();
+}
+
+}  // namespace
+
+cudaError_t launch_chunk_mma(const ChunkParams& p, int head_dim, bool fp8, int rows16, const ChunkItem* items,
+                             int n_items, cudaStream_t s) {
+  if (head_dim == 128) {
+    if (rows16 == 1) return fp8 ? launch<128, true, 1>(p, items, n_items, s) : launch<128, false, 1>(p, items, n_items, s);
+    return fp8 ? launch<128, true, 2>(p, items, n_items, s) : launch<128, false, 2>(p, items, n_items, s);
+  }
+  if (rows16 == 1) return fp8 ? launch<64, true, 1>(p, items, n_items, s) : launch<64, false, 1>(p, items, n_items, s);
+  return fp8 ? launch<64, true, 2>(p, items, n_items, s) : launch<64, false, 2>(p, items, n_items, s);
+}
+
+cudaError_t launch_chunk_merge(const ChunkParams& p, int head_dim, const ChunkMerge* work, int n_work, cudaStream_t s) {
+  const dim3 grid(n_work, (p.h_q + 7) / 8);
+  if (head_dim == 128) chunk_merge_kernel<128><<<grid, 256, 0, s>>>(p, work);
+  else chunk_merge_kernel<64><<<grid, 256, 0, s>>>(p, work);
+  return cudaGetLastError();
+}
+
+}  // namespace pad

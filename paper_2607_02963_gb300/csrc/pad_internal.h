@@ -293,6 +293,16 @@ cudaError_t launch_attn_aggregate(const void* x, int64_t n_tokens, int32_t d, co
                                   const int32_t* offsets, int32_t n_segments, const int32_t* interval,
                                   int32_t n_events, const void* g_emb, float* seg_ws, float* out, cudaStream_t s);
 size_t attn_aggregate_ws_floats(int64_t n_tokens, int32_t n_segments, int32_t d);
+// What the entry points of other files share (pad_api.cu): the thread's error message, argument
+// checks, plan generations, and the page bookkeeping.
+pad_status api_fail(pad_status st, const char* fmt, ...);
+pad_status api_check_problem(const pad_problem* prob);
+int api_num_sms();
+uint64_t api_next_generation();
+int32_t api_next_free_page(const pad_cache_state* cache, int32_t from);   // -1: none
+void api_take_page(pad_cache_state* cache, int32_t page);
+// Asynchronous copy to device memory through a page-locked buffer of the library's; src may go at once.
+cudaError_t api_copy_in(void* dst, const void* src, size_t n, cudaStream_t s);
 cudaError_t launch_branch_merge(const KParams& p, const void* q, const void* k_pool,
                                 const void* v_pool, void* out, float* lse, bool pdl, cudaStream_t s);
 

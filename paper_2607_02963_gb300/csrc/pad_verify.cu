@@ -1,0 +1,184 @@
+// Verification of drafted tokens (pad_draft_verify): drafted token i, x_i, is kept while
+// u_i q_i(x_i) < p_i(x_i); at the first position a that fails the next token is drawn from
+// max(p_a - q_a, 0), after a whole accepted draft from p itself.  Together these give tokens
+// distributed as p.
+//
+// The draw needs the sum over the vocabulary and the place where the running sum passes a point of it.
+// The weights are integers, floor(2^38 min(r, 1)), and sums of integers do not depend on their order:
+// any split over threads gives the token that one running sum would.  2^38 keeps what fp32 has of
+// a probability down to 4e-12, and leaves 25 bits for the number of terms.
+//
+// Bound by bytes: one row of p and one of q per event.  A cluster of eight CTAs takes an event; each sums
+// an eighth of the rows, warp by warp over consecutive entries, the eight sums meet in distributed shared
+// memory, and the CTA that holds the point goes through the one warp's part it lies in again (a
+// 128th of the row, from L2).
+#include <cooperative_groups.h>
+#include <cuda_bf16.h>
+#include <algorithm>
+#include <cstdint>
+
+#include "pad_chunk.h"
+
+namespace pad {
+
+namespace {
+
+namespace cg = cooperative_groups;
+
+constexpr int kCtas = 8;       // of an event
+constexpr int kThreads = 512;
+constexpr int kWarps = kThreads / 32;
+
+__device__ __forceinline__ float value(float x) { return x; }
+__device__ __forceinline__ float value(__nv_bfloat16 x) { return __bfloat162float(x); }
+
+__device__ __forceinline__ int64_t weight(float r) {
+  return r > 0.f ? (int64_t)(fminf(r, 1.f) * 274877906944.f) : 0;  // 2^38 (a power of two: exact); NaN: 0
+}
+
+__device__ __forceinline__ int64_t warp_sum(int64_t v) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return v;
+}
+
+template <class T>
+__global__ void __cluster_dims__(kCtas, 1, 1) __launch_bounds__(kThreads)
+    draft_verify_kernel(const __grid_constant__ ChunkParams pr, const ChunkVerify* __restrict__ work, int vocab,
+                        const T* __restrict__ p, int64_t p_stride, const T* __restrict__ q, int64_t q_stride,
+                        const int32_t* __restrict__ draft, const float* __restrict__ u_accept,
+                        const float* __restrict__ u_pick, int32_t* __restrict__ accepted, int32_t* __restrict__ token) {
+  __shared__ int first_bad;
+  __shared__ int64_t part[2][kWarps];   // sums of each warp's entries: of the difference, of p
+  __shared__ int64_t mine[2];           // of this CTA's
+  __shared__ int64_t scan[kWarps];
+  cg::cluster_group cl = cg::this_cluster();
+  const int rank = (int)cl.block_rank(), e = (int)blockIdx.x / kCtas;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const ChunkVerify w = work[e];
+  if (w.n_draft < 0) {  // (the whole cluster)
+    if (rank == 0 && threadIdx.x == 0) accepted[e] = 0, token[e] = -1;
+    return;
+  }
+  if (threadIdx.x == 0) first_bad = w.n_draft;
+  __syncthreads();
+  for (int i = threadIdx.x; i < w.n_draft; i += kThreads) {
+    const int x = draft[w.draft0 + i];
+    bool ok = (unsigned)x < (unsigned)vocab;
+    if (!ok && rank == 0) pad_set_error(pr.header, pr.gen, PAD_ERR_DEVICE_BOUNDS, e, i, x);
+    if (ok)
+      ok = __fmul_rn(u_accept[w.draft0 + i], value(q[(int64_t)(w.draft0 + i) * q_stride + x])) <
+           value(p[(int64_t)(w.tok0 + i) * p_stride + x]);
+    if (!ok) atomicMin(&first_bad, i);
+  }
+  __syncthreads();
+  const int a = first_bad;
+  const bool sub = a < w.n_draft;
+  const T* pa = p + (int64_t)(w.tok0 + a) * p_stride;
+  const T* qa = q + (sub ? (int64_t)(w.draft0 + a) * q_stride : 0);
+  // this warp's entries: consecutive, the same number for every warp of the cluster
+  const int per = (vocab + kCtas * kWarps - 1) / (kCtas * kWarps);
+  auto begin_of = [&](int wp) { return (int)min((int64_t)vocab, (int64_t)(rank * kWarps + wp) * per); };
+  const int lo = begin_of(warp), hi = min(vocab, lo + per);
+  int64_t d = 0, s = 0;
+  constexpr int U = 8;
+  for (int i0 = lo + lane; i0 < hi; i0 += 32 * U) {
+    float x[U], y[U];
+#pragma unroll
+    for (int j = 0; j < U; ++j) {
+      x[j] = y[j] = 0.f;
+      if (i0 + 32 * j < hi) {
+        x[j] = value(pa[i0 + 32 * j]);
+        if (sub) y[j] = value(qa[i0 + 32 * j]);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < U; ++j) {
+      s += weight(x[j]);
+      if (sub) d += weight(x[j] - y[j]);
+    }
+  }
+  s = warp_sum(s);
+  d = sub ? warp_sum(d) : s;
+  if (lane == 0) part[0][warp] = d, part[1][warp] = s;
+  __syncthreads();
+  if (threadIdx.x < 2) {
+    int64_t t = 0;
+    for (int k = 0; k < kWarps; ++k) t += part[threadIdx.x][k];
+    mine[threadIdx.x] = t;
+  }
+  cl.sync();
+  int64_t total[2] = {0, 0}, before[2] = {0, 0};
+#pragma unroll
+  for (int k = 0; k < kCtas; ++k) {
+    const int64_t* m = cl.map_shared_rank(mine, k);
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int64_t v = m[u];
+      if (k < rank) before[u] += v;
+      total[u] += v;
+    }
+  }
+  cl.sync();  // (nobody leaves while its sums may still be read)
+  const bool diff = total[0] > 0;  // else: nothing left of the difference, p itself
+  const int64_t sum = diff ? total[0] : total[1];
+  if (rank == 0 && threadIdx.x == 0) {
+    accepted[e] = a;
+    if (sum == 0) token[e] = -1;
+  }
+  if (sum == 0) return;
+  const float u = u_pick[e];
+  const int64_t m = (int64_t)fminf(fmaxf(floorf(u * 16777216.f), 0.f), 16777215.f);  // (a NaN: 0)
+  const int64_t goal = m * (sum >> 24) + ((m * (sum & 0xffffff)) >> 24) - (diff ? before[0] : before[1]);
+  if (goal < 0 || goal >= (diff ? mine[0] : mine[1])) return;  // (the whole CTA)
+  const int64_t* ps = part[diff ? 0 : 1];
+  int wp = 0;
+  int64_t base = 0;
+  while (wp < kWarps - 1 && base + ps[wp] <= goal) base += ps[wp++];
+  // that warp's entries again, a few consecutive ones per thread
+  const int wlo = begin_of(wp), whi = min(vocab, wlo + per);
+  const int c = (whi - wlo + kThreads - 1) / kThreads, tlo = min(whi, wlo + (int)threadIdx.x * c), thi = min(whi, tlo + c);
+  const bool take = sub && diff;
+  auto weight_of = [&](int i) { return weight(take ? value(pa[i]) - value(qa[i]) : value(pa[i])); };
+  int64_t t = 0;
+  for (int i = tlo; i < thi; ++i) t += weight_of(i);
+  int64_t inc = t;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int64_t v = __shfl_up_sync(0xffffffffu, inc, o);
+    if (lane >= o) inc += v;
+  }
+  if (lane == 31) scan[warp] = inc;
+  __syncthreads();
+  int64_t at = base + inc - t;
+  for (int k = 0; k < warp; ++k) at += scan[k];
+  if (at <= goal && goal < at + t) {
+    int i = tlo;
+    for (;; ++i) {
+      at += weight_of(i);
+      if (at > goal || i + 1 >= thi) break;
+    }
+    token[e] = i;
+  }
+}
+
+template <class T>
+cudaError_t launch(const ChunkParams& p, const ChunkVerify* work, int n, int vocab, const void* tp, int64_t ps,
+                   const void* dq, int64_t qs, const int32_t* draft, const float* ua, const float* up, int32_t* acc,
+                   int32_t* tok, cudaStream_t s) {
+  draft_verify_kernel<T><<<n * kCtas, kThreads, 0, s>>>(p, work, vocab, static_cast<const T*>(tp), ps, static_cast<const T*>(dq),
+                                                        qs, draft, ua, up, acc, tok);
+  return cudaGetLastError();
+}
+
+}  // namespace
+
+cudaError_t launch_draft_verify(const ChunkParams& p, const ChunkVerify* work, int n_events, int vocab, bool bf16,
+                                const void* tp, int64_t p_stride, const void* dq, int64_t q_stride,
+                                const int32_t* draft, const float* u_accept, const float* u_pick, int32_t* accepted,
+                                int32_t* token, cudaStream_t s) {
+  return bf16 ? launch<__nv_bfloat16>(p, work, n_events, vocab, tp, p_stride, dq, q_stride, draft, u_accept, u_pick, accepted, token, s)
+              : launch<float>(p, work, n_events, vocab, tp, p_stride, dq, q_stride, draft, u_accept, u_pick, accepted, token, s);
+}
+
+}  // namespace pad
