@@ -207,6 +207,13 @@ def _stream(stream):
     return c_void_p(stream.cuda_stream)
 
 
+def _stream_handle(stream):
+    """The handle that _stream wraps, as an integer."""
+    if stream is None:
+        return _raw_stream() if _raw_stream is not None else _current_stream()
+    return stream if isinstance(stream, int) else stream.cuda_stream
+
+
 def make_problem(h_q, h_kv, head_dim, page_size=16, scale=None, out_dtype=0, num_sms=0, flags=0):
     if scale is None:
         scale = 1.0 / float(head_dim) ** 0.5
@@ -421,22 +428,29 @@ def pad_device_status(plan: Plan, stream=None):
     _check(lib().pad_device_status(plan.handle, _stream(stream)))
 
 
-def _rows(t):
-    """Device pointer and row stride (elements) of a tensor whose rows are contiguous (None -> NULL, packed)."""
+def _dev(t, name, shape, dtype):
+    """Device address of a contiguous tensor of this shape and type (None -> NULL)."""
     if t is None:
-        return None, 0
+        return None
+    if t.shape != shape or t.dtype is not dtype:
+        raise ValueError(f"{name}: {tuple(t.shape)} {t.dtype}, expected {tuple(shape)} {dtype}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name}: tensors passed to libpad must be contiguous")
+    return t.data_ptr()
+
+
+def _rows(t, name, shape, dtype):
+    """Device address and row stride (elements; 0 = packed) of a tensor whose rows are contiguous."""
+    if t.shape != shape or t.dtype is not dtype:
+        raise ValueError(f"{name}: {tuple(t.shape)} {t.dtype}, expected {tuple(shape)} {dtype}")
+    if t.is_contiguous():
+        return t.data_ptr(), 0
     want = 1
     for n, st in zip(reversed(t.shape[1:]), reversed(t.stride()[1:])):
         if n != 1 and st != want:
-            raise ValueError("the rows of tensors passed to libpad must be contiguous")
+            raise ValueError(f"{name}: the rows of tensors passed to libpad must be contiguous")
         want *= n
-    return c_void_p(t.data_ptr()), (int(t.stride(0)) if t.shape[0] > 1 else 0)
-
-
-def _shaped(t, name, shape, dtype):
-    """A tensor's shape and type checked against what the plan says."""
-    if t is not None and (tuple(t.shape) != tuple(shape) or t.dtype != dtype):
-        raise ValueError(f"{name}: {tuple(t.shape)} {t.dtype}, expected {tuple(shape)} {dtype}")
+    return t.data_ptr(), (int(t.stride(0)) if t.shape[0] > 1 else 0)
 
 
 class ChunkPlan:
@@ -451,6 +465,16 @@ class ChunkPlan:
         self._keep = keep  # device memory that the plan points to
         i = self.info()
         self.n_tokens, self.n_cached, self.n_drafts = i["n_tokens"], i["n_cached"], i["n_drafts"]
+        # what every call's tensors are checked against
+        import torch
+        hq, hk, d = problem.h_q, problem.h_kv, problem.head_dim
+        self._q_shape, self._lse_shape = (self.n_tokens, hq, d), (self.n_tokens, hq)
+        self._new_shape, self._read_shape = (self.n_tokens, hk, d), (self.n_cached, hk, d)
+        self._scale_shape = (n_pages, hk, problem.page_size)
+        self._pool_shape = self._scale_shape + (d,)
+        self._bf16, self._f32, self._i32, self._u8 = torch.bfloat16, torch.float32, torch.int32, torch.uint8
+        self._pool_type = torch.uint8 if kv_format == KV_FP8 else torch.bfloat16
+        self._out_type = torch.bfloat16 if problem.out_dtype == 1 else torch.float32
 
     @property
     def handle(self):
@@ -480,14 +504,11 @@ class ChunkPlan:
                                       out.ctypes.data_as(_I32P)))
         return out
 
-    def check_pools(self, k_pool, v_pool, k_scale, v_scale):
-        import torch
-        p = self.problem
-        shape = (self.n_pages, p.h_kv, p.page_size, p.head_dim)
-        dt = torch.uint8 if self.kv_format == KV_FP8 else torch.bfloat16
-        for name, pool, scale in (("k", k_pool, k_scale), ("v", v_pool, v_scale)):
-            _shaped(pool, name + "_pool", shape, dt)
-            _shaped(scale, name + "_scale", shape[:3], torch.uint8)
+    def _pools(self, k_pool, v_pool, k_scale, v_scale):
+        return (_dev(k_pool, "k_pool", self._pool_shape, self._pool_type),
+                _dev(v_pool, "v_pool", self._pool_shape, self._pool_type),
+                _dev(k_scale, "k_scale", self._scale_shape, self._u8),
+                _dev(v_scale, "v_scale", self._scale_shape, self._u8))
 
     def destroy(self):
         if self._h is not None and _lib is not None:
@@ -549,65 +570,55 @@ def pad_chunk_plan(problem: Problem, cache, prefix_len, event_video, event_len, 
 
 def pad_chunk_append(plan: ChunkPlan, k_new, v_new, k_pool, v_pool, k_scale=None, v_scale=None, stream=None):
     """Write the new tokens' K/V into the branches' pages (quantised in an 8-bit cache)."""
-    import torch
-    p = plan.problem
-    shape = (plan.n_tokens, p.h_kv, p.head_dim)
-    _shaped(k_new, "k_new", shape, torch.bfloat16)
-    _shaped(v_new, "v_new", shape, torch.bfloat16)
-    plan.check_pools(k_pool, v_pool, k_scale, v_scale)
-    kp, ks = _rows(k_new)
-    vp, vs = _rows(v_new)
+    kn, ks = _rows(k_new, "k_new", plan._new_shape, plan._bf16)
+    vn, vs = _rows(v_new, "v_new", plan._new_shape, plan._bf16)
     if ks != vs:
         raise ValueError("k_new and v_new must have the same token stride")
-    _check(lib().pad_chunk_append(plan.handle, kp, vp, ks, _ptr(k_pool), _ptr(v_pool), _ptr(k_scale), _ptr(v_scale),
-                                  _stream(stream)))
+    kp, vp, ksc, vsc = plan._pools(k_pool, v_pool, k_scale, v_scale)
+    st = lib().pad_chunk_append(plan._h, kn, vn, ks, kp, vp, ksc, vsc, _stream_handle(stream))
+    if st:
+        _check(st)
 
 
 def pad_chunk_read(plan: ChunkPlan, k_pool, v_pool, k_out, v_out, k_scale=None, v_scale=None, stream=None):
     """Copy every branch's cached tokens out as contiguous bf16 [n_cached, h_kv, head_dim]."""
-    import torch
-    p = plan.problem
-    plan.check_pools(k_pool, v_pool, k_scale, v_scale)
-    shape = (plan.n_cached, p.h_kv, p.head_dim)
-    _shaped(k_out, "k_out", shape, torch.bfloat16)
-    _shaped(v_out, "v_out", shape, torch.bfloat16)
-    _check(lib().pad_chunk_read(plan.handle, _ptr(k_pool), _ptr(v_pool), _ptr(k_scale), _ptr(v_scale), _ptr(k_out),
-                                _ptr(v_out), _stream(stream)))
+    kp, vp, ksc, vsc = plan._pools(k_pool, v_pool, k_scale, v_scale)
+    ko, vo = (_dev(k_out, "k_out", plan._read_shape, plan._bf16), _dev(v_out, "v_out", plan._read_shape, plan._bf16))
+    st = lib().pad_chunk_read(plan._h, kp, vp, ksc, vsc, ko, vo, _stream_handle(stream))
+    if st:
+        _check(st)
 
 
 def pad_chunk_attn(plan: ChunkPlan, q, k_prefix, v_prefix, k_pool, v_pool, out, lse=None, k_scale=None, v_scale=None,
                    stream=None):
     """Attention of the step's new tokens over their video's prefix and their branch's cached tokens."""
-    import torch
-    p = plan.problem
-    shape = (plan.n_tokens, p.h_q, p.head_dim)
-    _shaped(q, "q", shape, torch.bfloat16)
-    _shaped(out, "out", shape, torch.bfloat16 if p.out_dtype == 1 else torch.float32)
-    _shaped(lse, "lse", shape[:2], torch.float32)
-    plan.check_pools(k_pool, v_pool, k_scale, v_scale)
-    qp, qs = _rows(q)
-    _check(lib().pad_chunk_attn(plan.handle, qp, qs, _ptr(k_prefix), _ptr(v_prefix), _ptr(k_pool), _ptr(v_pool),
-                                _ptr(k_scale), _ptr(v_scale), _ptr(out), _ptr(lse), _stream(stream)))
+    qp, qs = _rows(q, "q", plan._q_shape, plan._bf16)
+    kp, vp, ksc, vsc = plan._pools(k_pool, v_pool, k_scale, v_scale)
+    kx, vx = None, None
+    if k_prefix is not None:
+        kx = _dev(k_prefix, "k_prefix", (k_prefix.shape[0],) + plan._new_shape[1:], plan._bf16)
+        vx = _dev(v_prefix, "v_prefix", k_prefix.shape, plan._bf16)
+    st = lib().pad_chunk_attn(plan._h, qp, qs, kx, vx, kp, vp, ksc, vsc, _dev(out, "out", plan._q_shape, plan._out_type),
+                              _dev(lse, "lse", plan._lse_shape, plan._f32), _stream_handle(stream))
+    if st:
+        _check(st)
 
 
 def pad_draft_verify(plan: ChunkPlan, p, q, draft, u_accept, u_pick, accepted, token, stream=None):
     """Accept or reject the step's drafted tokens against the target's probabilities p [n_tokens, vocab] and
     the draft's q [n_drafts, vocab] (fp32 or bf16), and draw each branch's next token."""
-    import torch
-    if p.dtype not in (torch.float32, torch.bfloat16):
-        raise ValueError(f"p: {p.dtype}, expected float32 or bfloat16")
+    bf16 = p.dtype is plan._bf16
+    kind = plan._bf16 if bf16 else plan._f32
     vocab = int(p.shape[1])
-    _shaped(p, "p", (plan.n_tokens, vocab), p.dtype)
-    _shaped(q, "q", (plan.n_drafts, vocab), p.dtype)
-    _shaped(draft, "draft", (plan.n_drafts,), torch.int32)
-    _shaped(u_accept, "u_accept", (plan.n_drafts,), torch.float32)
-    _shaped(u_pick, "u_pick", (plan.n_events,), torch.float32)
-    _shaped(accepted, "accepted", (plan.n_events,), torch.int32)
-    _shaped(token, "token", (plan.n_events,), torch.int32)
-    pp, ps = _rows(p)
-    qp, qs = _rows(q)
-    _check(lib().pad_draft_verify(plan.handle, vocab, 1 if p.dtype == torch.bfloat16 else 0, pp, ps, qp, qs, _ptr(draft),
-                                  _ptr(u_accept), _ptr(u_pick), _ptr(accepted), _ptr(token), _stream(stream)))
+    pp, ps = _rows(p, "p", (plan.n_tokens, vocab), kind)
+    qp, qs = _rows(q, "q", (plan.n_drafts, vocab), kind)
+    nd, ne = (plan.n_drafts,), (plan.n_events,)
+    st = lib().pad_draft_verify(plan._h, vocab, 1 if bf16 else 0, pp, ps, qp, qs, _dev(draft, "draft", nd, plan._i32),
+                                _dev(u_accept, "u_accept", nd, plan._f32), _dev(u_pick, "u_pick", ne, plan._f32),
+                                _dev(accepted, "accepted", ne, plan._i32), _dev(token, "token", ne, plan._i32),
+                                _stream_handle(stream))
+    if st:
+        _check(st)
 
 
 def pad_chunk_status(plan: ChunkPlan, stream=None):

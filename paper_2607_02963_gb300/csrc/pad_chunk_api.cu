@@ -25,6 +25,7 @@ constexpr int64_t kMaxLen = 1 << 30;
 constexpr int64_t kMaxTokens = INT32_MAX / 2;  // packed new tokens of a step
 constexpr int kSplitUnit = 64;                 // key ranges are multiples of this
 constexpr int kMinSplit = 256;
+constexpr int kMmaRows = 32;                   // rows of a branch (tokens x group) up to which the warp-level kernel takes it
 
 size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
@@ -83,7 +84,9 @@ pad_status check_batch(const Batch& b) {
 
 // The work lists (all but the page ids) and the layout of the workspace.
 struct Lists {
+  std::vector<ChunkItem> tc;             // items of the tcgen05 kernel
   std::vector<ChunkItem> pre, page;      // items of the warp-level kernel: of the prefixes, of the pages
+  bool tc_split = false, has_prefix = false;
   int pre_rows16 = 1, page_rows16 = 1;
   std::vector<ChunkMerge> merge;
   std::vector<ChunkPages> pages;
@@ -91,7 +94,7 @@ struct Lists {
   std::vector<ChunkVerify> verify;
   int64_t n_tokens = 0, n_cached = 0, n_drafts = 0, partial_rows = 0;
   int32_t n_spans = 0, pre_splits = 0, page_splits = 0;
-  size_t off_pre = 0, off_page = 0, off_merge = 0, off_pages = 0, off_read = 0, off_verify = 0, image_bytes = 0;
+  size_t off_tc = 0, off_pre = 0, off_page = 0, off_merge = 0, off_pages = 0, off_read = 0, off_verify = 0, image_bytes = 0;
   size_t off_ml = 0, off_o = 0, total = 0;
 };
 
@@ -101,57 +104,108 @@ struct Segment {
   int32_t keys;       // of its last token
   int32_t tok0, ntok;
   int32_t lim0, paged;
+  bool tc;            // on the tcgen05 kernel
   int32_t n_splits, split_len;
   int64_t part_row;
 };
 
-// Items of the warp-level kernel.  Its CTAs take 32 rows at most (16 when no segment has more: twice
-// the CTAs per SM), and key ranges are cut so that there are some eight CTAs for each SM, no
-// shorter than kMinSplit keys.
-void cut(std::vector<Segment>& segs, const pad_problem& prob, int sms, int& rows16, int32_t& most) {
+// Key ranges of about `len` keys, all about as long.
+void split_by(Segment& s, int64_t len, int64_t unit) {
+  s.n_splits = (int32_t)std::max<int64_t>(1, (s.keys + len - 1) / len);
+  const int64_t even = (s.keys + s.n_splits - 1) / s.n_splits;
+  s.split_len = (int32_t)align_up((size_t)std::max<int64_t>(1, even), (size_t)unit);
+  s.n_splits = std::max(1, (s.keys + s.split_len - 1) / s.split_len);
+}
+
+// The warp-level kernel's CTAs take 32 rows at most (16 when no segment has more: twice the CTAs per
+// SM), and key ranges are cut so that there are some eight CTAs for each SM, no shorter than
+// kMinSplit keys.
+void cut_mma(std::vector<Segment>& segs, int paged, const pad_problem& prob, int sms, int& rows16) {
   const int G = prob.h_q / prob.h_kv;
   int longest = 0;
-  for (const Segment& s : segs) longest = std::max(longest, s.ntok);
+  for (const Segment& s : segs)
+    if (!s.tc && s.paged == paged) longest = std::max(longest, s.ntok);
   rows16 = (int64_t)longest * G <= 16 ? 1 : 2;
   const int tpt = 16 * rows16 / G;
   double work = 0;
-  for (const Segment& s : segs) work += (double)((s.ntok + tpt - 1) / tpt) * s.keys * prob.h_kv;
+  for (const Segment& s : segs)
+    if (!s.tc && s.paged == paged) work += (double)((s.ntok + tpt - 1) / tpt) * s.keys * prob.h_kv;
   const double per = work / (8.0 * sms);
   const int64_t len = std::max<int64_t>(kMinSplit, ((int64_t)(per / kSplitUnit) + 1) * kSplitUnit);
-  for (Segment& s : segs) {
-    s.n_splits = (int32_t)std::max<int64_t>(1, (s.keys + len - 1) / len);
-    const int32_t even = (s.keys + s.n_splits - 1) / s.n_splits;  // (all about as long)
-    s.split_len = (int32_t)align_up(std::max(1, even), kSplitUnit);
-    s.n_splits = std::max(1, (s.keys + s.split_len - 1) / s.split_len);
-    most = std::max(most, s.n_splits);
-  }
+  for (Segment& s : segs)
+    if (!s.tc && s.paged == paged) split_by(s, len, kSplitUnit);
 }
 
-void items_of(const std::vector<Segment>& segs, const pad_problem& prob, int rows16, std::vector<ChunkItem>& out) {
-  const int tpt = 16 * rows16 / (prob.h_q / prob.h_kv);
+// The tcgen05 kernel: one CTA per SM at a time, so its time is that of its waves: a CTA's start and end, and
+// its tiles one after the other.  Both forms and the key ranges' length (in tiles) are costed with what was
+// measured on GB300 (us), the partial states with their way out and in again.
+constexpr double kTcCta = 5.0, kTcFirst = 4.0, kPairTile = 1.55, kSplitTile = 1.8, kPartialRate = 3e6;  // bytes per us
+void cut_tc(std::vector<Segment>& segs, const pad_problem& prob, int sms, bool& split) {
+  const int tps = 128 / (prob.h_q / prob.h_kv);
+  double best = 1e300;
+  int64_t best_len = 0;
+  auto tiles_of = [](const Segment& s) { return ((int64_t)s.keys + 127) / 128; };
+  int64_t longest = 0;
   for (const Segment& s : segs)
-    for (int t = 0; t < s.ntok; t += tpt)
-      for (int k = 0; k < s.n_splits; ++k) {
-        ChunkItem it;
-        it.src = s.src;
-        it.tok0 = s.tok0 + t;
-        it.ntok = std::min(tpt, s.ntok - t);
-        it.lim0 = s.lim0 + (s.paged ? t : 0);
-        it.paged = s.paged;
-        it.key0 = (int32_t)std::min<int64_t>((int64_t)k * s.split_len, s.keys);
-        const int32_t seen = s.paged ? it.lim0 + it.ntok - 1 : s.keys;
-        it.key1 = (int32_t)std::min<int64_t>((int64_t)(k + 1) * s.split_len, seen);
-        it.part_row = s.part_row < 0 ? -1 : s.part_row + ((int64_t)k * s.ntok + t) * prob.h_q;
-        out.push_back(it);
+    if (s.tc) longest = std::max(longest, tiles_of(s));
+  if (longest == 0) return;
+  for (int form = 0; form < 2; ++form) {
+    const int tpc = form ? tps : 2 * tps;
+    const double tile = form ? kSplitTile : kPairTile;
+    for (int64_t len = longest;; len = len > 16 ? std::max<int64_t>(16, len * 7 / 8) : len - 1) {
+      double ctas = 0, work = 0, bytes = 0;
+      int64_t most = 0;
+      for (const Segment& s : segs) {
+        if (!s.tc) continue;
+        const int64_t tiles = tiles_of(s), n = (tiles + len - 1) / len, each = (tiles + n - 1) / n;
+        const double rows = (double)((s.ntok + tpc - 1) / tpc) * prob.h_kv;
+        ctas += rows * (double)n;
+        work += rows * (double)tiles;
+        most = std::max(most, each);
+        if (n > 1) bytes += 2.0 * (double)n * s.ntok * prob.h_q * (prob.head_dim + 2) * 4;
       }
+      const double waves = std::ceil(ctas / sms);
+      // few waves are as long as their longest CTAs; many even out
+      const double t = kTcFirst + bytes / kPartialRate +
+                       (waves <= 4 ? waves * (kTcCta + tile * (double)most) : (ctas * kTcCta + work * tile) / sms + tile * (double)most);
+      if (t < best) {
+        best = t;
+        best_len = len;
+        split = form != 0;
+      }
+      if (len <= 1) break;
+    }
+  }
+  for (Segment& s : segs)
+    if (s.tc) split_by(s, best_len * 128, 128);
+}
+
+// tpt: tokens per item.
+void items_of(const Segment& s, const pad_problem& prob, int tpt, std::vector<ChunkItem>& out) {
+  for (int t = 0; t < s.ntok; t += tpt)
+    for (int k = 0; k < s.n_splits; ++k) {
+      ChunkItem it;
+      it.src = s.src;
+      it.tok0 = s.tok0 + t;
+      it.ntok = std::min(tpt, s.ntok - t);
+      it.lim0 = s.lim0 + (s.paged ? t : 0);
+      it.paged = s.paged;
+      it.key0 = (int32_t)std::min<int64_t>((int64_t)k * s.split_len, s.keys);
+      const int32_t seen = s.paged ? it.lim0 + it.ntok - 1 : s.keys;
+      it.key1 = (int32_t)std::min<int64_t>((int64_t)(k + 1) * s.split_len, seen);
+      it.part_row = s.part_row < 0 ? -1 : s.part_row + ((int64_t)k * s.ntok + t) * prob.h_q;
+      out.push_back(it);
+    }
 }
 
 void build(const Batch& b, const int64_t* prefix_offset, Lists& L) {
   const pad_problem& prob = *b.prob;
   const int ps = prob.page_size, span = chunk_read_tokens();
   const int sms = prob.num_sms > 0 ? prob.num_sms : api_num_sms();
-  std::vector<Segment> pre, own;
+  const int G = prob.h_q / prob.h_kv;
+  std::vector<Segment> segs;
   std::vector<int32_t> pre_of(b.n_events, -1), own_of(b.n_events, -1);
+  int32_t open = -1;  // the video whose prefix segment is growing
   std::vector<int64_t> off(b.n_videos);
   int64_t o = 0;
   for (int v = 0; v < b.n_videos; ++v) {
@@ -162,13 +216,16 @@ void build(const Batch& b, const int64_t* prefix_offset, Lists& L) {
     const int n = b.n_new[e], len = b.event_len[e], v = b.n_videos > 0 ? b.event_video[e] : -1;
     const int32_t tok0 = (int32_t)L.n_tokens;
     if (n > 0 && v >= 0 && b.prefix_len[v] > 0) {
-      if (pre.empty() || pre.back().src != v) pre.push_back({v, b.prefix_len[v], tok0, 0, b.prefix_len[v], 0, 0, 0, -1});
-      pre.back().ntok += n;
-      pre_of[e] = (int32_t)pre.size() - 1;
+      if (open < 0 || segs[open].src != v) {
+        open = (int32_t)segs.size();
+        segs.push_back({v, b.prefix_len[v], tok0, 0, b.prefix_len[v], 0, false, 0, 0, -1});
+      }
+      segs[open].ntok += n;
+      pre_of[e] = open;
     }
     if (n > 0) {
-      own_of[e] = (int32_t)own.size();
-      own.push_back({e, len + n, tok0, n, len + 1, 1, 0, 0, -1});
+      own_of[e] = (int32_t)segs.size();
+      segs.push_back({e, len + n, tok0, n, len + 1, 1, false, 0, 0, -1});
     }
     for (int i = 0; i < n;) {
       const int pos = len + i, count = std::min(n - i, ps - pos % ps);
@@ -182,17 +239,27 @@ void build(const Batch& b, const int64_t* prefix_offset, Lists& L) {
     L.n_cached += (int64_t)len + n;
     L.n_drafts += std::max(0, n - 1);
   }
-  cut(pre, prob, sms, L.pre_rows16, L.pre_splits);
-  cut(own, prob, sms, L.page_rows16, L.page_splits);
+  for (Segment& s : segs) {
+    if (prob.flags & (PAD_FLAG_PREFIX_MMA | PAD_FLAG_PREFIX_TC)) s.tc = (prob.flags & PAD_FLAG_PREFIX_TC) != 0;
+    else s.tc = !s.paged || (int64_t)s.ntok * G > kMmaRows;
+  }
+  cut_tc(segs, prob, sms, L.tc_split);
+  cut_mma(segs, 0, prob, sms, L.pre_rows16);
+  cut_mma(segs, 1, prob, sms, L.page_rows16);
+  for (const Segment& s : segs) {
+    int32_t& most = s.paged ? L.page_splits : L.pre_splits;
+    most = std::max(most, s.n_splits);
+  }
   // a token whose keys are in more than one piece is joined from partial states
   auto partial = [&](Segment& s) {
     s.part_row = L.partial_rows;
     L.partial_rows += (int64_t)s.n_splits * s.ntok * prob.h_q;
   };
-  for (Segment& s : pre) partial(s);  // (the tokens' own keys are a second piece at least)
+  for (Segment& s : segs)
+    if (!s.paged) partial(s);  // (the tokens' own keys are a second piece at least)
   for (int e = 0; e < b.n_events; ++e)
-    if (own_of[e] >= 0 && (pre_of[e] >= 0 || own[own_of[e]].n_splits > 1)) {
-      Segment& s = own[own_of[e]];
+    if (own_of[e] >= 0 && (pre_of[e] >= 0 || segs[own_of[e]].n_splits > 1)) {
+      Segment& s = segs[own_of[e]];
       partial(s);
       for (int i = 0; i < s.ntok; ++i) {
         ChunkMerge m{};
@@ -201,7 +268,7 @@ void build(const Batch& b, const int64_t* prefix_offset, Lists& L) {
         m.page_row = s.part_row + (int64_t)i * prob.h_q;
         m.page_stride = (int64_t)s.ntok * prob.h_q;
         if (pre_of[e] >= 0) {
-          const Segment& q = pre[pre_of[e]];
+          const Segment& q = segs[pre_of[e]];
           m.pre_n = q.n_splits;
           m.pre_row = q.part_row + (int64_t)(m.tok - q.tok0) * prob.h_q;
           m.pre_stride = (int64_t)q.ntok * prob.h_q;
@@ -209,14 +276,24 @@ void build(const Batch& b, const int64_t* prefix_offset, Lists& L) {
         L.merge.push_back(m);
       }
     }
-  for (Segment& s : pre) s.src = off[s.src];
-  items_of(pre, prob, L.pre_rows16, L.pre);
-  items_of(own, prob, L.page_rows16, L.page);
+  for (Segment& s : segs) {
+    if (!s.paged) {
+      s.src = off[s.src];
+      L.has_prefix = true;
+    }
+    if (s.tc) items_of(s, prob, (L.tc_split ? 1 : 2) * (128 / G), L.tc);
+    else items_of(s, prob, 16 * (s.paged ? L.page_rows16 : L.pre_rows16) / G, s.paged ? L.page : L.pre);
+  }
+  // the longest first: what is left at the end of the grid is short
+  auto longer = [](const ChunkItem& x, const ChunkItem& y) { return x.key1 - x.key0 > y.key1 - y.key0; };
+  std::stable_sort(L.tc.begin(), L.tc.end(), longer);
+  std::stable_sort(L.page.begin(), L.page.end(), longer);
   size_t at = sizeof(PadDevHeader);
   auto place = [&](size_t& where, size_t bytes) {
     where = at;
     at = align_up(at + bytes, 16);
   };
+  place(L.off_tc, L.tc.size() * sizeof(ChunkItem));
   place(L.off_pre, L.pre.size() * sizeof(ChunkItem));
   place(L.off_page, L.page.size() * sizeof(ChunkItem));
   place(L.off_merge, L.merge.size() * sizeof(ChunkMerge));
@@ -240,7 +317,7 @@ struct pad_chunk_t {
   int32_t* page_table = nullptr;
   uint8_t* workspace = nullptr;
   uint64_t gen = 0;
-  bool has_prefix = false, from_cache = false, committed = false;
+  bool from_cache = false, committed = false;
   Lists L;
   std::vector<int32_t> event_len, n_new;
   std::vector<int32_t> new_event, new_column, new_page;
@@ -367,7 +444,6 @@ pad_status pad_chunk_plan(const pad_problem* prob, int32_t kv_format, pad_cache_
       c->n_new.assign(n_new, n_new + n_events);
     }
     build(b, prefix_offset, c->L);
-    c->has_prefix = !c->L.pre.empty();
     if (workspace && workspace_bytes < c->L.total)
       return api_fail(PAD_ERR_WORKSPACE_TOO_SMALL, "workspace has %zu bytes, the plan needs %zu", workspace_bytes, c->L.total);
     if (cache) {
@@ -390,6 +466,7 @@ pad_status pad_chunk_plan(const pad_problem* prob, int32_t kv_format, pad_cache_
       auto put = [&](size_t off, const void* src, size_t n) {
         if (n) memcpy(image.data() + off - sizeof(PadDevHeader), src, n);
       };
+      put(c->L.off_tc, c->L.tc.data(), c->L.tc.size() * sizeof(ChunkItem));
       put(c->L.off_pre, c->L.pre.data(), c->L.pre.size() * sizeof(ChunkItem));
       put(c->L.off_page, c->L.page.data(), c->L.page.size() * sizeof(ChunkItem));
       put(c->L.off_merge, c->L.merge.data(), c->L.merge.size() * sizeof(ChunkMerge));
@@ -424,6 +501,7 @@ pad_status pad_chunk_get_info(const pad_chunk_t* c, pad_chunk_info* info) {
   info->n_new_pages = (int32_t)c->new_page.size();
   info->prefix_splits = c->L.pre_splits;
   info->page_splits = c->L.page_splits;
+  info->tc_items = (int32_t)c->L.tc.size();
   info->mma_items = (int32_t)(c->L.pre.size() + c->L.page.size());
   return PAD_OK;
 }
@@ -493,7 +571,7 @@ pad_status pad_chunk_attn(const pad_chunk_t* c, const void* q, int64_t q_stride,
   st = check_pools(c, k_pool, v_pool, k_scale, v_scale);
   if (st != PAD_OK) return st;
   if (!q || !out) return api_fail(PAD_ERR_INVALID_ARG, "NULL tensor");
-  if (c->has_prefix && (!k_prefix || !v_prefix)) return api_fail(PAD_ERR_INVALID_ARG, "the plan has a prefix, k_prefix or v_prefix is NULL");
+  if (c->L.has_prefix && (!k_prefix || !v_prefix)) return api_fail(PAD_ERR_INVALID_ARG, "the plan has a prefix, k_prefix or v_prefix is NULL");
   if (!aligned(q, 16) || !aligned(out, 16) || !aligned(k_prefix, 16) || !aligned(v_prefix, 16) || !aligned(lse, 4))
     return api_fail(PAD_ERR_INVALID_ARG, "tensors must be 16-byte aligned (lse 4-byte)");
   ChunkParams p = params_of(c);
@@ -509,7 +587,10 @@ pad_status pad_chunk_attn(const pad_chunk_t* c, const void* q, int64_t q_stride,
   p.lse = lse;
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   cudaError_t e = cudaSuccess;
-  if (!c->L.pre.empty())
+  if (!c->L.tc.empty())
+    e = launch_chunk_tc(p, c->prob.head_dim, c->kv_format == PAD_KV_FP8, c->L.tc_split, list<ChunkItem>(c, c->L.off_tc),
+                        (int)c->L.tc.size(), s);
+  if (e == cudaSuccess && !c->L.pre.empty())
     e = launch_chunk_mma(p, c->prob.head_dim, false, c->L.pre_rows16, list<ChunkItem>(c, c->L.off_pre), (int)c->L.pre.size(), s);
   if (e == cudaSuccess && !c->L.page.empty())
     e = launch_chunk_mma(p, c->prob.head_dim, c->kv_format == PAD_KV_FP8, c->L.page_rows16, list<ChunkItem>(c, c->L.off_page),
