@@ -81,8 +81,9 @@ int chunk_read_tokens();
 cudaError_t launch_chunk_mma(const ChunkParams& p, int head_dim, bool fp8, int rows16, const ChunkItem* items,
                              int n_items, cudaStream_t s);
 // split: one slot of 128 / group tokens per CTA, its tiles taken in turn by two halves; else two slots.
-cudaError_t launch_chunk_tc(const ChunkParams& p, int head_dim, bool fp8, bool split, const ChunkItem* items, int n_items,
-                            cudaStream_t s);
+// prefix_tokens: tokens of k_prefix up to the last one that an item reads, 0 without prefix items.
+cudaError_t launch_chunk_tc(const ChunkParams& p, int head_dim, bool fp8, bool split, int64_t prefix_tokens,
+                            const ChunkItem* items, int n_items, cudaStream_t s);
 cudaError_t launch_chunk_merge(const ChunkParams& p, int head_dim, const ChunkMerge* work, int n_work, cudaStream_t s);
 cudaError_t launch_draft_verify(const ChunkParams& p, const ChunkVerify* work, int n_events, int vocab, bool bf16,
                                 const void* tp, int64_t p_stride, const void* dq, int64_t q_stride,

@@ -93,6 +93,7 @@ struct Lists {
   std::vector<ChunkRead> read;
   std::vector<ChunkVerify> verify;
   int64_t n_tokens = 0, n_cached = 0, n_drafts = 0, partial_rows = 0;
+  int64_t prefix_tokens = 0;             // of k_prefix, up to the last one read
   int32_t n_spans = 0, pre_splits = 0, page_splits = 0;
   size_t off_tc = 0, off_pre = 0, off_page = 0, off_merge = 0, off_pages = 0, off_read = 0, off_verify = 0, image_bytes = 0;
   size_t off_ml = 0, off_o = 0, total = 0;
@@ -280,6 +281,7 @@ void build(const Batch& b, const int64_t* prefix_offset, Lists& L) {
     if (!s.paged) {
       s.src = off[s.src];
       L.has_prefix = true;
+      L.prefix_tokens = std::max(L.prefix_tokens, s.src + s.keys);
     }
     if (s.tc) items_of(s, prob, (L.tc_split ? 1 : 2) * (128 / G), L.tc);
     else items_of(s, prob, 16 * (s.paged ? L.page_rows16 : L.pre_rows16) / G, s.paged ? L.page : L.pre);
@@ -444,6 +446,7 @@ pad_status pad_chunk_plan(const pad_problem* prob, int32_t kv_format, pad_cache_
       c->n_new.assign(n_new, n_new + n_events);
     }
     build(b, prefix_offset, c->L);
+    if (c->L.prefix_tokens > INT32_MAX) return api_fail(PAD_ERR_UNSUPPORTED, "prefixes past 2^31 tokens of k_prefix");
     if (workspace && workspace_bytes < c->L.total)
       return api_fail(PAD_ERR_WORKSPACE_TOO_SMALL, "workspace has %zu bytes, the plan needs %zu", workspace_bytes, c->L.total);
     if (cache) {
@@ -588,7 +591,7 @@ pad_status pad_chunk_attn(const pad_chunk_t* c, const void* q, int64_t q_stride,
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   cudaError_t e = cudaSuccess;
   if (!c->L.tc.empty())
-    e = launch_chunk_tc(p, c->prob.head_dim, c->kv_format == PAD_KV_FP8, c->L.tc_split, list<ChunkItem>(c, c->L.off_tc),
+    e = launch_chunk_tc(p, c->prob.head_dim, c->kv_format == PAD_KV_FP8, c->L.tc_split, c->L.prefix_tokens, list<ChunkItem>(c, c->L.off_tc),
                         (int)c->L.tc.size(), s);
   if (e == cudaSuccess && !c->L.pre.empty())
     e = launch_chunk_mma(p, c->prob.head_dim, false, c->L.pre_rows16, list<ChunkItem>(c, c->L.off_pre), (int)c->L.pre.size(), s);

@@ -8,13 +8,15 @@
 // slot, whose tiles two halves of the softmax warps take in turn, each with an S buffer, a maximum and an O
 // of its own, joined at the end: the shorter chain where there are few rows.
 //
-//   warps 12-15  bring the tiles in, K and V alternating, 32 rows each: 16-byte cp.async into the
-//                128-byte-swizzled layout that the MMAs read, a page looked up per key (so every page size
-//                takes the same path, and no slot past a branch's last token is ever read).  Their arrival
-//                at the stage's barrier is left to the hardware, once a thread's copies have landed; the
-//                issuers fence the proxies.  8-bit tiles are staged as codes first, each thread widening
-//                those it has copied itself.  (Through registers instead, the fence behind a tile's stores
-//                waited for the next tile's loads: 2300 cycles per K or V tile.)
+//   warps 12-15  bring the tiles in.  bf16: TMA boxes of a page (of 128 tokens of a prefix) and 64 columns,
+//                128-byte swizzle, warp 12 those of K, warp 13 of V, a lane looking up and fetching one page;
+//                V tiles that some row does not see in full are looked over before they count as loaded
+//                (warps 13-15): slots past the last token hold anything.  Pages of four tokens, which are half a
+//                swizzle atom: 16-byte cp.async, 32 rows a warp, arrival left to the hardware, the
+//                issuers fence the proxies.  8 bits: codes by cp.async, each thread widening those it has
+//                copied itself.  (Through registers instead, the fence behind a tile's stores waited for
+//                the next tile's loads: 2300 cycles per K or V tile.  bf16 by cp.async throughout: 838 us for
+//                2048 new tokens over 30720, 28/4 heads; the pages' boxes take 701 us.)
 //   warp 0       S issuer: S_g(k) = Q_g K(k)^T
 //   warp 1       TMEM allocation (512 columns) and deallocation, P.V issuer: O_g += P_g(k) V(k), P read
 //                back from TMEM, 96 keys and then the last 32
@@ -76,8 +78,14 @@ struct Cfg {
 // Registers per thread after setmaxnreg: 512 x 128 at launch; 128 x 48 + 256 x 192 + 128 x 80 = 65536.
 constexpr int kRegsIssue = 48, kRegsSoftmax = 192, kRegsLoad = 80;
 
+struct ChunkMaps {
+  CUtensorMap k_pool, v_pool;      // rows of (page, head, slot), boxes of a page x 64 columns
+  CUtensorMap k_prefix, v_prefix;  // (column, head, token), boxes of 128 tokens x 64 columns
+  int32_t pages;                   // the pools' maps are there
+};
+
 struct Bars {
-  uint64_t kfull[4], kfree[4];  // (full: an arrival of every loader thread)
+  uint64_t kfull[4], kfree[4];  // (full: one arrival with the bytes; by cp.async one of every loader thread)
   uint64_t vfull[4], vfree[4];
   uint64_t sfull[2];
   uint64_t plo[2], phi[2];
@@ -85,6 +93,7 @@ struct Bars {
   uint64_t pvdone[2];
   uint64_t drain_s, drain_pv;
   uint64_t tdone;
+  uint64_t vraw, vbad;          // V tiles that are looked over once they have landed
   alignas(16) uint32_t mask[kMasks][4];  // which keys of the tile are there
   uint32_t tmem_base;
   int32_t abort;
@@ -193,7 +202,8 @@ __device__ __forceinline__ void proxy_fence() { asm volatile("fence.proxy.async.
 
 template <int D, bool FP8, bool SPLIT>
 __global__ void __launch_bounds__(kThreads, 1)
-    chunk_tc_kernel(const __grid_constant__ ChunkParams p, const ChunkItem* __restrict__ items) {
+    chunk_tc_kernel(const __grid_constant__ ChunkParams p, const __grid_constant__ ChunkMaps maps,
+                    const ChunkItem* __restrict__ items) {
   using C = Cfg<D, FP8>;
   extern __shared__ __align__(1024) uint8_t smem[];
   const uint32_t sbase = smem_u32(smem);
@@ -216,11 +226,14 @@ __global__ void __launch_bounds__(kThreads, 1)
     return;
   }
 
-  if (threadIdx.x == 0) {
+  const bool paged = it.paged != 0;
+  const bool wide = FP8 && paged;                     // 8-bit tiles
+  const bool bulk = !wide && (!paged || maps.pages);  // tiles by TMA
+  if (threadIdx.x == 384) {  // (of the warp that fetches the first tile)
     for (int s = 0; s < 4; ++s) {
-      mbar_init(&bars->kfull[s], 128);
+      mbar_init(&bars->kfull[s], bulk ? 1 : 128);
       mbar_init(&bars->kfree[s], 1);
-      mbar_init(&bars->vfull[s], 128);
+      mbar_init(&bars->vfull[s], bulk ? 1 : 128);
       mbar_init(&bars->vfree[s], 1);
     }
     for (int g = 0; g < 2; ++g) {
@@ -233,6 +246,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     mbar_init(&bars->drain_s, 1);
     mbar_init(&bars->drain_pv, 1);
     mbar_init(&bars->tdone, 8);
+    mbar_init(&bars->vraw, 1);
+    mbar_init(&bars->vbad, 1);
     bars->abort = 0;
     bars->dirty = 0;
     bars->item = it;
@@ -246,9 +261,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   }
 
   // What a loader warp needs of its 32 rows of a tile, lane L's being 32 w + L.
-  const bool paged = it.paged != 0;
   const int w = warp & 3;
-  const bool wide = FP8 && paged;               // 8-bit tiles
   const int32_t* table = p.page_table + (paged ? it.src * p.max_pages : 0);
   auto page_of = [&](int t) -> int {
     const int key = key0 + t * kBN + 32 * w + lane;
@@ -286,11 +299,57 @@ __global__ void __launch_bounds__(kThreads, 1)
       cp16(dst + r * 128 + (((c & 7) ^ (r & 7)) << 4), src + (uint64_t)i * mul + (on ? in : 0u), on * 16u);
     }
   };
+  // By TMA: lane L's page of a tile holds keys L x page size on; the pages that are there.
+  auto tile_page = [&](int t) -> int {
+    const int key = key0 + t * kBN + (lane << p.page_shift);
+    return paged && t < n_tiles && lane < (kBN >> p.page_shift) && key < key1 ? __ldg(table + (key >> p.page_shift)) : 0;
+  };
+  auto tile_pages = [&](int t, int page) -> uint32_t {
+    const int key = key0 + t * kBN + (lane << p.page_shift);
+    const bool in = paged && lane < (kBN >> p.page_shift) && key < key1, ok = in && (unsigned)page < (unsigned)p.n_pages;
+    if (in && !ok && warp == 12) pad_set_error(p.header, p.gen, PAD_ERR_DEVICE_BOUNDS, (int)it.src, key >> p.page_shift, page);
+    return __ballot_sync(0xffffffffu, ok);
+  };
+  auto key_there = [&](int t, int r, uint32_t pages) -> bool {
+    return key0 + t * kBN + r < key1 && (!paged || ((pages >> (r >> p.page_shift)) & 1u));
+  };
+  auto fetch_tile = [&](const CUtensorMap* pool, const CUtensorMap* prefix, uint32_t tile, int t, int page, uint32_t pages,
+                        uint64_t* full) {
+    if (paged) {
+      const uint32_t bytes = (uint32_t)__popc(pages) * (uint32_t)p.page_size * (2 * D);
+      if (lane == 0) {
+        if (bytes) mbar_expect_tx(full, bytes);
+        else mbar_arrive(full);
+      }
+      __syncwarp();
+      if ((pages >> lane) & 1u) {
+        const int row = (page * p.h_kv + kvh) << p.page_shift;  // (the map's rows are fewer than 2^31)
+#pragma unroll
+        for (int h = 0; h < C::kHalves; ++h)
+          tma_load_3d(tile + h * C::kBoxBytes + ((uint32_t)lane << p.page_shift) * 128, pool, 64 * h, 0, row, full);
+      }
+    } else if (lane == 0) {
+      mbar_expect_tx(full, C::kTileBytes);
+#pragma unroll
+      for (int h = 0; h < C::kHalves; ++h)
+        tma_load_3d(tile + h * C::kBoxBytes, prefix, 64 * h, kvh, (int)it.src + key0 + t * kBN, full);
+    }
+    __syncwarp();
+  };
   uint32_t idx = 0, there = 0;
   if (warp >= 12) {
-    // the first K tile goes out before the CTA has met (its arrival after)
-    rows_of(0, page_of(0), idx, there);
-    if (!wide) issue_bf16(k_base, sbase + C::kOffK, 0, idx, there);
+    // the first K tile goes out before the CTA has met (by cp.async: its arrival after)
+    if (bulk) {
+      if (warp == 12) {
+        const int page = tile_page(0);
+        there = tile_pages(0, page);
+        __syncwarp();
+        fetch_tile(&maps.k_pool, &maps.k_prefix, sbase + C::kOffK, 0, page, there, &bars->kfull[0]);
+      }
+    } else {
+      rows_of(0, page_of(0), idx, there);
+      if (!wide) issue_bf16(k_base, sbase + C::kOffK, 0, idx, there);
+    }
   } else {
     // Q of the slots by the others: row = token * G + head; what has no token is zero
     constexpr int CH = D / 8;
@@ -319,7 +378,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       int s = 0, ph = 0;
       for (int t = 0; t < n_tiles && ok; ++t) {
         ok = cwait_warp(&bars->kfull[s], (uint32_t)ph, bars, p, 3);
-        proxy_fence();  // (the loaders' writes, before the MMAs read them)
+        if (!bulk) proxy_fence();  // (the loaders' writes, before the MMAs read them)
         const int j = SPLIT ? t >> 1 : t;  // the slot's how-manieth tile
 #pragma unroll
         for (int i = 0; i < (SPLIT ? 1 : 2); ++i) {
@@ -358,7 +417,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       for (int t = 0; t < n_tiles && ok; ++t) {
         if (!early) {
           ok = cwait_warp(&bars->vfull[s], (uint32_t)ph, bars, p, 4);
-          proxy_fence();
+          if (!bulk) proxy_fence();
         }
         early = false;
         const uint64_t vd = dV + ((uint32_t)s * C::kTileBytes >> 4);
@@ -387,7 +446,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             // (between the two slots there is time: the next tile's V, if it is there already)
             if (!SPLIT && h == 1 && g == 0 && ok && t + 1 < n_tiles) {
               early = __all_sync(0xffffffffu, mbar_test(&bars->vfull[s + 1 == C::kVS ? 0 : s + 1], (uint32_t)(s + 1 == C::kVS ? ph ^ 1 : ph)));
-              if (early) proxy_fence();
+              if (early && !bulk) proxy_fence();
             }
           }
         }
@@ -415,7 +474,129 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (lane == 0) bars->mask[t % kMasks][w] = there;
     };
     int ks = 0, kph = 0, vs = 0, vph = 0;  // a tile's stages, and how often they have been used before
-    if (!wide) {
+    if (bulk) {
+      // the tiles from here on are looked over: not every row sees them in full
+      const int t_look = min(n_tiles, max(0, all_see - key0) / kBN);
+      const uint32_t every = paged ? (kBN >> p.page_shift) >= 32 ? 0xffffffffu : (1u << (kBN >> p.page_shift)) - 1u : 0u;
+      // A landed V tile: keys that are not there become zeros, values that are not finite and that some row
+      // does not see are left out.
+      auto look = [&](int t, uint32_t tile, uint32_t pages, int r_lo, int thread, int threads) {
+        constexpr int CH = D / 8;
+        bool bad = false;
+#pragma unroll 2
+        for (int i = thread; i < (kBN - r_lo) * CH; i += threads) {
+          const int r = r_lo + i / CH, c = i % CH;
+          const uint32_t a = tile + (c >> 3) * C::kBoxBytes + r * 128 + (((c & 7) ^ (r & 7)) << 4);
+          if (!key_there(t, r, pages)) {
+            sts128(a, make_uint4(0u, 0u, 0u, 0u));
+          } else if (key0 + t * kBN + r >= all_see) {
+            const uint4 v = lds128(a);
+            if (odd2(v.x) | odd2(v.y) | odd2(v.z) | odd2(v.w)) {
+              bad = true;
+              sts128(a, make_uint4(clean2(v.x), clean2(v.y), clean2(v.z), clean2(v.w)));
+            }
+          }
+        }
+        if (bad) *reinterpret_cast<volatile int32_t*>(&bars->dirty) = 1;
+        proxy_fence();
+      };
+      if (warp == 12) {
+        int page = 0, issued = 0;
+        for (int t = 0; t < n_tiles; ++t) {
+          if (t > 0) {
+            there = tile_pages(t, page);
+            if (kph > 0) ok = cwait_warp(&bars->kfree[ks], (uint32_t)((kph - 1) & 1), bars, p, 1);
+            if (!ok) break;
+          }
+          uint32_t mine = 0u;  // lane's word of the mask
+          if (key0 + (t + 1) * kBN <= key1 && (!paged || there == every)) {
+            mine = 0xffffffffu;
+          } else {
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+              const uint32_t m = __ballot_sync(0xffffffffu, key_there(t, 32 * u + lane, there));
+              if (lane == u) mine = m;
+            }
+          }
+          if (lane < 4) bars->mask[t % kMasks][lane] = mine;
+          __syncwarp();
+          if (t > 0) fetch_tile(&maps.k_pool, &maps.k_prefix, sbase + C::kOffK + (uint32_t)ks * C::kTileBytes, t, page, there, &bars->kfull[ks]);
+          page = tile_page(t + 1);
+          issued = t + 1;
+          if (++ks == C::kKS) {
+            ks = 0;
+            ++kph;
+          }
+        }
+        // given up: the loads under way must land before the CTA leaves
+        if (!ok)
+          for (int t = max(0, issued - C::kKS); t < issued; ++t) drain_wait(&bars->kfull[t % C::kKS], (uint32_t)((t / C::kKS) & 1));
+      } else {
+        // (the three warps agree on going on: one that leaves alone would leave the others at their barrier)
+        auto agree = [&](bool fine) -> bool {
+          uint32_t all;
+          asm volatile("{\n .reg .pred p, q;\n setp.ne.u32 q, %1, 0;\n barrier.cta.red.and.pred p, 2, 96, q;\n selp.u32 %0, 1, 0, p;\n}\n"
+                       : "=r"(all) : "r"((uint32_t)fine) : "memory");
+          return all != 0;
+        };
+        int page = warp == 13 ? tile_page(0) : 0, issued = 0, gaps = 0;
+        if (warp == 13) {
+          for (int t = 0; t < t_look; ++t) {
+            const uint32_t tile = sbase + C::kOffV + (uint32_t)vs * C::kTileBytes;
+            const uint32_t pages = tile_pages(t, page);
+            if (vph > 0) ok = cwait_warp(&bars->vfree[vs], (uint32_t)((vph - 1) & 1), bars, p, 2);
+            if (!ok) break;
+            const bool gap = pages != every;
+            fetch_tile(&maps.v_pool, &maps.v_prefix, tile, t, page, pages, gap ? &bars->vbad : &bars->vfull[vs]);
+            issued = t + 1;
+            page = tile_page(t + 1);
+            if (gap) {
+              ok = cwait_warp(&bars->vbad, (uint32_t)(gaps++ & 1), bars, p, 13);
+              if (!ok) break;
+              look(t, tile, pages, 0, lane, 32);
+              __syncwarp();
+              if (lane == 0) mbar_arrive(&bars->vfull[vs]);
+            }
+            if (++vs == C::kVS) {
+              vs = 0;
+              ++vph;
+            }
+          }
+        } else {
+          vs = t_look % C::kVS;
+        }
+        for (int t = t_look; t < n_tiles; ++t) {
+          const uint32_t tile = sbase + C::kOffV + (uint32_t)vs * C::kTileBytes;
+          if (warp > 13) page = tile_page(t);
+          const uint32_t pages = tile_pages(t, page);
+          if (warp == 13) {
+            if (ok && vph > 0) ok = cwait_warp(&bars->vfree[vs], (uint32_t)((vph - 1) & 1), bars, p, 2);
+            if (ok) {
+              fetch_tile(&maps.v_pool, &maps.v_prefix, tile, t, page, pages, &bars->vraw);
+              issued = t + 1;
+              page = tile_page(t + 1);
+            }
+          }
+          if (ok) ok = cwait_warp(&bars->vraw, (uint32_t)((t - t_look) & 1), bars, p, 14);
+          if (ok) {
+            const int keys = min(key1 - key0 - t * kBN, kBN);  // of the tile, if all of their pages are there
+            const int n = (keys + p.page_size - 1) >> p.page_shift;
+            const bool gap = paged && pages != (n >= 32 ? 0xffffffffu : (1u << n) - 1u);
+            look(t, tile, pages, gap ? 0 : paged ? min(max(0, all_see - key0 - t * kBN), kBN) : keys, (int)threadIdx.x - 416, 96);
+          }
+          ok = agree(ok);
+          if (!ok) break;
+          if (threadIdx.x == 416) mbar_arrive(&bars->vfull[vs]);
+          if (++vs == C::kVS) {
+            vs = 0;
+            ++vph;
+          }
+        }
+        if (!ok && warp == 13)
+          for (int t = max(0, issued - C::kVS); t < issued; ++t)
+            drain_wait(t >= t_look ? &bars->vraw : &bars->vfull[t % C::kVS], (uint32_t)((t >= t_look ? t - t_look : t / C::kVS) & 1));
+      }
+    } else if (!wide) {
       int page = page_of(1);
       note(0);
       for (int t = 0; t < n_tiles; ++t) {
@@ -836,7 +1017,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 }
 
 template <int D, bool FP8, bool SPLIT>
-cudaError_t launch(const ChunkParams& p, const ChunkItem* items, int n, cudaStream_t s) {
+cudaError_t launch(const ChunkParams& p, int64_t prefix_tokens, const ChunkItem* items, int n, cudaStream_t s) {
   static bool configured[64] = {};
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
@@ -847,20 +1028,30 @@ cudaError_t launch(const ChunkParams& p, const ChunkItem* items, int n, cudaStre
     if (dev >= 0 && dev < 64) configured[dev] = true;
   }
   if ((int64_t)n * p.h_kv > INT32_MAX) return cudaErrorInvalidValue;
-  chunk_tc_kernel<D, FP8, SPLIT><<<n * p.h_kv, kThreads, Cfg<D, FP8>::kSmemBytes, s>>>(p, items);
+  ChunkMaps maps = {};
+  const int64_t rows = (int64_t)p.n_pages * p.h_kv * p.page_size;
+  if (!FP8 && p.page_size >= 8 && rows > 0 && rows <= INT32_MAX) {
+    if (!tma_map(&maps.k_pool, p.k_pool, D, 1, rows, 1, p.page_size) || !tma_map(&maps.v_pool, p.v_pool, D, 1, rows, 1, p.page_size))
+      return cudaErrorInvalidValue;
+    maps.pages = 1;
+  }
+  if (prefix_tokens > 0 && !prefix_tensor_maps(p.k_prefix, p.v_prefix, D, p.h_kv, prefix_tokens, &maps.k_prefix, &maps.v_prefix))
+    return cudaErrorInvalidValue;
+  chunk_tc_kernel<D, FP8, SPLIT><<<n * p.h_kv, kThreads, Cfg<D, FP8>::kSmemBytes, s>>>(p, maps, items);
   return cudaGetLastError();
 }
 
 }  // namespace
 
-cudaError_t launch_chunk_tc(const ChunkParams& p, int head_dim, bool fp8, bool split, const ChunkItem* items, int n_items,
-                            cudaStream_t s) {
+cudaError_t launch_chunk_tc(const ChunkParams& p, int head_dim, bool fp8, bool split, int64_t prefix_tokens,
+                            const ChunkItem* items, int n, cudaStream_t s) {
+  if (prefix_tokens > INT32_MAX) return cudaErrorInvalidValue;  // (the maps' token coordinates; checked when planning)
   if (head_dim == 128) {
-    if (split) return fp8 ? launch<128, true, true>(p, items, n_items, s) : launch<128, false, true>(p, items, n_items, s);
-    return fp8 ? launch<128, true, false>(p, items, n_items, s) : launch<128, false, false>(p, items, n_items, s);
+    if (split) return fp8 ? launch<128, true, true>(p, prefix_tokens, items, n, s) : launch<128, false, true>(p, prefix_tokens, items, n, s);
+    return fp8 ? launch<128, true, false>(p, prefix_tokens, items, n, s) : launch<128, false, false>(p, prefix_tokens, items, n, s);
   }
-  if (split) return fp8 ? launch<64, true, true>(p, items, n_items, s) : launch<64, false, true>(p, items, n_items, s);
-  return fp8 ? launch<64, true, false>(p, items, n_items, s) : launch<64, false, false>(p, items, n_items, s);
+  if (split) return fp8 ? launch<64, true, true>(p, prefix_tokens, items, n, s) : launch<64, false, true>(p, prefix_tokens, items, n, s);
+  return fp8 ? launch<64, true, false>(p, prefix_tokens, items, n, s) : launch<64, false, false>(p, prefix_tokens, items, n, s);
 }
 
 }  // namespace pad
