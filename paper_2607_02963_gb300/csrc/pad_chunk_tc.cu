@@ -93,7 +93,7 @@ struct Bars {
   uint64_t pvdone[2];
   uint64_t drain_s, drain_pv;
   uint64_t tdone;
-  uint64_t vraw, vbad;          // V tiles that are looked over once they have landed
+  uint64_t vraw, vbad, vlooked; // V tiles that are looked over once they have landed (by three warps together, by one)
   alignas(16) uint32_t mask[kMasks][4];  // which keys of the tile are there
   uint32_t tmem_base;
   int32_t abort;
@@ -248,6 +248,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     mbar_init(&bars->tdone, 8);
     mbar_init(&bars->vraw, 1);
     mbar_init(&bars->vbad, 1);
+    mbar_init(&bars->vlooked, 3);
     bars->abort = 0;
     bars->dirty = 0;
     bars->item = it;
@@ -532,13 +533,6 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (!ok)
           for (int t = max(0, issued - C::kKS); t < issued; ++t) drain_wait(&bars->kfull[t % C::kKS], (uint32_t)((t / C::kKS) & 1));
       } else {
-        // (the three warps agree on going on: one that leaves alone would leave the others at their barrier)
-        auto agree = [&](bool fine) -> bool {
-          uint32_t all;
-          asm volatile("{\n .reg .pred p, q;\n setp.ne.u32 q, %1, 0;\n barrier.cta.red.and.pred p, 2, 96, q;\n selp.u32 %0, 1, 0, p;\n}\n"
-                       : "=r"(all) : "r"((uint32_t)fine) : "memory");
-          return all != 0;
-        };
         int page = warp == 13 ? tile_page(0) : 0, issued = 0, gaps = 0;
         if (warp == 13) {
           for (int t = 0; t < t_look; ++t) {
@@ -569,24 +563,27 @@ __global__ void __launch_bounds__(kThreads, 1)
           const uint32_t tile = sbase + C::kOffV + (uint32_t)vs * C::kTileBytes;
           if (warp > 13) page = tile_page(t);
           const uint32_t pages = tile_pages(t, page);
+          const uint32_t par = (uint32_t)((t - t_look) & 1);
           if (warp == 13) {
             if (ok && vph > 0) ok = cwait_warp(&bars->vfree[vs], (uint32_t)((vph - 1) & 1), bars, p, 2);
-            if (ok) {
-              fetch_tile(&maps.v_pool, &maps.v_prefix, tile, t, page, pages, &bars->vraw);
-              issued = t + 1;
-              page = tile_page(t + 1);
-            }
+            if (!ok) break;
+            fetch_tile(&maps.v_pool, &maps.v_prefix, tile, t, page, pages, &bars->vraw);
+            issued = t + 1;
+            page = tile_page(t + 1);
           }
-          if (ok) ok = cwait_warp(&bars->vraw, (uint32_t)((t - t_look) & 1), bars, p, 14);
-          if (ok) {
-            const int keys = min(key1 - key0 - t * kBN, kBN);  // of the tile, if all of their pages are there
-            const int n = (keys + p.page_size - 1) >> p.page_shift;
-            const bool gap = paged && pages != (n >= 32 ? 0xffffffffu : (1u << n) - 1u);
-            look(t, tile, pages, gap ? 0 : paged ? min(max(0, all_see - key0 - t * kBN), kBN) : keys, (int)threadIdx.x - 416, 96);
-          }
-          ok = agree(ok);
+          ok = cwait_warp(&bars->vraw, par, bars, p, 14);
           if (!ok) break;
-          if (threadIdx.x == 416) mbar_arrive(&bars->vfull[vs]);
+          const int keys = min(key1 - key0 - t * kBN, kBN);  // of the tile, if all of their pages are there
+          const int n = (keys + p.page_size - 1) >> p.page_shift;
+          const bool gap = paged && pages != (n >= 32 ? 0xffffffffu : (1u << n) - 1u);
+          look(t, tile, pages, gap ? 0 : paged ? min(max(0, all_see - key0 - t * kBN), kBN) : keys, (int)threadIdx.x - 416, 96);
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&bars->vlooked);
+          if (warp == 13) {
+            ok = cwait_warp(&bars->vlooked, par, bars, p, 15);
+            if (!ok) break;
+            if (lane == 0) mbar_arrive(&bars->vfull[vs]);
+          }
           if (++vs == C::kVS) {
             vs = 0;
             ++vph;
@@ -827,13 +824,13 @@ __global__ void __launch_bounds__(kThreads, 1)
           // (a row that has seen no visible key keeps m = -inf; its exponent base is 0)
           part_exp<N>(s, sc2, m_run == kNegInf ? 0.f : m_run, tS + 16 * C0, sum);
         }
-        if (H == 0) load(kLoGroups, std::integral_constant<int, 4 - kLoGroups>{});
-#pragma unroll
-        for (int u = 0; u < 4; ++u) acc[u] = fadd2(acc[u], sum[u]);
         tmem_wait_st();
         fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(H ? &bars->phi[g] : &bars->plo[g]);
+        if (H == 0) load(kLoGroups, std::integral_constant<int, 4 - kLoGroups>{});
+#pragma unroll
+        for (int u = 0; u < 4; ++u) acc[u] = fadd2(acc[u], sum[u]);
         return true;
       };
       load(0, std::integral_constant<int, kLoGroups>{});
@@ -869,6 +866,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     uint8_t* so = smem + C::kOffK + (uint32_t)row * (4 * D);
     if (SPLIT) {
       sml[g * 128 + row] = make_float2(m_run, l);
+      __syncwarp();
       asm volatile("bar.sync 1, 256;" ::: "memory");
       const float2 other = sml[(g ^ 1) * 128 + row];
       // (l = 0: that half saw nothing; a NaN counts)
@@ -896,6 +894,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
         }
       }
+      __syncwarp();
       asm volatile("bar.sync 1, 256;" ::: "memory");
       wgt = has ? wgt : 0.f;
     }
