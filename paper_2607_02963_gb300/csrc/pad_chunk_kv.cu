@@ -33,51 +33,64 @@ __global__ void __launch_bounds__(kThreads) chunk_append_kernel(const __grid_con
   const ChunkPages w = work[blockIdx.x];
   int32_t* entry = p.page_table + (int64_t)w.event * p.max_pages + w.column;
   const int page = w.page >= 0 ? w.page : __ldg(entry);
-  if (w.page >= 0 && threadIdx.x == 0) *entry = page;
-  if ((unsigned)page >= (unsigned)p.n_pages) {
-    if (threadIdx.x == 0) pad_set_error(p.header, p.gen, PAD_ERR_DEVICE_BOUNDS, w.event, w.column, page);
-    return;
-  }
-  const int groups = w.count * p.h_kv * 2;
-  for (int i = threadIdx.x; i < (groups * L + 31) / 32 * 32; i += kThreads) {
-    const int g = i / L, c = i % L;
-    const bool on = g < groups;
-    const int tok = g / (2 * p.h_kv), r = g % (2 * p.h_kv), h = r >> 1;
-    uint4 x = make_uint4(0u, 0u, 0u, 0u);
-    if (on) x = __ldcs(reinterpret_cast<const uint4*>(((r & 1) ? v_new : k_new) + (w.tok + tok) * stride + h * D) + c);
-    const int64_t slot = ((int64_t)page * p.h_kv + h) * p.page_size + w.slot + tok;
-    if (!FP8) {
-      if (on) *(reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>((r & 1) ? v_pool : k_pool) + slot * D) + c) = x;
-      continue;
+  const int groups = w.count * p.h_kv * 2, lanes = (groups * L + 31) / 32 * 32, c = threadIdx.x % L;
+  constexpr int U = 4;  // groups of a thread under way together
+#pragma unroll 1
+  for (int i0 = threadIdx.x; i0 < lanes; i0 += U * kThreads) {
+    uint4 x[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int g = (i0 + u * kThreads) / L, tok = g / (2 * p.h_kv), r = g % (2 * p.h_kv);
+      x[u] = make_uint4(0u, 0u, 0u, 0u);
+      if (g < groups) x[u] = __ldcs(reinterpret_cast<const uint4*>(((r & 1) ? v_new : k_new) + (w.tok + tok) * stride + (r >> 1) * D) + c);
     }
-    // the largest magnitude as a bf16 pattern: integer order is theirs, NaN and infinity on top
-    uint32_t m = 0u;
-    const uint32_t xs[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-    for (int j = 0; j < 4; ++j) m = max(m, max(xs[j] & 0x7fffu, (xs[j] >> 16) & 0x7fffu));
-#pragma unroll
-    for (int o = L / 2; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
-    // max = f * 2^(e - 127) with f in [1, 2): max <= 448 * 2^k = 1.75 * 2^(k + 8).  (A subnormal's k
-    // is below the range in any case.)
-    const int e = (int)(m >> 7);
-    const int k = min(max(e - 127 - 8 + ((m & 0x7fu) > 0x60u ? 1 : 0), -120), 7);
-    const bool bad = m >= 0x7f80u;
-    const float inv = __uint_as_float((uint32_t)(127 - k) << 23);  // 2^-k
-    uint32_t code[2];
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      uint32_t two[2];
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const uint32_t v = xs[2 * j + u];
-        const float2 f = make_float2(__uint_as_float(v << 16) * inv, __uint_as_float(v & 0xffff0000u) * inv);
-        two[u] = __nv_cvt_float2_to_fp8x2(f, __NV_SATFINITE, __NV_E4M3);
+    // (the data is on its way while the page is looked up)
+    if (i0 == (int)threadIdx.x) {
+      if (w.page >= 0 && threadIdx.x == 0) *entry = page;
+      if ((unsigned)page >= (unsigned)p.n_pages) {
+        if (threadIdx.x == 0) pad_set_error(p.header, p.gen, PAD_ERR_DEVICE_BOUNDS, w.event, w.column, page);
+        return;
       }
-      code[j] = two[0] | (two[1] << 16);
     }
-    if (on) {
-      *(reinterpret_cast<uint2*>(static_cast<uint8_t*>((r & 1) ? v_pool : k_pool) + slot * D) + c) = make_uint2(code[0], code[1]);
-      if (c == 0) ((r & 1) ? v_scale : k_scale)[slot] = (uint8_t)(bad ? 255 : m == 0u ? 0 : k + 127);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (i0 + u * kThreads >= lanes) break;  // (whole warps)
+      const int g = (i0 + u * kThreads) / L, tok = g / (2 * p.h_kv), r = g % (2 * p.h_kv), h = r >> 1;
+      const bool on = g < groups;
+      const int64_t slot = ((int64_t)page * p.h_kv + h) * p.page_size + w.slot + tok;
+      if (!FP8) {
+        if (on) *(reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>((r & 1) ? v_pool : k_pool) + slot * D) + c) = x[u];
+        continue;
+      }
+      // the largest magnitude as a bf16 pattern: integer order is theirs, NaN and infinity on top
+      uint32_t m = 0u;
+      const uint32_t xs[4] = {x[u].x, x[u].y, x[u].z, x[u].w};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) m = max(m, max(xs[j] & 0x7fffu, (xs[j] >> 16) & 0x7fffu));
+#pragma unroll
+      for (int o = L / 2; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
+      // max = f * 2^(e - 127) with f in [1, 2): max <= 448 * 2^k = 1.75 * 2^(k + 8).  (A subnormal's k
+      // is below the range in any case.)
+      const int e = (int)(m >> 7);
+      const int k = min(max(e - 127 - 8 + ((m & 0x7fu) > 0x60u ? 1 : 0), -120), 7);
+      const bool bad = m >= 0x7f80u;
+      const float inv = __uint_as_float((uint32_t)(127 - k) << 23);  // 2^-k
+      uint32_t code[2];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        uint32_t two[2];
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+          const uint32_t v = xs[2 * j + q];
+          const float2 f = make_float2(__uint_as_float(v << 16) * inv, __uint_as_float(v & 0xffff0000u) * inv);
+          two[q] = __nv_cvt_float2_to_fp8x2(f, __NV_SATFINITE, __NV_E4M3);
+        }
+        code[j] = two[0] | (two[1] << 16);
+      }
+      if (on) {
+        *(reinterpret_cast<uint2*>(static_cast<uint8_t*>((r & 1) ? v_pool : k_pool) + slot * D) + c) = make_uint2(code[0], code[1]);
+        if (c == 0) ((r & 1) ? v_scale : k_scale)[slot] = (uint8_t)(bad ? 255 : m == 0u ? 0 : k + 127);
+      }
     }
   }
 }
@@ -91,44 +104,62 @@ __global__ void __launch_bounds__(kThreads) chunk_read_kernel(const __grid_const
                                                               __nv_bfloat16* __restrict__ v_out) {
   constexpr int L = D / 8;
   __shared__ int pages[kReadTokens];
+  __shared__ ChunkRead mine;
   __shared__ int event;
   const int b = (int)blockIdx.x;
   for (int e = threadIdx.x; e < n_events; e += kThreads) {
-    const int first = __ldg(&work[e].span0), spans = (__ldg(&work[e].count) + kReadTokens - 1) / kReadTokens;
-    if (b >= first && b < first + spans) event = e;  // (one event holds it)
+    const ChunkRead w = work[e];
+    if (b >= w.span0 && b < w.span0 + (w.count + kReadTokens - 1) / kReadTokens) mine = w, event = e;  // (one event holds it)
   }
   __syncthreads();
-  const ChunkRead w = work[event];
-  const int pos = (b - w.span0) * kReadTokens, count = min(kReadTokens, w.count - pos);
+  const int pos = (b - mine.span0) * kReadTokens, count = min(kReadTokens, mine.count - pos);
   if ((int)threadIdx.x < count) {
     const int col = (pos + (int)threadIdx.x) >> p.page_shift, pg = p.page_table[(int64_t)event * p.max_pages + col];
     pages[threadIdx.x] = pg;
     if ((unsigned)pg >= (unsigned)p.n_pages) pad_set_error(p.header, p.gen, PAD_ERR_DEVICE_BOUNDS, event, col, pg);
   }
   __syncthreads();
-  const int n = count * p.h_kv * L;
-  for (int i = threadIdx.x; i < n; i += kThreads) {
-    const int c = i % L, g = i / L, h = g % p.h_kv, t = g / p.h_kv;
-    const int pg = pages[t];
-    if ((unsigned)pg >= (unsigned)p.n_pages) continue;
-    const int64_t slot = ((int64_t)pg * p.h_kv + h) * p.page_size + ((pos + t) & (p.page_size - 1));
-    const int64_t to = ((w.out + pos + t) * p.h_kv + h) * D + 8 * c;
+  const int n = count * p.h_kv * L, c = threadIdx.x % L;
+  constexpr int U = 4;  // rows of a thread under way together, K and V
+#pragma unroll 1
+  for (int i0 = threadIdx.x; i0 < n; i0 += U * kThreads) {
+    uint4 x[U][2];
+    uint32_t sc[U][2];
+    int64_t to[U];
 #pragma unroll
-    for (int kv = 0; kv < 2; ++kv) {
-      const void* pool = kv ? p.v_pool : p.k_pool;
-      uint4 o;
-      if (FP8) {
-        const uint2 x = __ldg(reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(pool) + slot * D) + c);
-        uint32_t m = scale_mult(__ldg((kv ? p.v_scale : p.k_scale) + slot));
-        m |= m << 16;
-        o.x = e4m3_pair(__byte_perm(x.x, 0u, 0x1404), m);
-        o.y = e4m3_pair(__byte_perm(x.x, 0u, 0x3424), m);
-        o.z = e4m3_pair(__byte_perm(x.y, 0u, 0x1404), m);
-        o.w = e4m3_pair(__byte_perm(x.y, 0u, 0x3424), m);
-      } else {
-        o = __ldg(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(pool) + slot * D) + c);
+    for (int u = 0; u < U; ++u) {
+      const int i = i0 + u * kThreads, g = i / L, h = g % p.h_kv, t = g / p.h_kv;
+      const int pg = i < n ? pages[t] : -1;
+      to[u] = (unsigned)pg < (unsigned)p.n_pages ? ((mine.out + pos + t) * p.h_kv + h) * D + 8 * c : -1;
+      if (to[u] < 0) continue;
+      const int64_t slot = ((int64_t)pg * p.h_kv + h) * p.page_size + ((pos + t) & (p.page_size - 1));
+#pragma unroll
+      for (int kv = 0; kv < 2; ++kv) {
+        const void* pool = kv ? p.v_pool : p.k_pool;
+        if (FP8) {
+          const uint2 v = __ldg(reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(pool) + slot * D) + c);
+          x[u][kv].x = v.x;
+          x[u][kv].y = v.y;
+          sc[u][kv] = __ldg((kv ? p.v_scale : p.k_scale) + slot);
+        } else {
+          x[u][kv] = __ldg(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(pool) + slot * D) + c);
+        }
       }
-      __stcs(reinterpret_cast<uint4*>((kv ? v_out : k_out) + to), o);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (to[u] < 0) continue;
+#pragma unroll
+      for (int kv = 0; kv < 2; ++kv) {
+        uint4 o = x[u][kv];
+        if (FP8) {
+          uint32_t m = scale_mult(sc[u][kv]);
+          m |= m << 16;
+          o = make_uint4(e4m3_pair(__byte_perm(x[u][kv].x, 0u, 0x1404), m), e4m3_pair(__byte_perm(x[u][kv].x, 0u, 0x3424), m),
+                         e4m3_pair(__byte_perm(x[u][kv].y, 0u, 0x1404), m), e4m3_pair(__byte_perm(x[u][kv].y, 0u, 0x3424), m));
+        }
+        __stcs(reinterpret_cast<uint4*>((kv ? v_out : k_out) + to[u]), o);
+      }
     }
   }
 }

@@ -75,8 +75,8 @@ struct Cfg {
   static_assert(kSmemBytes <= 232448, "fits the 227 KB opt-in shared memory");
 };
 
-// Registers per thread after setmaxnreg: 512 x 128 at launch; 128 x 48 + 256 x 192 + 128 x 80 = 65536.
-constexpr int kRegsIssue = 48, kRegsSoftmax = 192, kRegsLoad = 80;
+// Registers per thread after setmaxnreg: 512 x 128 at launch; 128 x 48 + 256 x 184 + 128 x 96 = 65536.
+constexpr int kRegsIssue = 48, kRegsSoftmax = 184, kRegsLoad = 96;
 
 struct ChunkMaps {
   CUtensorMap k_pool, v_pool;      // rows of (page, head, slot), boxes of a page x 64 columns
@@ -187,16 +187,6 @@ __device__ __forceinline__ uint32_t clean2(uint32_t v) {
 // This thread's arrival, once all of its cp.async so far have completed.
 __device__ __forceinline__ void mbar_arrive_copies(uint64_t* bar) {
   asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
-}
-// Whether the phase has completed, without waiting (mbarrier.try_wait may suspend the thread for a while).
-__device__ __forceinline__ bool mbar_test(uint64_t* bar, uint32_t parity) {
-  uint32_t ok;
-  asm volatile(
-      "{\n .reg .pred p;\n mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}\n"
-      : "=r"(ok)
-      : "r"(smem_u32(bar)), "r"(parity)
-      : "memory");
-  return ok != 0;
 }
 __device__ __forceinline__ void proxy_fence() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
@@ -414,13 +404,9 @@ __global__ void __launch_bounds__(kThreads, 1)
       const bool el = elect_one();
       const uint64_t dV = sdesc(sbase + C::kOffV, C::kBoxBytes, 1024);
       int s = 0, ph = 0;
-      bool early = false;  // the tile's V has been waited for while the tile before was in work
       for (int t = 0; t < n_tiles && ok; ++t) {
-        if (!early) {
-          ok = cwait_warp(&bars->vfull[s], (uint32_t)ph, bars, p, 4);
-          if (!bulk) proxy_fence();
-        }
-        early = false;
+        ok = cwait_warp(&bars->vfull[s], (uint32_t)ph, bars, p, 4);
+        if (!bulk) proxy_fence();
         const uint64_t vd = dV + ((uint32_t)s * C::kTileBytes >> 4);
         const int j = SPLIT ? t >> 1 : t;
 #pragma unroll
@@ -444,11 +430,6 @@ __global__ void __launch_bounds__(kThreads, 1)
               }
             }
             __syncwarp();
-            // (between the two slots there is time: the next tile's V, if it is there already)
-            if (!SPLIT && h == 1 && g == 0 && ok && t + 1 < n_tiles) {
-              early = __all_sync(0xffffffffu, mbar_test(&bars->vfull[s + 1 == C::kVS ? 0 : s + 1], (uint32_t)(s + 1 == C::kVS ? ph ^ 1 : ph)));
-              if (early && !bulk) proxy_fence();
-            }
           }
         }
         if (++s == C::kVS) {

@@ -9,9 +9,9 @@
 // a probability down to 4e-12, and leaves 25 bits for the number of terms.
 //
 // Bound by bytes: one row of p and one of q per event.  A cluster of eight CTAs takes an event; each sums
-// an eighth of the rows, warp by warp over consecutive entries, the eight sums meet in distributed shared
-// memory, and the CTA that holds the point goes through the one warp's part it lies in again (a
-// 128th of the row, from L2).
+// an eighth of the rows, warp by warp over consecutive entries, hands its sum to the others through
+// distributed shared memory, and the CTA that holds the point goes through the one warp's part it lies
+// in again (a 128th of the row, from L2).
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
 #include <algorithm>
@@ -32,8 +32,11 @@ constexpr int kWarps = kThreads / 32;
 __device__ __forceinline__ float value(float x) { return x; }
 __device__ __forceinline__ float value(__nv_bfloat16 x) { return __bfloat162float(x); }
 
+// floor(2^38 min(r, 1)), 0 for a NaN: the 24-bit mantissa shifted (a 64-bit conversion takes longer).
 __device__ __forceinline__ int64_t weight(float r) {
-  return r > 0.f ? (int64_t)(fminf(r, 1.f) * 274877906944.f) : 0;  // 2^38 (a power of two: exact); NaN: 0
+  const uint32_t b = r > 0.f ? __float_as_uint(fminf(r, 1.f)) : 0u;
+  const uint64_t m = (uint64_t)((b & 0x7fffffu) | (b >= 0x800000u ? 0x800000u : 0u)) << 15;  // 2^38 at r = 1
+  return (int64_t)(m >> min(127u - (b >> 23), 63u));  // (a subnormal, far below 2^-38, becomes 0)
 }
 
 __device__ __forceinline__ int64_t warp_sum(int64_t v) {
@@ -49,8 +52,8 @@ __global__ void __cluster_dims__(kCtas, 1, 1) __launch_bounds__(kThreads)
                         const int32_t* __restrict__ draft, const float* __restrict__ u_accept,
                         const float* __restrict__ u_pick, int32_t* __restrict__ accepted, int32_t* __restrict__ token) {
   __shared__ int first_bad;
-  __shared__ int64_t part[2][kWarps];   // sums of each warp's entries: of the difference, of p
-  __shared__ int64_t mine[2];           // of this CTA's
+  __shared__ int64_t part[kWarps];       // sums of each warp's entries
+  __shared__ int64_t sums[2][kCtas];     // of each CTA's: first round, second round
   __shared__ int64_t scan[kWarps];
   cg::cluster_group cl = cg::this_cluster();
   const int rank = (int)cl.block_rank(), e = (int)blockIdx.x / kCtas;
@@ -60,6 +63,7 @@ __global__ void __cluster_dims__(kCtas, 1, 1) __launch_bounds__(kThreads)
     if (rank == 0 && threadIdx.x == 0) accepted[e] = 0, token[e] = -1;
     return;
   }
+  cl.barrier_arrive();  // (every CTA of the cluster runs before one writes into another's memory)
   if (threadIdx.x == 0) first_bad = w.n_draft;
   __syncthreads();
   for (int i = threadIdx.x; i < w.n_draft; i += kThreads) {
@@ -80,65 +84,61 @@ __global__ void __cluster_dims__(kCtas, 1, 1) __launch_bounds__(kThreads)
   const int per = (vocab + kCtas * kWarps - 1) / (kCtas * kWarps);
   auto begin_of = [&](int wp) { return (int)min((int64_t)vocab, (int64_t)(rank * kWarps + wp) * per); };
   const int lo = begin_of(warp), hi = min(vocab, lo + per);
-  int64_t d = 0, s = 0;
-  constexpr int U = 8;
-  for (int i0 = lo + lane; i0 < hi; i0 += 32 * U) {
-    float x[U], y[U];
+  // first of the difference, where there is one; of p itself if it has no weight (or there is none)
+  bool take = sub;
+  int64_t total = 0, before = 0, mine = 0;
+  for (int round = 0;; ++round) {
+    int64_t s = 0;
+    constexpr int U = 8;
+    for (int i0 = lo + lane; i0 < hi; i0 += 32 * U) {
+      float x[U], y[U];
 #pragma unroll
-    for (int j = 0; j < U; ++j) {
-      x[j] = y[j] = 0.f;
-      if (i0 + 32 * j < hi) {
-        x[j] = value(pa[i0 + 32 * j]);
-        if (sub) y[j] = value(qa[i0 + 32 * j]);
+      for (int j = 0; j < U; ++j) {
+        x[j] = y[j] = 0.f;
+        if (i0 + 32 * j < hi) {
+          x[j] = value(pa[i0 + 32 * j]);
+          if (take) y[j] = value(qa[i0 + 32 * j]);
+        }
       }
-    }
 #pragma unroll
-    for (int j = 0; j < U; ++j) {
-      s += weight(x[j]);
-      if (sub) d += weight(x[j] - y[j]);
+      for (int j = 0; j < U; ++j) s += weight(x[j] - y[j]);
     }
-  }
-  s = warp_sum(s);
-  d = sub ? warp_sum(d) : s;
-  if (lane == 0) part[0][warp] = d, part[1][warp] = s;
-  __syncthreads();
-  if (threadIdx.x < 2) {
-    int64_t t = 0;
-    for (int k = 0; k < kWarps; ++k) t += part[threadIdx.x][k];
-    mine[threadIdx.x] = t;
-  }
-  cl.sync();
-  int64_t total[2] = {0, 0}, before[2] = {0, 0};
-#pragma unroll
-  for (int k = 0; k < kCtas; ++k) {
-    const int64_t* m = cl.map_shared_rank(mine, k);
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      const int64_t v = m[u];
-      if (k < rank) before[u] += v;
-      total[u] += v;
+    s = warp_sum(s);
+    if (lane == 0) part[warp] = s;
+    __syncthreads();
+    if (round == 0) cl.barrier_wait();
+    if (threadIdx.x < kCtas) {
+      int64_t t = 0;
+      for (int k = 0; k < kWarps; ++k) t += part[k];
+      *cl.map_shared_rank(&sums[round][rank], threadIdx.x) = t;
     }
+    cl.sync();  // (nobody reads another CTA's memory after this)
+    total = before = 0;
+#pragma unroll
+    for (int k = 0; k < kCtas; ++k) {
+      const int64_t v = sums[round][k];
+      if (k < rank) before += v;
+      total += v;
+    }
+    mine = sums[round][rank];
+    if (total > 0 || !take) break;
+    take = false;
   }
-  cl.sync();  // (nobody leaves while its sums may still be read)
-  const bool diff = total[0] > 0;  // else: nothing left of the difference, p itself
-  const int64_t sum = diff ? total[0] : total[1];
   if (rank == 0 && threadIdx.x == 0) {
     accepted[e] = a;
-    if (sum == 0) token[e] = -1;
+    if (total == 0) token[e] = -1;
   }
-  if (sum == 0) return;
+  if (total == 0) return;
   const float u = u_pick[e];
   const int64_t m = (int64_t)fminf(fmaxf(floorf(u * 16777216.f), 0.f), 16777215.f);  // (a NaN: 0)
-  const int64_t goal = m * (sum >> 24) + ((m * (sum & 0xffffff)) >> 24) - (diff ? before[0] : before[1]);
-  if (goal < 0 || goal >= (diff ? mine[0] : mine[1])) return;  // (the whole CTA)
-  const int64_t* ps = part[diff ? 0 : 1];
+  const int64_t goal = m * (total >> 24) + ((m * (total & 0xffffff)) >> 24) - before;
+  if (goal < 0 || goal >= mine) return;  // (the whole CTA)
   int wp = 0;
   int64_t base = 0;
-  while (wp < kWarps - 1 && base + ps[wp] <= goal) base += ps[wp++];
+  while (wp < kWarps - 1 && base + part[wp] <= goal) base += part[wp++];
   // that warp's entries again, a few consecutive ones per thread
   const int wlo = begin_of(wp), whi = min(vocab, wlo + per);
   const int c = (whi - wlo + kThreads - 1) / kThreads, tlo = min(whi, wlo + (int)threadIdx.x * c), thi = min(whi, tlo + c);
-  const bool take = sub && diff;
   auto weight_of = [&](int i) { return weight(take ? value(pa[i]) - value(qa[i]) : value(pa[i])); };
   int64_t t = 0;
   for (int i = tlo; i < thi; ++i) t += weight_of(i);
