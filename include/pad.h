@@ -511,7 +511,8 @@ pad_status pad_prefill_status(pad_stream_t stream);
  * 8-bit groups: with a = max|x| over the head_dim values, k is the smallest integer with
  * a <= 448 * 2^k, kept in [-120, 7]; a code is x / 2^k in e4m3, rounded to nearest even, values
  * beyond +-448 (a > 57344) saturated; the scale byte is k + 127, or 0 for a group of zeros, or
- * 255 for a group that holds a NaN or an infinity, which reads back as NaN throughout.  A power
+ * 255 for a group that holds a NaN or an infinity, which reads back as NaN throughout (its codes
+ * are 0; the codes 0x7f and 0xff do not occur).  A power
  * of two costs e4m3 no accuracy (its relative spacing is the same everywhere) and makes code
  * times scale exact in bf16: what the attention multiplies is what pad_chunk_read returns.
  * --------------------------------------------------------------------------- */

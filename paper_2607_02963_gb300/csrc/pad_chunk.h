@@ -84,7 +84,8 @@ cudaError_t launch_chunk_mma(const ChunkParams& p, int head_dim, bool fp8, int r
 // prefix_tokens: tokens of k_prefix up to the last one that an item reads, 0 without prefix items.
 cudaError_t launch_chunk_tc(const ChunkParams& p, int head_dim, bool fp8, bool split, int64_t prefix_tokens,
                             const ChunkItem* items, int n_items, cudaStream_t s);
-cudaError_t launch_chunk_merge(const ChunkParams& p, int head_dim, const ChunkMerge* work, int n_work, cudaStream_t s);
+// most: splits of the row that has the most.
+cudaError_t launch_chunk_merge(const ChunkParams& p, int head_dim, int most, const ChunkMerge* work, int n_work, cudaStream_t s);
 cudaError_t launch_draft_verify(const ChunkParams& p, const ChunkVerify* work, int n_events, int vocab, bool bf16,
                                 const void* tp, int64_t p_stride, const void* dq, int64_t q_stride,
                                 const int32_t* draft, const float* u_accept, const float* u_pick, int32_t* accepted,

@@ -599,7 +599,7 @@ pad_status pad_chunk_attn(const pad_chunk_t* c, const void* q, int64_t q_stride,
     e = launch_chunk_mma(p, c->prob.head_dim, c->kv_format == PAD_KV_FP8, c->L.page_rows16, list<ChunkItem>(c, c->L.off_page),
                          (int)c->L.page.size(), s);
   if (e == cudaSuccess && !c->L.merge.empty())
-    e = launch_chunk_merge(p, c->prob.head_dim, list<ChunkMerge>(c, c->L.off_merge), (int)c->L.merge.size(), s);
+    e = launch_chunk_merge(p, c->prob.head_dim, c->L.pre_splits + c->L.page_splits, list<ChunkMerge>(c, c->L.off_merge), (int)c->L.merge.size(), s);
   return e == cudaSuccess ? PAD_OK : cuda_fail(e, "chunk attention launch");
 }
 

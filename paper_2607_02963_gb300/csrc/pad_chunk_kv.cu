@@ -83,7 +83,7 @@ __global__ void __launch_bounds__(kThreads) chunk_append_kernel(const __grid_con
         for (int q = 0; q < 2; ++q) {
           const uint32_t v = xs[2 * j + q];
           const float2 f = make_float2(__uint_as_float(v << 16) * inv, __uint_as_float(v & 0xffff0000u) * inv);
-          two[q] = __nv_cvt_float2_to_fp8x2(f, __NV_SATFINITE, __NV_E4M3);
+          two[q] = bad ? 0u : __nv_cvt_float2_to_fp8x2(f, __NV_SATFINITE, __NV_E4M3);  // (codes are finite, always)
         }
         code[j] = two[0] | (two[1] << 16);
       }

@@ -9,13 +9,19 @@
 // states that chunk_merge_kernel joins, when the item is one of several of its rows.
 //
 // 8-bit caches: the codes are staged as they are (half the bytes in flight buys twice the keys) and
-// widened to bf16 in the fragments: a K word holds four dimensions of a key (which Q's fragments follow:
-// the order of a sum's terms is free), a V word four columns of a key, so that words of two keys give the
-// pairs P.V wants without a transpose.  Code times scale is exact in bf16, so the products are those
-// of the values that pad_chunk_read returns.
+// widened in the fragments to f16, which holds every e4m3 value exactly, two codes an instruction; the
+// scales of K multiply the scores, those of V the weights.  A K word holds four dimensions of a key
+// (which Q's fragments follow: the order of a sum's terms is free), a V word four columns of a key, so
+// that words of two keys give the pairs P.V wants without a transpose.  Range: Q rows are scaled by a
+// power of two to below 2^15 (exact down to 2^-29 of their largest value), weights go in as p 2^(k - r + 15)
+// with r the largest V scale so far, which is exact to eleven bits down to 2^-29 of r's; a block whose scales
+// lie further apart than 2^12 takes V widened to bf16 instead, whose range is that of fp32.
+// (Widened to bf16 throughout, four to five integer instructions a pair: 129 us for 295k cached tokens, 28/4 heads,
+// no faster than the bf16 cache.)
 //
 // P goes into P.V rounded to bf16 (2^-8 of each weight at most, as in every kernel of this library); the row sum is that of the unrounded fp32 weights, and all states are fp32.
 #include <cuda_bf16.h>
+#include <cuda_fp16.h>
 #include <algorithm>
 #include <cstdint>
 
@@ -72,6 +78,30 @@ __device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint3
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma_f16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// The two e4m3 codes in the lower half of x as f16, exactly.
+__device__ __forceinline__ uint32_t f16_of_e4m3(uint32_t x) {
+  uint32_t r;
+  asm("{\n .reg .b16 lo, hi;\n mov.b32 {lo, hi}, %1;\n cvt.rn.f16x2.e4m3x2 %0, lo;\n}\n" : "=r"(r) : "r"(x));
+  return r;
+}
+__device__ __forceinline__ uint32_t f16_of_e4m3_hi(uint32_t x) {
+  uint32_t r;
+  asm("{\n .reg .b16 lo, hi;\n mov.b32 {lo, hi}, %1;\n cvt.rn.f16x2.e4m3x2 %0, hi;\n}\n" : "=r"(r) : "r"(x));
+  return r;
+}
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+  const __half2 h = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&h);
+}
+// 2^(byte - 127), 0 for a group of zeros, NaN for one that holds a NaN.
+__device__ __forceinline__ float scale_value(uint32_t byte) {
+  return byte == 255u ? __uint_as_float(0x7fc00000u) : byte == 0u ? 0.f : __uint_as_float(min(max(byte, 7u), 134u) << 23);
 }
 __device__ __forceinline__ uint32_t lds32(uint32_t a) {
   uint32_t v;
@@ -151,8 +181,10 @@ __global__ void __launch_bounds__(kThreads) chunk_mma_kernel(const __grid_consta
     page = next;
   }
 
-  // Q fragments (rows g and g + 8 of each 16-row group), in the order of K's
+  // Q fragments (rows g and g + 8 of each 16-row group), in the order of K's; 8 bits: as f16 of the row
+  // times 2^-e, e such that its largest value lies in [2^14, 2^15), and what a score is to be multiplied by
   uint32_t qf[MT][D / 16][4];
+  float qs[MT][2];
 #pragma unroll
   for (int m = 0; m < MT; ++m)
 #pragma unroll
@@ -160,32 +192,46 @@ __global__ void __launch_bounds__(kThreads) chunk_mma_kernel(const __grid_consta
       const int r = 16 * m + 8 * u + g;
       const bool on = r < n_rows;
       const __nv_bfloat16* src = p.q + (on ? (it.tok0 + r / G) * p.q_stride + (int64_t)(h * G + r % G) * D : 0);
+      if (FP8) {
+        uint2 x[D / 16];
+        uint32_t top = 0u;
 #pragma unroll
-      for (int j = 0; j < D / 16; ++j) {
-        uint32_t a = 0u, b = 0u;
-        if (on) {
-          if (FP8) {
-            const uint2 x = __ldg(reinterpret_cast<const uint2*>(src + 16 * j + 4 * t4));
-            a = __byte_perm(x.x, x.y, 0x5410);
-            b = __byte_perm(x.x, x.y, 0x7632);
-          } else {
-            a = __ldg(reinterpret_cast<const uint32_t*>(src + 16 * j + 2 * t4));
-            b = __ldg(reinterpret_cast<const uint32_t*>(src + 16 * j + 2 * t4 + 8));
-          }
+        for (int j = 0; j < D / 16; ++j) {
+          x[j] = on ? __ldg(reinterpret_cast<const uint2*>(src + 16 * j + 4 * t4)) : make_uint2(0u, 0u);
+          top = max(max(max(top, x[j].x & 0x7fffu), max((x[j].x >> 16) & 0x7fffu, x[j].y & 0x7fffu)), (x[j].y >> 16) & 0x7fffu);
         }
-        qf[m][j][u] = a;
-        qf[m][j][2 + u] = b;
+        top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+        top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+        // (the exponent kept where both powers of two are normal numbers; a row with a NaN or an infinity
+        // keeps it whatever the scale)
+        const int e = min(max((int)(top >> 7) - 127 - 14, -120), 113);
+        const float down = __uint_as_float((uint32_t)(127 - e) << 23);
+        qs[m][u] = p.scale_log2 * __uint_as_float((uint32_t)(127 + e) << 23);
+#pragma unroll
+        for (int j = 0; j < D / 16; ++j) {
+          qf[m][j][u] = pack_f16(__uint_as_float(x[j].x << 16) * down, __uint_as_float(x[j].x & 0xffff0000u) * down);
+          qf[m][j][2 + u] = pack_f16(__uint_as_float(x[j].y << 16) * down, __uint_as_float(x[j].y & 0xffff0000u) * down);
+        }
+      } else {
+        qs[m][u] = p.scale_log2;
+#pragma unroll
+        for (int j = 0; j < D / 16; ++j) {
+          qf[m][j][u] = on ? __ldg(reinterpret_cast<const uint32_t*>(src + 16 * j + 2 * t4)) : 0u;
+          qf[m][j][2 + u] = on ? __ldg(reinterpret_cast<const uint32_t*>(src + 16 * j + 2 * t4 + 8)) : 0u;
+        }
       }
     }
-  // keys that each of the thread's rows sees
-  int lim[MT][2];
+  // keys that each of the thread's rows sees, and that all rows see
+  int lim[MT][2], lim_all = 0x7fffffff;
 #pragma unroll
   for (int m = 0; m < MT; ++m)
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       const int r = 16 * m + 8 * u + g;
       lim[m][u] = r < n_rows ? min(it.lim0 + (it.paged ? r / G : 0), it.key1) : 0;
+      if (r < n_rows) lim_all = min(lim_all, lim[m][u]);
     }
+  lim_all = __reduce_min_sync(0xffffffffu, lim_all);
 
   float o[MT][D / 8][4], mx[MT][2], l[MT][2];
 #pragma unroll
@@ -197,6 +243,7 @@ __global__ void __launch_bounds__(kThreads) chunk_mma_kernel(const __grid_consta
     mx[m][0] = mx[m][1] = kNegInf;
     l[m][0] = l[m][1] = 0.f;
   }
+  int ref = 0;  // 8 bits: O is in units of 2^(ref - 127), the largest V scale so far (0: none)
 
 #pragma unroll 1
   for (int i = 0; i < mine; ++i) {
@@ -221,21 +268,14 @@ __global__ void __launch_bounds__(kThreads) chunk_mma_kernel(const __grid_consta
 #pragma unroll
         for (int u = 0; u < 4; ++u) s[m][b][u] = 0.f;
     if (FP8) {
-      uint32_t mult[2];
-#pragma unroll
-      for (int b = 0; b < 2; ++b) {
-        const int key = 8 * b + g;
-        const uint32_t x = (there >> key) & 1u ? scale_mult(lds8(st + R::kScale + key)) : 0u;
-        mult[b] = x | (x << 16);
-      }
 #pragma unroll
       for (int j = 0; j < D / 16; ++j)
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
           const uint32_t w = lds32(st + (8 * b + g) * R::kPitch + 16 * j + 4 * t4);
-          const uint32_t b0 = e4m3_pair(w << 8, mult[b]), b1 = e4m3_pair(w, mult[b]);
+          const uint32_t b0 = f16_of_e4m3(w), b1 = f16_of_e4m3_hi(w);
 #pragma unroll
-          for (int m = 0; m < MT; ++m) mma(s[m][b], qf[m][j], b0, b1);
+          for (int m = 0; m < MT; ++m) mma_f16(s[m][b], qf[m][j], b0, b1);
         }
     } else {
 #pragma unroll
@@ -251,93 +291,150 @@ __global__ void __launch_bounds__(kThreads) chunk_mma_kernel(const __grid_consta
       }
     }
 
+    // a block that every row sees in full needs no mask
+    const bool full = there == 0xffffu && k0 + kBlk <= lim_all;
+    float kf4[2][2], vf4[2][2];  // 8 bits: the scales of the thread's four keys
+    bool far = false;            // V scales too far apart for f16
+    if (FP8) {
+      const uint32_t mine = lds8(st + R::kScale + 16 + (lane & 15));
+      const bool counts = ((there >> (lane & 15)) & 1u) && mine != 0u && mine != 255u;
+      const int hi = (int)__reduce_max_sync(0xffffffffu, counts ? mine : 0u);
+      const int lo = (int)__reduce_min_sync(0xffffffffu, counts ? mine : 255u);
+      if (hi > ref) {
+        const float down = ref == 0 ? 0.f : __uint_as_float((uint32_t)(max(127 + ref - hi, 0)) << 23);
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+          for (int c = 0; c < D / 8; ++c)
+#pragma unroll
+            for (int u = 0; u < 4; ++u) o[m][c][u] = ref == 0 ? 0.f : o[m][c][u] * down;
+        ref = hi;
+      }
+      far = lo < ref - 12;
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int v = 0; v < 2; ++v) {
+          const int key = 8 * b + 2 * t4 + v;
+          kf4[b][v] = scale_value(lds8(st + R::kScale + key));
+          const int byte = (int)lds8(st + R::kScale + 16 + key);
+          // 2^(k - r + 15); what is not there, or does not count above, is masked or 0
+          vf4[b][v] = far ? 32768.f : byte == 255 ? __uint_as_float(0x7fc00000u) : byte == 0 ? 0.f
+                          : __uint_as_float((uint32_t)min(max(142 + min(max(byte, 7), 134) - ref, 1), 254) << 23);
+        }
+    }
+
     uint32_t pf[MT][4];
     bool hidden = false;  // some row here does not see some key of the block
 #pragma unroll
     for (int m = 0; m < MT; ++m)
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
-        const int n = lim[m][u] - k0;  // keys of the block that the row sees, if they are there
-        uint32_t see = n >= kBlk ? 0xffffu : n <= 0 ? 0u : (1u << n) - 1u;
-        hidden |= see != 0xffffu && 16 * m + 8 * u + g < n_rows;
-        see &= there;
+        uint32_t see = 0xffffu;
+        if (!full) {
+          const int n = lim[m][u] - k0;  // keys of the block that the row sees, if they are there
+          see = n >= kBlk ? 0xffffu : n <= 0 ? 0u : (1u << n) - 1u;
+          hidden |= see != 0xffffu && 16 * m + 8 * u + g < n_rows;
+          see &= there;
+        }
         float top = kNegInf;
 #pragma unroll
         for (int b = 0; b < 2; ++b)
 #pragma unroll
           for (int v = 0; v < 2; ++v) {
             float& x = s[m][b][2 * u + v];
-            x = (see >> (8 * b + 2 * t4 + v)) & 1u ? x * p.scale_log2 : kNegInf;
+            x *= FP8 ? qs[m][u] * kf4[b][v] : qs[m][u];
+            if (!full && !((see >> (8 * b + 2 * t4 + v)) & 1u)) x = kNegInf;
             top = fmaxf(top, x);
           }
         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
         const float m_new = fmaxf(mx[m][u], top), base = m_new == kNegInf ? 0.f : m_new;
-        const float alpha = ex2(mx[m][u] - base);
-        mx[m][u] = m_new;
+        // (the maximum of few blocks is above all before them)
+        if (__any_sync(0xffffffffu, m_new > mx[m][u])) {
+          const float alpha = ex2(mx[m][u] - base);
+          l[m][u] *= alpha;
+#pragma unroll
+          for (int c = 0; c < D / 8; ++c) {
+            o[m][c][2 * u] *= alpha;
+            o[m][c][2 * u + 1] *= alpha;
+          }
+          mx[m][u] = m_new;
+        }
         float sum = 0.f;
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
-          const float a = ex2(s[m][b][2 * u] - base), c = ex2(s[m][b][2 * u + 1] - base);
+          float a = ex2(s[m][b][2 * u] - base), c = ex2(s[m][b][2 * u + 1] - base);
           sum += a + c;
-          pf[m][2 * b + u] = pack_bf16(a, c);
+          if (FP8) {
+            // (a NaN scale reaches the rows that see its key alone)
+            a *= full || ((see >> (8 * b + 2 * t4)) & 1u) ? vf4[b][0] : 0.f;
+            c *= full || ((see >> (8 * b + 2 * t4 + 1)) & 1u) ? vf4[b][1] : 0.f;
+            pf[m][2 * b + u] = far ? pack_bf16(a, c) : pack_f16(a, c);
+          } else {
+            pf[m][2 * b + u] = pack_bf16(a, c);
+          }
         }
-        l[m][u] = l[m][u] * alpha + sum;
-#pragma unroll
-        for (int c = 0; c < D / 8; ++c) {
-          o[m][c][2 * u] *= alpha;
-          o[m][c][2 * u + 1] *= alpha;
-        }
+        l[m][u] += sum;
       }
 
     // P.V.  A weight of 0 times a NaN or an infinity is not 0: where a row does not see all of the block
-    // and its values are not all finite, the products are formed one by one instead.
-    const bool any_hidden = __any_sync(0xffffffffu, hidden);
+    // and its values are not all finite, the products are formed one by one instead.  (8-bit codes are
+    // finite; a group's NaN is in its scale.)
+    const bool any_hidden = !full && __any_sync(0xffffffffu, hidden);
     if (FP8) {
-      uint32_t mult[2];
-      bool bad = false;
+      if (!far) {
 #pragma unroll
-      for (int b = 0; b < 2; ++b) {
-        const int key = 8 * b + 2 * t4;
-        const uint32_t x = (there >> key) & 1u ? scale_mult(lds8(st + R::kScale + 16 + key)) : 0u;
-        const uint32_t y = (there >> (key + 1)) & 1u ? scale_mult(lds8(st + R::kScale + 17 + key)) : 0u;
-        mult[b] = x | (y << 16);
-        bad |= not_finite2(mult[b]);
-      }
-      if (!(any_hidden && __any_sync(0xffffffffu, bad))) {
+        for (int q = 0; q < D / 32; ++q) {
+          const uint32_t a = sv + 2 * t4 * R::kPitch + 32 * q + 4 * g;
+          const uint32_t w0 = lds32(a), w1 = lds32(a + R::kPitch), w2 = lds32(a + 8 * R::kPitch), w3 = lds32(a + 9 * R::kPitch);
+          // column 32 q + 4 g + r of two keys each: column g of O tile 4 q + r
+          const uint32_t x01 = __byte_perm(w0, w1, 0x5140), x23 = __byte_perm(w0, w1, 0x7362);
+          const uint32_t y01 = __byte_perm(w2, w3, 0x5140), y23 = __byte_perm(w2, w3, 0x7362);
+          const uint32_t b0[4] = {f16_of_e4m3(x01), f16_of_e4m3_hi(x01), f16_of_e4m3(x23), f16_of_e4m3_hi(x23)};
+          const uint32_t b1[4] = {f16_of_e4m3(y01), f16_of_e4m3_hi(y01), f16_of_e4m3(y23), f16_of_e4m3_hi(y23)};
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int m = 0; m < MT; ++m) mma_f16(o[m][4 * q + r], pf[m], b0[r], b1[r]);
+        }
+      } else {
+        // V as code 2^(k - r) in bf16, the weights as they are (a NaN group by its scale, one by one)
+        const uint32_t nan_keys = __ballot_sync(0xffffffffu, lane < kBlk && ((there >> lane) & 1u) && lds8(st + R::kScale + 16 + (lane & 15)) == 255u);
+        uint32_t mult[2];
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+          uint32_t two[2];
+#pragma unroll
+          for (int v = 0; v < 2; ++v) {
+            const int key = 8 * b + 2 * t4 + v;
+            const int byte = (there >> key) & 1u ? (int)lds8(st + R::kScale + 16 + key) : 0;
+            // 2^(120 + k - r): what lies 2^120 below r's is nothing beside it even in fp32
+            const int ex = 120 + byte - ref + 127;
+            two[v] = byte == 0 || byte == 255 || ex < 1 ? 0u : (uint32_t)ex << 7;
+          }
+          mult[b] = two[0] | (two[1] << 16);
+        }
 #pragma unroll
         for (int q = 0; q < D / 32; ++q) {
           const uint32_t a = sv + 2 * t4 * R::kPitch + 32 * q + 4 * g;
           const uint32_t w0 = lds32(a), w1 = lds32(a + R::kPitch), w2 = lds32(a + 8 * R::kPitch), w3 = lds32(a + 9 * R::kPitch);
 #pragma unroll
-          for (int r = 0; r < 4; ++r) {  // column 32 q + 4 g + r: column g of O tile 4 q + r
+          for (int r = 0; r < 4; ++r) {
             const uint32_t sel = (uint32_t)(r << 4) | ((uint32_t)(4 + r) << 12);  // (the low bytes are masked out)
             const uint32_t b0 = e4m3_pair(__byte_perm(w0, w1, sel), mult[0]), b1 = e4m3_pair(__byte_perm(w2, w3, sel), mult[1]);
 #pragma unroll
             for (int m = 0; m < MT; ++m) mma(o[m][4 * q + r], pf[m], b0, b1);
           }
         }
-      } else {
-        // (only whole groups are NaN: every column of such a key)
-#pragma unroll 1
-        for (int key = 0; key < kBlk; ++key) {
-          const uint32_t x = (there >> key) & 1u ? scale_mult(lds8(st + R::kScale + 16 + key)) : 0u;
-          const int src = 4 * g + ((key & 7) >> 1);
+        if (nan_keys) {
 #pragma unroll
           for (int m = 0; m < MT; ++m)
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
-              const uint32_t w = __shfl_sync(0xffffffffu, key < 8 ? pf[m][u] : pf[m][2 + u], src);
-              const float pw = __uint_as_float(key & 1 ? w & 0xffff0000u : w << 16);
-              if (k0 + key >= lim[m][u] || !((there >> key) & 1u)) continue;
-#pragma unroll
-              for (int c = 0; c < D / 8; ++c)
-#pragma unroll
-                for (int v = 0; v < 2; ++v) {
-                  // accumulator column 2 t + v of tile c: column 32 (c / 4) + 4 (2 t + v) + c % 4
-                  const uint32_t code = lds8(sv + key * R::kPitch + 32 * (c / 4) + 4 * (2 * t4 + v) + c % 4);
-                  o[m][c][2 * u + v] = fmaf(pw, __uint_as_float(e4m3_pair(code << 8, x) << 16), o[m][c][2 * u + v]);
-                }
+              const int n = lim[m][u] - k0;
+              const uint32_t see = n >= kBlk ? 0xffffu : n <= 0 ? 0u : (1u << n) - 1u;
+              if (see & nan_keys) l[m][u] = __uint_as_float(0x7fc00000u);
             }
         }
       }
@@ -400,6 +497,8 @@ __global__ void __launch_bounds__(kThreads) chunk_mma_kernel(const __grid_consta
       l[m][u] += __shfl_xor_sync(0xffffffffu, l[m][u], 1);
       l[m][u] += __shfl_xor_sync(0xffffffffu, l[m][u], 2);
     }
+  // (2^(ref - 127 - 15) in two factors: the whole may lie below fp32's normal numbers)
+  const float unit_lo = __uint_as_float((uint32_t)(127 - 15) << 23), unit_hi = __uint_as_float((uint32_t)(ref == 0 ? 127 : ref) << 23);
   __syncthreads();
   float* so = reinterpret_cast<float*>(smem);
   float2* sml = reinterpret_cast<float2*>(so + kWarps * kRows * D);
@@ -414,7 +513,7 @@ __global__ void __launch_bounds__(kThreads) chunk_mma_kernel(const __grid_consta
 #pragma unroll
         for (int v = 0; v < 2; ++v) {
           const int n = 2 * t4 + v, col = FP8 ? 32 * (c / 4) + 4 * n + c % 4 : 8 * c + n;
-          dst[col ^ (4 * (r & 7))] = o[m][c][2 * u + v];  // (rows 8 apart in a warp's store: other banks)
+          dst[col ^ (4 * (r & 7))] = FP8 ? (o[m][c][2 * u + v] * unit_lo) * unit_hi : o[m][c][2 * u + v];  // (rows 8 apart in a warp's store: other banks)
         }
       if (t4 == 0) sml[warp * kRows + r] = make_float2(mx[m][u], l[m][u]);
     }
@@ -460,14 +559,17 @@ __global__ void __launch_bounds__(kThreads) chunk_mma_kernel(const __grid_consta
   }
 }
 
-// The split key ranges of one (token, query head) joined, a warp each: weights 2^(m_s - max m), O and l
-// added up in the order of the splits.
-template <int D>
-__global__ void __launch_bounds__(256) chunk_merge_kernel(const __grid_constant__ ChunkParams p,
+// The split key ranges of one (token, query head) joined: weights 2^(m_s - max m), O and l added up in a fixed
+// order.  WARPS warps share a row's splits (every WARPS-th each, eight under way at a time), and
+// their sums are added through shared memory.
+template <int D, int WARPS>
+__global__ void __launch_bounds__(128) chunk_merge_kernel(const __grid_constant__ ChunkParams p,
                                                           const ChunkMerge* __restrict__ work) {
+  constexpr int V = D / 32, ROWS = 4 / WARPS;  // columns of a lane, rows of a CTA
+  __shared__ float red[4][D + 1];
   const ChunkMerge w = work[blockIdx.x];
-  const int head = blockIdx.y * 8 + (threadIdx.x >> 5), lane = threadIdx.x & 31;
-  if (head >= p.h_q) return;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, part = warp % WARPS;
+  const int head = min((int)blockIdx.y * ROWS + warp / WARPS, p.h_q - 1);  // (a row too many is done twice)
   const int n = w.pre_n + w.page_n;
   auto row_of = [&](int s) {
     return (s < w.pre_n ? w.pre_row + s * w.pre_stride : w.page_row + (s - w.pre_n) * w.page_stride) + head;
@@ -476,40 +578,53 @@ __global__ void __launch_bounds__(256) chunk_merge_kernel(const __grid_constant_
   for (int s = lane; s < n; s += 32) m_all = fmaxf(m_all, p.part_ml[row_of(s)].x);
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) m_all = fmaxf(m_all, __shfl_xor_sync(0xffffffffu, m_all, o));
-  constexpr int V = D / 32;  // columns of a lane
   float acc[V], l = 0.f;
 #pragma unroll
   for (int v = 0; v < V; ++v) acc[v] = 0.f;
-  for (int s0 = 0; s0 < n; s0 += 32) {
-    float wt = 0.f;
-    int64_t row = 0;
-    if (s0 + lane < n) {
-      row = row_of(s0 + lane);
-      const float2 ml = p.part_ml[row];
-      wt = ml.y == 0.f ? 0.f : ex2(ml.x - m_all);  // (l = 0: nothing was visible there; a NaN passes)
-      l += wt * ml.y;
-    }
-    const int k = min(32, n - s0);
-#pragma unroll 4
-    for (int s = 0; s < k; ++s) {
-      const float ws = __shfl_sync(0xffffffffu, wt, s);
-      const float* src = p.part_o + __shfl_sync(0xffffffffu, row, s) * D + V * lane;
-      if (ws == 0.f) continue;  // (its O, then, may not have been written)
-      if constexpr (V == 4) {
-        const float4 x = *reinterpret_cast<const float4*>(src);
-        acc[0] += ws * x.x;
-        acc[1] += ws * x.y;
-        acc[2] += ws * x.z;
-        acc[3] += ws * x.w;
-      } else {
-        const float2 x = *reinterpret_cast<const float2*>(src);
-        acc[0] += ws * x.x;
-        acc[1] += ws * x.y;
+  constexpr int U = 8;
+  for (int s0 = part; s0 < n; s0 += U * WARPS) {
+    float x[U][V], ws[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int s = s0 + u * WARPS;
+      ws[u] = 0.f;
+#pragma unroll
+      for (int v = 0; v < V; ++v) x[u][v] = 0.f;
+      if (s < n) {
+        const int64_t row = row_of(s);
+        const float2 ml = p.part_ml[row];
+        const float* src = p.part_o + row * D + V * lane;
+        if constexpr (V == 4) {
+          const float4 t = *reinterpret_cast<const float4*>(src);
+          x[u][0] = t.x, x[u][1] = t.y, x[u][2] = t.z, x[u][3] = t.w;
+        } else {
+          const float2 t = *reinterpret_cast<const float2*>(src);
+          x[u][0] = t.x, x[u][1] = t.y;
+        }
+        if (ml.y != 0.f) {  // (l = 0: nothing was visible there, and its O may not have been written; a NaN passes)
+          ws[u] = ex2(ml.x - m_all);
+          l += ws[u] * ml.y;
+        }
       }
     }
-  }
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int v = 0; v < V; ++v)
+        if (ws[u] != 0.f) acc[v] += ws[u] * x[u][v];
+  }
+  if constexpr (WARPS > 1) {
+#pragma unroll
+    for (int v = 0; v < V; ++v) red[warp][V * lane + v] = acc[v];
+    if (lane == 0) red[warp][D] = l;
+    __syncthreads();
+    if (part != 0) return;
+    for (int k = 1; k < WARPS; ++k) {
+#pragma unroll
+      for (int v = 0; v < V; ++v) acc[v] += red[warp + k][V * lane + v];
+      l += red[warp + k][D];
+    }
+  }
   const float inv = l == 0.f ? 0.f : 1.f / l;
   const int64_t row = (int64_t)w.tok * p.h_q + head;
   if (p.out_bf16) {
@@ -556,10 +671,17 @@ cudaError_t launch_chunk_mma(const ChunkParams& p, int head_dim, bool fp8, int r
   return fp8 ? launch<64, true, 2>(p, items, n_items, s) : launch<64, false, 2>(p, items, n_items, s);
 }
 
-cudaError_t launch_chunk_merge(const ChunkParams& p, int head_dim, const ChunkMerge* work, int n_work, cudaStream_t s) {
-  const dim3 grid(n_work, (p.h_q + 7) / 8);
-  if (head_dim == 128) chunk_merge_kernel<128><<<grid, 256, 0, s>>>(p, work);
-  else chunk_merge_kernel<64><<<grid, 256, 0, s>>>(p, work);
+cudaError_t launch_chunk_merge(const ChunkParams& p, int head_dim, int most, const ChunkMerge* work, int n_work, cudaStream_t s) {
+  // four warps to a row where it has more splits than one of them keeps under way
+  const bool many = most > 8;
+  const dim3 grid(n_work, many ? p.h_q : (p.h_q + 3) / 4);
+  if (head_dim == 128) {
+    if (many) chunk_merge_kernel<128, 4><<<grid, 128, 0, s>>>(p, work);
+    else chunk_merge_kernel<128, 1><<<grid, 128, 0, s>>>(p, work);
+  } else {
+    if (many) chunk_merge_kernel<64, 4><<<grid, 128, 0, s>>>(p, work);
+    else chunk_merge_kernel<64, 1><<<grid, 128, 0, s>>>(p, work);
+  }
   return cudaGetLastError();
 }
 

@@ -195,6 +195,29 @@ def test_large_scores_and_a_key_that_dominates(fp8, flags):
         assert np.all(np.abs(lse[at:at + n] - l) <= 1e-3)
 
 
+@pytest.mark.parametrize("flags", [0, B.FLAG_PREFIX_MMA, B.FLAG_PREFIX_TC])
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("d", [64, 128])
+def test_values_of_very_different_size(d, fp8, flags):
+    """V whose tokens differ by 2^40 in size, the large ones hardly attended to, Q and K whose channels differ by
+    2^20: what is small is as exact as what is large."""
+    c = Case(14, [200, 15], [2, 3], None, None, 8, 2, d, 16, fp8)
+    wide = torch.where(torch.arange(d) % 8 == 0, 2.0 ** 10, 2.0 ** -10)
+    c.q = (c.q.float() * wide * 2.0 ** -3).bfloat16()
+    for e in range(2):
+        n = c.k[e].shape[0]
+        big = torch.arange(n) % 3 == 1
+        c.k[e] = (c.k[e].float() / wide).bfloat16()
+        c.v[e] = (c.v[e].float() * torch.where(big, 2.0 ** 12, 2.0 ** -28)[:, None, None]).bfloat16()
+    # channel 0 of every query is large and positive, and pushes the large tokens' scores 80 and more below
+    c.q[:, :, 0] = 2.0 ** 10
+    for e in range(2):
+        big = torch.arange(c.k[e].shape[0]) % 3 == 1
+        c.k[e][:, :, 0] = torch.where(big, -1.0, 0.0)[:, None].bfloat16()
+    c.store().device()
+    c.check(*c.attend(c.plan(flags=flags)))
+
+
 @pytest.mark.parametrize("fp8", [False, True])
 @pytest.mark.parametrize("flags", [0, B.FLAG_PREFIX_MMA, B.FLAG_PREFIX_TC])
 @pytest.mark.parametrize("what", [float("nan"), float("inf"), float("-inf")])
