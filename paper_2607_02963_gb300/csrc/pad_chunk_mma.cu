@@ -134,8 +134,11 @@ __global__ void __launch_bounds__(kThreads) chunk_mma_kernel(const __grid_consta
   const int n_blocks = it.key1 > it.key0 ? (it.key1 - it.key0 + kBlk - 1) / kBlk : 0;
   const int mine = n_blocks > warp ? (n_blocks - warp + kWarps - 1) / kWarps : 0;
   const int32_t* table = p.page_table + (it.paged ? it.src * p.max_pages : 0);
-  const uint8_t* kb = static_cast<const uint8_t*>(it.paged ? p.k_pool : p.k_prefix);
-  const uint8_t* vb = static_cast<const uint8_t*>(it.paged ? p.v_pool : p.v_prefix);
+  const uint32_t mul = (uint32_t)(p.h_kv * R::kRow * (it.paged ? p.page_size : 1));
+  const uint32_t in_page = it.paged ? (uint32_t)(p.page_size - 1) : 0u;
+  const int64_t base = (it.paged ? (int64_t)h * p.page_size : it.src * p.h_kv + h) * R::kRow + 16 * (lane % (R::kRow / 16));
+  const uint8_t* kb = static_cast<const uint8_t*>(it.paged ? p.k_pool : p.k_prefix) + base;
+  const uint8_t* vb = static_cast<const uint8_t*>(it.paged ? p.v_pool : p.v_prefix) + base;
 
   // page of this lane's key (lanes 0-15, one key each) of the warp's i-th block
   auto page_of = [&](int i) -> int {
@@ -152,22 +155,24 @@ __global__ void __launch_bounds__(kThreads) chunk_mma_kernel(const __grid_consta
       pad_set_error(p.header, p.gen, PAD_ERR_DEVICE_BOUNDS, (int)it.src, key >> p.page_shift, page);
     }
     const uint32_t there = __ballot_sync(0xffffffffu, ok) & 0xffffu;
-    // first slot (token and head) of the lane's key
-    const int64_t slot = !ok ? 0 : it.paged ? ((int64_t)page * p.h_kv + h) * p.page_size + (key & (p.page_size - 1))
-                                            : (it.src + key) * p.h_kv + h;
-    constexpr int CH = R::kRow / 16, kIter = kBlk * CH / 32;
+    // a key lies index x mul (+ its slot within the page) from the base: its page, or of a prefix its token
+    const uint32_t index = !ok ? 0u : (uint32_t)(it.paged ? page : key);
+    constexpr int CH = R::kRow / 16, kIter = kBlk * CH / 32, RPI = 32 / CH;
+    const int r0 = lane / CH, c = lane % CH;
 #pragma unroll
     for (int j = 0; j < kIter; ++j) {
-      const int row = (j * 32 + lane) / CH, c = (j * 32 + lane) % CH;
-      const int64_t off = __shfl_sync(0xffffffffu, slot, row) * R::kRow + 16 * c;
-      const uint32_t n = (there >> row) & 1u ? 16u : 0u;
+      const int row = j * RPI + r0;
+      const uint32_t on = (there >> row) & 1u;
+      const uint64_t off = (uint64_t)__shfl_sync(0xffffffffu, index, row) * mul + (on ? ((uint32_t)(k0 + row) & in_page) * R::kRow : 0u);
       const uint32_t dst = st + row * R::kPitch + 16 * (FP8 ? c : c ^ (row & 7));
-      cp16(dst, kb + off, n);
-      cp16(dst + kBlk * R::kPitch, vb + off, n);
+      cp16(dst, kb + off, on * 16u);
+      cp16(dst + kBlk * R::kPitch, vb + off, on * 16u);
     }
     if (FP8) {  // four keys' scale bytes each (they share a page)
-      const int64_t s4 = __shfl_sync(0xffffffffu, slot, 4 * (lane & 3));
-      if (lane < 8) cp4(st + R::kScale + 4 * lane, (lane < 4 ? p.k_scale : p.v_scale) + (s4 & ~(int64_t)3), (there >> (4 * (lane & 3))) & 1u ? 4u : 0u);
+      const uint32_t four = 4 * (lane & 3), on = (there >> four) & 1u;
+      const uint64_t at = (uint64_t)__shfl_sync(0xffffffffu, index, four) * (uint32_t)(p.h_kv * p.page_size) +
+                          (on ? (uint32_t)(h * p.page_size) + ((uint32_t)(k0 + four) & in_page) : 0u);
+      if (lane < 8) cp4(st + R::kScale + 4 * lane, (lane < 4 ? p.k_scale : p.v_scale) + at, on * 4u);
     }
     if (lane == 0) *reinterpret_cast<uint32_t*>(smem + (st - smem_u32(smem)) + R::kMask) = there;
   };
@@ -502,19 +507,31 @@ __global__ void __launch_bounds__(kThreads) chunk_mma_kernel(const __grid_consta
   __syncthreads();
   float* so = reinterpret_cast<float*>(smem);
   float2* sml = reinterpret_cast<float2*>(so + kWarps * kRows * D);
+  auto swap = [](int r) { return FP8 ? 4 * (r & 7) : 8 * (r & 3); };
 #pragma unroll
   for (int m = 0; m < MT; ++m)
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       const int r = 16 * m + 8 * u + g;
       float* dst = so + (warp * kRows + r) * D;
+      // (a store's lanes touch distinct banks: the rows' columns are exchanged by groups of four or eight)
+      if (FP8) {
 #pragma unroll
-      for (int c = 0; c < D / 8; ++c)
+        for (int q = 0; q < D / 32; ++q)
 #pragma unroll
-        for (int v = 0; v < 2; ++v) {
-          const int n = 2 * t4 + v, col = FP8 ? 32 * (c / 4) + 4 * n + c % 4 : 8 * c + n;
-          dst[col ^ (4 * (r & 7))] = FP8 ? (o[m][c][2 * u + v] * unit_lo) * unit_hi : o[m][c][2 * u + v];  // (rows 8 apart in a warp's store: other banks)
-        }
+          for (int v = 0; v < 2; ++v) {
+            float4 x;
+            x.x = (o[m][4 * q][2 * u + v] * unit_lo) * unit_hi;
+            x.y = (o[m][4 * q + 1][2 * u + v] * unit_lo) * unit_hi;
+            x.z = (o[m][4 * q + 2][2 * u + v] * unit_lo) * unit_hi;
+            x.w = (o[m][4 * q + 3][2 * u + v] * unit_lo) * unit_hi;
+            *reinterpret_cast<float4*>(dst + ((32 * q + 4 * (2 * t4 + v)) ^ swap(r))) = x;
+          }
+      } else {
+#pragma unroll
+        for (int c = 0; c < D / 8; ++c)
+          *reinterpret_cast<float2*>(dst + ((8 * c + 2 * t4) ^ swap(r))) = make_float2(o[m][c][2 * u], o[m][c][2 * u + 1]);
+      }
       if (t4 == 0) sml[warp * kRows + r] = make_float2(mx[m][u], l[m][u]);
     }
   __syncthreads();
@@ -534,7 +551,7 @@ __global__ void __launch_bounds__(kThreads) chunk_mma_kernel(const __grid_consta
 #pragma unroll
     for (int k = 0; k < kWarps; ++k) {
       if (sml[k * kRows + r].y == 0.f) continue;
-      const float4 x = *reinterpret_cast<const float4*>(so + (k * kRows + r) * D + ((4 * c) ^ (4 * (r & 7))));
+      const float4 x = *reinterpret_cast<const float4*>(so + (k * kRows + r) * D + ((4 * c) ^ swap(r)));
       a.x += w[k] * x.x;
       a.y += w[k] * x.y;
       a.z += w[k] * x.z;
