@@ -14,8 +14,8 @@
 // (which Q's fragments follow: the order of a sum's terms is free), a V word four columns of a key, so
 // that words of two keys give the pairs P.V wants without a transpose.  Range: Q rows are scaled by a
 // power of two to below 2^15 (exact down to 2^-29 of their largest value), weights go in as p 2^(k - r + 15)
-// with r the largest V scale so far, which is exact to eleven bits down to 2^-29 of r's; a block whose scales
-// lie further apart than 2^12 takes V widened to bf16 instead, whose range is that of fp32.
+// with r the largest V scale so far; where a block's scales lie more than 2^12 below that, they go in as
+// bf16, whose range is fp32's, and so do the codes.
 // (Widened to bf16 throughout, four to five integer instructions a pair: 129 us for 295k cached tokens, 28/4 heads,
 // no faster than the bf16 cache.)
 //
@@ -38,24 +38,28 @@ using tc::smem_u32;
 
 constexpr int kWarps = 4;
 constexpr int kThreads = 32 * kWarps;
-constexpr int kBlk = 16;  // keys of a block
 constexpr float kNegInf = -__builtin_huge_valf();
 constexpr float kLn2 = 0.69314718055994531f;
 
-template <int D, bool FP8>
+// A warp's stages.  NB: 16-key groups of a block; two where the registers allow it (8 bits, 16 rows): the
+// look-ups, the maximum and the waits are per block.
+template <int D, bool FP8, int MT>
 struct Ring {
+  static constexpr int NB = FP8 && MT == 1 ? 2 : 1;
+  static constexpr int kBlk = 16 * NB;                    // keys of a block
   static constexpr int kRow = FP8 ? D : 2 * D;            // bytes of a key
   static constexpr int kPitch = FP8 ? D + 16 : 2 * D;     // (8 bits: rows 4 banks apart; bf16: swizzled)
-  static constexpr int kScale = 2 * kBlk * kPitch;        // scale bytes: 16 of K, 16 of V
-  static constexpr int kMask = kScale + 32;               // which keys are there
-  static constexpr int kStage = kScale + 48;
-  static constexpr int kStages = FP8 ? 4 : 3;
+  static constexpr int kV = kBlk * kPitch;
+  static constexpr int kScale = 2 * kBlk * kPitch;        // scale bytes: of K, then of V
+  static constexpr int kMask = kScale + 2 * kBlk;         // which keys are there
+  static constexpr int kStage = kMask + 16;
+  static constexpr int kStages = FP8 && NB == 1 ? 4 : 3;
   static constexpr int kWarpBytes = kStages * kStage;
 };
 
 template <int D, bool FP8, int MT>
 constexpr int smem_bytes() {
-  constexpr int ring = kWarps * Ring<D, FP8>::kWarpBytes;
+  constexpr int ring = kWarps * Ring<D, FP8, MT>::kWarpBytes;
   constexpr int join = kWarps * 16 * MT * (D + 2) * 4;
   return ring > join ? ring : join;
 }
@@ -75,12 +79,12 @@ __device__ __forceinline__ void ldsm4t(uint32_t (&r)[4], uint32_t a) {
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(a) : "memory");
 }
 __device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 __device__ __forceinline__ void mma_f16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
@@ -99,20 +103,9 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
   const __half2 h = __floats2half2_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&h);
 }
-// 2^(byte - 127), 0 for a group of zeros, NaN for one that holds a NaN.
-__device__ __forceinline__ float scale_value(uint32_t byte) {
-  return byte == 255u ? __uint_as_float(0x7fc00000u) : byte == 0u ? 0.f : __uint_as_float(min(max(byte, 7u), 134u) << 23);
-}
-__device__ __forceinline__ uint32_t lds32(uint32_t a) {
-  uint32_t v;
-  asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
-  return v;
-}
-__device__ __forceinline__ uint32_t lds8(uint32_t a) {
-  uint32_t v;
-  asm volatile("ld.shared.u8 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
-  return v;
-}
+// A scale byte as a number: 2^(byte - 127), 0 for a group of zeros, and for one that holds a NaN (whose codes
+// are 0) an infinity, which makes a NaN of them.
+__device__ __forceinline__ float scale_value(uint32_t byte) { return __uint_as_float(byte << 23); }
 __device__ __forceinline__ bool not_finite2(uint32_t v) {  // either half's exponent is all ones
   return (v & 0x7f80u) == 0x7f80u || (v & 0x7f800000u) == 0x7f800000u;
 }
@@ -121,14 +114,15 @@ __device__ __forceinline__ bool not_finite2(uint32_t v) {  // either half's expo
 template <int D, bool FP8, int MT>
 __global__ void __launch_bounds__(kThreads) chunk_mma_kernel(const __grid_constant__ ChunkParams p,
                                                              const ChunkItem* __restrict__ items) {
-  using R = Ring<D, FP8>;
-  constexpr int kRows = 16 * MT;
+  using R = Ring<D, FP8, MT>;
+  constexpr int kRows = 16 * MT, NB = R::NB, kBlk = R::kBlk;
+  constexpr uint32_t kEvery = kBlk == 32 ? 0xffffffffu : 0xffffu;
   extern __shared__ __align__(128) uint8_t smem[];
   const ChunkItem it = items[blockIdx.x / p.h_kv];
   const int h = (int)blockIdx.x % p.h_kv, G = p.group;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t4 = lane & 3;
-  const uint32_t ring = smem_u32(smem) + warp * R::kWarpBytes;
-  const uint8_t* ring_ptr = smem + warp * R::kWarpBytes;
+  uint8_t* ring = smem + warp * R::kWarpBytes;
+  const uint32_t ring_at = smem_u32(ring);
   const int n_rows = it.ntok * G;
 
   const int n_blocks = it.key1 > it.key0 ? (it.key1 - it.key0 + kBlk - 1) / kBlk : 0;
@@ -140,21 +134,21 @@ __global__ void __launch_bounds__(kThreads) chunk_mma_kernel(const __grid_consta
   const uint8_t* kb = static_cast<const uint8_t*>(it.paged ? p.k_pool : p.k_prefix) + base;
   const uint8_t* vb = static_cast<const uint8_t*>(it.paged ? p.v_pool : p.v_prefix) + base;
 
-  // page of this lane's key (lanes 0-15, one key each) of the warp's i-th block
+  // page of this lane's key (one lane each) of the warp's i-th block
   auto page_of = [&](int i) -> int {
     const int key = it.key0 + (warp + kWarps * i) * kBlk + lane;
     return it.paged && i < mine && lane < kBlk && key < it.key1 ? __ldg(table + (key >> p.page_shift)) : 0;
   };
-  auto issue = [&](int i, int page) {
+  auto issue = [&](int i, int page, int stage) {
     if (i >= mine) return;
-    const uint32_t st = ring + (i % R::kStages) * R::kStage;
-    const int k0 = it.key0 + (warp + kWarps * i) * kBlk, key = k0 + (lane & 15);
+    const uint32_t st = ring_at + stage * R::kStage;
+    const int k0 = it.key0 + (warp + kWarps * i) * kBlk, key = k0 + (lane & (kBlk - 1));
     bool ok = key < it.key1;
     if (it.paged && ok && lane < kBlk && (unsigned)page >= (unsigned)p.n_pages) {
       ok = false;
       pad_set_error(p.header, p.gen, PAD_ERR_DEVICE_BOUNDS, (int)it.src, key >> p.page_shift, page);
     }
-    const uint32_t there = __ballot_sync(0xffffffffu, ok) & 0xffffu;
+    const uint32_t there = __ballot_sync(0xffffffffu, ok) & kEvery;
     // a key lies index x mul (+ its slot within the page) from the base: its page, or of a prefix its token
     const uint32_t index = !ok ? 0u : (uint32_t)(it.paged ? page : key);
     constexpr int CH = R::kRow / 16, kIter = kBlk * CH / 32, RPI = 32 / CH;
@@ -166,22 +160,22 @@ __global__ void __launch_bounds__(kThreads) chunk_mma_kernel(const __grid_consta
       const uint64_t off = (uint64_t)__shfl_sync(0xffffffffu, index, row) * mul + (on ? ((uint32_t)(k0 + row) & in_page) * R::kRow : 0u);
       const uint32_t dst = st + row * R::kPitch + 16 * (FP8 ? c : c ^ (row & 7));
       cp16(dst, kb + off, on * 16u);
-      cp16(dst + kBlk * R::kPitch, vb + off, on * 16u);
+      cp16(dst + R::kV, vb + off, on * 16u);
     }
     if (FP8) {  // four keys' scale bytes each (they share a page)
-      const uint32_t four = 4 * (lane & 3), on = (there >> four) & 1u;
+      const uint32_t four = (4 * lane) & (kBlk - 1), on = (there >> four) & 1u;
       const uint64_t at = (uint64_t)__shfl_sync(0xffffffffu, index, four) * (uint32_t)(p.h_kv * p.page_size) +
                           (on ? (uint32_t)(h * p.page_size) + ((uint32_t)(k0 + four) & in_page) : 0u);
-      if (lane < 8) cp4(st + R::kScale + 4 * lane, (lane < 4 ? p.k_scale : p.v_scale) + at, on * 4u);
+      if (lane < kBlk / 2) cp4(st + R::kScale + 4 * lane, (lane < kBlk / 4 ? p.k_scale : p.v_scale) + at, on * 4u);
     }
-    if (lane == 0) *reinterpret_cast<uint32_t*>(smem + (st - smem_u32(smem)) + R::kMask) = there;
+    if (lane == 0) *reinterpret_cast<uint32_t*>(ring + stage * R::kStage + R::kMask) = there;
   };
 
   int page = page_of(0);
 #pragma unroll
   for (int i = 0; i < R::kStages - 1; ++i) {
     const int next = page_of(i + 1);
-    issue(i, page);
+    issue(i, page, i);
     asm volatile("cp.async.commit_group;" ::: "memory");
     page = next;
   }
@@ -248,103 +242,113 @@ __global__ void __launch_bounds__(kThreads) chunk_mma_kernel(const __grid_consta
     mx[m][0] = mx[m][1] = kNegInf;
     l[m][0] = l[m][1] = 0.f;
   }
-  int ref = 0;  // 8 bits: O is in units of 2^(ref - 127), the largest V scale so far (0: none)
+  // 8 bits: the largest V scale so far (a byte, 0: none), and 2^unit, which V scales are multiplied by: O is in
+  // units of 2^-unit
+  int ref = 0, unit = 0;
 
+  int s_use = 0, s_fill = R::kStages - 1;  // the stages of this block and of the one being fetched
 #pragma unroll 1
   for (int i = 0; i < mine; ++i) {
     {
       const int next = page_of(i + R::kStages);
-      issue(i + R::kStages - 1, page);
+      issue(i + R::kStages - 1, page, s_fill);
       asm volatile("cp.async.commit_group;" ::: "memory");
       page = next;
+      s_fill = s_fill == R::kStages - 1 ? 0 : s_fill + 1;
     }
     asm volatile("cp.async.wait_group %0;" ::"n"(R::kStages - 1) : "memory");
     __syncwarp();
-    const uint32_t st = ring + (i % R::kStages) * R::kStage;
-    const uint32_t sv = st + kBlk * R::kPitch;
-    const uint32_t there = *reinterpret_cast<const uint32_t*>(ring_ptr + (i % R::kStages) * R::kStage + R::kMask);
+    const uint8_t* st = ring + s_use * R::kStage;
+    const uint32_t st_at = ring_at + s_use * R::kStage;
+    const uint8_t* sv = st + R::kV;
+    s_use = s_use == R::kStages - 1 ? 0 : s_use + 1;
+    const uint32_t there = *reinterpret_cast<const uint32_t*>(st + R::kMask);
     const int k0 = it.key0 + (warp + kWarps * i) * kBlk;
+    auto word = [](const uint8_t* a) { return *reinterpret_cast<const uint32_t*>(a); };
 
-    float s[MT][2][4];
+    float s[MT][2 * NB][4];
 #pragma unroll
     for (int m = 0; m < MT; ++m)
 #pragma unroll
-      for (int b = 0; b < 2; ++b)
+      for (int b = 0; b < 2 * NB; ++b)
 #pragma unroll
         for (int u = 0; u < 4; ++u) s[m][b][u] = 0.f;
     if (FP8) {
 #pragma unroll
       for (int j = 0; j < D / 16; ++j)
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
-          const uint32_t w = lds32(st + (8 * b + g) * R::kPitch + 16 * j + 4 * t4);
+        for (int b = 0; b < 2 * NB; ++b) {
+          const uint32_t w = word(st + (8 * b + g) * R::kPitch + 16 * j + 4 * t4);
           const uint32_t b0 = f16_of_e4m3(w), b1 = f16_of_e4m3_hi(w);
 #pragma unroll
           for (int m = 0; m < MT; ++m) mma_f16(s[m][b], qf[m][j], b0, b1);
         }
     } else {
 #pragma unroll
-      for (int j = 0; j < D / 16; ++j) {
-        uint32_t kf[4];
-        const int row = (lane & 7) + ((lane >> 4) << 3), c = 2 * j + ((lane >> 3) & 1);
-        ldsm4(kf, st + row * R::kPitch + 16 * (c ^ (row & 7)));
+      for (int j = 0; j < D / 16; ++j)
 #pragma unroll
-        for (int m = 0; m < MT; ++m) {
-          mma(s[m][0], qf[m][j], kf[0], kf[1]);
-          mma(s[m][1], qf[m][j], kf[2], kf[3]);
+        for (int nb = 0; nb < NB; ++nb) {
+          uint32_t kf[4];
+          const int row = 16 * nb + (lane & 7) + ((lane >> 4) << 3), c = 2 * j + ((lane >> 3) & 1);
+          ldsm4(kf, st_at + row * R::kPitch + 16 * (c ^ (row & 7)));
+#pragma unroll
+          for (int m = 0; m < MT; ++m) {
+            mma(s[m][2 * nb], qf[m][j], kf[0], kf[1]);
+            mma(s[m][2 * nb + 1], qf[m][j], kf[2], kf[3]);
+          }
         }
-      }
     }
 
     // a block that every row sees in full needs no mask
-    const bool full = there == 0xffffu && k0 + kBlk <= lim_all;
-    float kf4[2][2], vf4[2][2];  // 8 bits: the scales of the thread's four keys
-    bool far = false;            // V scales too far apart for f16
+    const bool full = there == kEvery && k0 + kBlk <= lim_all;
+    float kf4[2 * NB][2], vf4[2 * NB][2];  // 8 bits: the scales of the thread's keys
+    bool far = false;                      // V scales too far apart for f16
     if (FP8) {
-      const uint32_t mine = lds8(st + R::kScale + 16 + (lane & 15));
-      const bool counts = ((there >> (lane & 15)) & 1u) && mine != 0u && mine != 255u;
-      const int hi = (int)__reduce_max_sync(0xffffffffu, counts ? mine : 0u);
-      const int lo = (int)__reduce_min_sync(0xffffffffu, counts ? mine : 255u);
+      const uint32_t byte = st[R::kScale + kBlk + (lane & (kBlk - 1))];
+      const bool counts = ((there >> (lane & (kBlk - 1))) & 1u) && byte != 0u && byte != 255u;
+      const int hi = (int)__reduce_max_sync(0xffffffffu, counts ? byte : 0u);
+      const int lo = (int)__reduce_min_sync(0xffffffffu, counts ? byte : 255u);
       if (hi > ref) {
-        const float down = ref == 0 ? 0.f : __uint_as_float((uint32_t)(max(127 + ref - hi, 0)) << 23);
+        const int now = min(142 - hi, 127);  // 2^15 for the largest scale (less where that is no fp32 number)
+        const float down = ref == 0 ? 1.f : __uint_as_float((uint32_t)max(127 + now - unit, 0) << 23);
 #pragma unroll
         for (int m = 0; m < MT; ++m)
 #pragma unroll
           for (int c = 0; c < D / 8; ++c)
 #pragma unroll
-            for (int u = 0; u < 4; ++u) o[m][c][u] = ref == 0 ? 0.f : o[m][c][u] * down;
+            for (int u = 0; u < 4; ++u) o[m][c][u] *= down;
         ref = hi;
+        unit = now;
       }
       far = lo < ref - 12;
+      const float up = __uint_as_float((uint32_t)(127 + unit) << 23);
 #pragma unroll
-      for (int b = 0; b < 2; ++b)
-#pragma unroll
-        for (int v = 0; v < 2; ++v) {
-          const int key = 8 * b + 2 * t4 + v;
-          kf4[b][v] = scale_value(lds8(st + R::kScale + key));
-          const int byte = (int)lds8(st + R::kScale + 16 + key);
-          // 2^(k - r + 15); what is not there, or does not count above, is masked or 0
-          vf4[b][v] = far ? 32768.f : byte == 255 ? __uint_as_float(0x7fc00000u) : byte == 0 ? 0.f
-                          : __uint_as_float((uint32_t)min(max(142 + min(max(byte, 7), 134) - ref, 1), 254) << 23);
-        }
+      for (int b = 0; b < 2 * NB; ++b) {
+        const uint32_t k2 = *reinterpret_cast<const uint16_t*>(st + R::kScale + 8 * b + 2 * t4);
+        const uint32_t v2 = *reinterpret_cast<const uint16_t*>(st + R::kScale + kBlk + 8 * b + 2 * t4);
+        kf4[b][0] = scale_value(k2 & 255u);
+        kf4[b][1] = scale_value(k2 >> 8);
+        vf4[b][0] = scale_value(v2 & 255u) * up;
+        vf4[b][1] = scale_value(v2 >> 8) * up;
+      }
     }
 
-    uint32_t pf[MT][4];
+    uint32_t pf[MT][NB][4];
     bool hidden = false;  // some row here does not see some key of the block
 #pragma unroll
     for (int m = 0; m < MT; ++m)
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
-        uint32_t see = 0xffffu;
+        uint32_t see = kEvery;
         if (!full) {
           const int n = lim[m][u] - k0;  // keys of the block that the row sees, if they are there
-          see = n >= kBlk ? 0xffffu : n <= 0 ? 0u : (1u << n) - 1u;
-          hidden |= see != 0xffffu && 16 * m + 8 * u + g < n_rows;
+          see = n >= kBlk ? kEvery : n <= 0 ? 0u : (1u << n) - 1u;
+          hidden |= see != kEvery && 16 * m + 8 * u + g < n_rows;
           see &= there;
         }
         float top = kNegInf;
 #pragma unroll
-        for (int b = 0; b < 2; ++b)
+        for (int b = 0; b < 2 * NB; ++b)
 #pragma unroll
           for (int v = 0; v < 2; ++v) {
             float& x = s[m][b][2 * u + v];
@@ -366,123 +370,99 @@ __global__ void __launch_bounds__(kThreads) chunk_mma_kernel(const __grid_consta
           }
           mx[m][u] = m_new;
         }
-        float sum = 0.f;
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
+        for (int b = 0; b < 2 * NB; ++b) {
           float a = ex2(s[m][b][2 * u] - base), c = ex2(s[m][b][2 * u + 1] - base);
-          sum += a + c;
+          l[m][u] += a + c;
           if (FP8) {
             // (a NaN scale reaches the rows that see its key alone)
             a *= full || ((see >> (8 * b + 2 * t4)) & 1u) ? vf4[b][0] : 0.f;
             c *= full || ((see >> (8 * b + 2 * t4 + 1)) & 1u) ? vf4[b][1] : 0.f;
-            pf[m][2 * b + u] = far ? pack_bf16(a, c) : pack_f16(a, c);
+            pf[m][b >> 1][2 * (b & 1) + u] = far ? pack_bf16(a, c) : pack_f16(a, c);
           } else {
-            pf[m][2 * b + u] = pack_bf16(a, c);
+            pf[m][b >> 1][2 * (b & 1) + u] = pack_bf16(a, c);
           }
         }
-        l[m][u] += sum;
       }
 
     // P.V.  A weight of 0 times a NaN or an infinity is not 0: where a row does not see all of the block
     // and its values are not all finite, the products are formed one by one instead.  (8-bit codes are
-    // finite; a group's NaN is in its scale.)
-    const bool any_hidden = !full && __any_sync(0xffffffffu, hidden);
+    // finite; a group's NaN is in its scale, and so in the weights of the rows that see it.)
     if (FP8) {
-      if (!far) {
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
         for (int q = 0; q < D / 32; ++q) {
-          const uint32_t a = sv + 2 * t4 * R::kPitch + 32 * q + 4 * g;
-          const uint32_t w0 = lds32(a), w1 = lds32(a + R::kPitch), w2 = lds32(a + 8 * R::kPitch), w3 = lds32(a + 9 * R::kPitch);
+          const uint8_t* a = sv + (16 * nb + 2 * t4) * R::kPitch + 32 * q + 4 * g;
+          const uint32_t w0 = word(a), w1 = word(a + R::kPitch), w2 = word(a + 8 * R::kPitch), w3 = word(a + 9 * R::kPitch);
           // column 32 q + 4 g + r of two keys each: column g of O tile 4 q + r
           const uint32_t x01 = __byte_perm(w0, w1, 0x5140), x23 = __byte_perm(w0, w1, 0x7362);
           const uint32_t y01 = __byte_perm(w2, w3, 0x5140), y23 = __byte_perm(w2, w3, 0x7362);
-          const uint32_t b0[4] = {f16_of_e4m3(x01), f16_of_e4m3_hi(x01), f16_of_e4m3(x23), f16_of_e4m3_hi(x23)};
-          const uint32_t b1[4] = {f16_of_e4m3(y01), f16_of_e4m3_hi(y01), f16_of_e4m3(y23), f16_of_e4m3_hi(y23)};
+          if (!far) {
+            const uint32_t b0[4] = {f16_of_e4m3(x01), f16_of_e4m3_hi(x01), f16_of_e4m3(x23), f16_of_e4m3_hi(x23)};
+            const uint32_t b1[4] = {f16_of_e4m3(y01), f16_of_e4m3_hi(y01), f16_of_e4m3(y23), f16_of_e4m3_hi(y23)};
 #pragma unroll
-          for (int r = 0; r < 4; ++r)
+            for (int r = 0; r < 4; ++r)
 #pragma unroll
-            for (int m = 0; m < MT; ++m) mma_f16(o[m][4 * q + r], pf[m], b0[r], b1[r]);
-        }
-      } else {
-        // V as code 2^(k - r) in bf16, the weights as they are (a NaN group by its scale, one by one)
-        const uint32_t nan_keys = __ballot_sync(0xffffffffu, lane < kBlk && ((there >> lane) & 1u) && lds8(st + R::kScale + 16 + (lane & 15)) == 255u);
-        uint32_t mult[2];
+              for (int m = 0; m < MT; ++m) mma_f16(o[m][4 * q + r], pf[m][nb], b0[r], b1[r]);
+          } else {
+            // weights of any size: the codes as bf16
+            const uint32_t one = 0x7b807b80u;  // 2^120 twice
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
-          uint32_t two[2];
+            for (int r = 0; r < 4; ++r) {
+              const uint32_t b0 = e4m3_pair(__byte_perm(r < 2 ? x01 : x23, 0u, r & 1 ? 0x3424u : 0x1404u), one);
+              const uint32_t b1 = e4m3_pair(__byte_perm(r < 2 ? y01 : y23, 0u, r & 1 ? 0x3424u : 0x1404u), one);
 #pragma unroll
-          for (int v = 0; v < 2; ++v) {
-            const int key = 8 * b + 2 * t4 + v;
-            const int byte = (there >> key) & 1u ? (int)lds8(st + R::kScale + 16 + key) : 0;
-            // 2^(120 + k - r): what lies 2^120 below r's is nothing beside it even in fp32
-            const int ex = 120 + byte - ref + 127;
-            two[v] = byte == 0 || byte == 255 || ex < 1 ? 0u : (uint32_t)ex << 7;
-          }
-          mult[b] = two[0] | (two[1] << 16);
-        }
-#pragma unroll
-        for (int q = 0; q < D / 32; ++q) {
-          const uint32_t a = sv + 2 * t4 * R::kPitch + 32 * q + 4 * g;
-          const uint32_t w0 = lds32(a), w1 = lds32(a + R::kPitch), w2 = lds32(a + 8 * R::kPitch), w3 = lds32(a + 9 * R::kPitch);
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            const uint32_t sel = (uint32_t)(r << 4) | ((uint32_t)(4 + r) << 12);  // (the low bytes are masked out)
-            const uint32_t b0 = e4m3_pair(__byte_perm(w0, w1, sel), mult[0]), b1 = e4m3_pair(__byte_perm(w2, w3, sel), mult[1]);
-#pragma unroll
-            for (int m = 0; m < MT; ++m) mma(o[m][4 * q + r], pf[m], b0, b1);
-          }
-        }
-        if (nan_keys) {
-#pragma unroll
-          for (int m = 0; m < MT; ++m)
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-              const int n = lim[m][u] - k0;
-              const uint32_t see = n >= kBlk ? 0xffffu : n <= 0 ? 0u : (1u << n) - 1u;
-              if (see & nan_keys) l[m][u] = __uint_as_float(0x7fc00000u);
+              for (int m = 0; m < MT; ++m) mma(o[m][4 * q + r], pf[m][nb], b0, b1);
             }
+          }
         }
-      }
     } else {
-      auto load_v = [&](uint32_t (&vf)[4], int c) {  // O tiles c and c + 1
-        const int row = (lane & 7) + (((lane >> 3) & 1) << 3), ch = c + (lane >> 4);
-        ldsm4t(vf, sv + row * R::kPitch + 16 * (ch ^ (row & 7)));
+      const bool any_hidden = !full && __any_sync(0xffffffffu, hidden);
+      auto load_v = [&](uint32_t (&vf)[4], int nb, int c) {  // O tiles c and c + 1
+        const int row = 16 * nb + (lane & 7) + (((lane >> 3) & 1) << 3), ch = c + (lane >> 4);
+        ldsm4t(vf, st_at + R::kV + row * R::kPitch + 16 * (ch ^ (row & 7)));
       };
       bool bad = false;
       if (any_hidden) {
 #pragma unroll
-        for (int c = 0; c < D / 8; c += 2) {
-          uint32_t vf[4];
-          load_v(vf, c);
-          bad |= not_finite2(vf[0]) | not_finite2(vf[1]) | not_finite2(vf[2]) | not_finite2(vf[3]);
-        }
+        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+          for (int c = 0; c < D / 8; c += 2) {
+            uint32_t vf[4];
+            load_v(vf, nb, c);
+            bad |= not_finite2(vf[0]) | not_finite2(vf[1]) | not_finite2(vf[2]) | not_finite2(vf[3]);
+          }
         bad = __any_sync(0xffffffffu, bad);
       }
       if (!bad) {
 #pragma unroll
-        for (int c = 0; c < D / 8; c += 2) {
-          uint32_t vf[4];
-          load_v(vf, c);
+        for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-          for (int m = 0; m < MT; ++m) {
-            mma(o[m][c], pf[m], vf[0], vf[1]);
-            mma(o[m][c + 1], pf[m], vf[2], vf[3]);
+          for (int c = 0; c < D / 8; c += 2) {
+            uint32_t vf[4];
+            load_v(vf, nb, c);
+#pragma unroll
+            for (int m = 0; m < MT; ++m) {
+              mma(o[m][c], pf[m][nb], vf[0], vf[1]);
+              mma(o[m][c + 1], pf[m][nb], vf[2], vf[3]);
+            }
           }
-        }
       } else {
+        static_assert(FP8 || NB == 1, "the keys below are those of one group");
 #pragma unroll 1
-        for (int key = 0; key < kBlk; ++key) {
+        for (int key = 0; key < 16; ++key) {
           const int src = 4 * g + ((key & 7) >> 1);
 #pragma unroll
           for (int m = 0; m < MT; ++m)
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
-              const uint32_t w = __shfl_sync(0xffffffffu, key < 8 ? pf[m][u] : pf[m][2 + u], src);
+              const uint32_t w = __shfl_sync(0xffffffffu, key < 8 ? pf[m][0][u] : pf[m][0][2 + u], src);
               const float pw = __uint_as_float(key & 1 ? w & 0xffff0000u : w << 16);
               if (k0 + key >= lim[m][u] || !((there >> key) & 1u)) continue;
 #pragma unroll
               for (int c = 0; c < D / 8; ++c) {
-                const uint32_t v2 = lds32(sv + key * R::kPitch + 16 * (c ^ (key & 7)) + 4 * t4);
+                const uint32_t v2 = word(sv + key * R::kPitch + 16 * (c ^ (key & 7)) + 4 * t4);
                 o[m][c][2 * u] = fmaf(pw, __uint_as_float(v2 << 16), o[m][c][2 * u]);
                 o[m][c][2 * u + 1] = fmaf(pw, __uint_as_float(v2 & 0xffff0000u), o[m][c][2 * u + 1]);
               }
@@ -502,8 +482,8 @@ __global__ void __launch_bounds__(kThreads) chunk_mma_kernel(const __grid_consta
       l[m][u] += __shfl_xor_sync(0xffffffffu, l[m][u], 1);
       l[m][u] += __shfl_xor_sync(0xffffffffu, l[m][u], 2);
     }
-  // (2^(ref - 127 - 15) in two factors: the whole may lie below fp32's normal numbers)
-  const float unit_lo = __uint_as_float((uint32_t)(127 - 15) << 23), unit_hi = __uint_as_float((uint32_t)(ref == 0 ? 127 : ref) << 23);
+  // (2^-unit in two factors: the whole may lie below fp32's normal numbers)
+  const float unit_lo = __uint_as_float((uint32_t)(127 - unit / 2) << 23), unit_hi = __uint_as_float((uint32_t)(127 - (unit - unit / 2)) << 23);
   __syncthreads();
   float* so = reinterpret_cast<float*>(smem);
   float2* sml = reinterpret_cast<float2*>(so + kWarps * kRows * D);
