@@ -505,10 +505,18 @@ class ChunkPlan:
         return out
 
     def _pools(self, k_pool, v_pool, k_scale, v_scale):
-        return (_dev(k_pool, "k_pool", self._pool_shape, self._pool_type),
-                _dev(v_pool, "v_pool", self._pool_shape, self._pool_type),
-                _dev(k_scale, "k_scale", self._scale_shape, self._u8),
-                _dev(v_scale, "v_scale", self._scale_shape, self._u8))
+        ps, pt = self._pool_shape, self._pool_type
+        if (k_pool.shape == ps and v_pool.shape == ps and k_pool.dtype is pt and v_pool.dtype is pt
+                and k_pool.is_contiguous() and v_pool.is_contiguous()):
+            if k_scale is None and v_scale is None:
+                return k_pool.data_ptr(), v_pool.data_ptr(), None, None
+            ss, u8 = self._scale_shape, self._u8
+            if (k_scale is not None and v_scale is not None and k_scale.shape == ss and v_scale.shape == ss
+                    and k_scale.dtype is u8 and v_scale.dtype is u8 and k_scale.is_contiguous()
+                    and v_scale.is_contiguous()):
+                return k_pool.data_ptr(), v_pool.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr()
+        return (_dev(k_pool, "k_pool", ps, pt), _dev(v_pool, "v_pool", ps, pt),
+                _dev(k_scale, "k_scale", self._scale_shape, self._u8), _dev(v_scale, "v_scale", self._scale_shape, self._u8))
 
     def destroy(self):
         if self._h is not None and _lib is not None:

@@ -52,6 +52,7 @@ struct ChunkVerify {
 struct ChunkParams {
   int32_t h_q, h_kv, group, page_size, page_shift, max_pages, n_pages;
   int32_t out_bf16;
+  int32_t beside;   // the warp-level kernel runs beside the tcgen05 kernel of the same call
   float scale_log2;
   uint64_t gen;
   PadDevHeader* header;
@@ -77,8 +78,8 @@ cudaError_t launch_chunk_append(const ChunkParams& p, int head_dim, bool fp8, co
 cudaError_t launch_chunk_read(const ChunkParams& p, int head_dim, bool fp8, const ChunkRead* work, int n_events,
                               int n_spans, void* k_out, void* v_out, cudaStream_t s);
 int chunk_read_tokens();
-// rows16: 16-row groups that the items' rows take, 1 or 2.
-cudaError_t launch_chunk_mma(const ChunkParams& p, int head_dim, bool fp8, int rows16, const ChunkItem* items,
+// rows16: 16-row groups that the items' rows take, 1 or 2.  early: not the call's first kernel.
+cudaError_t launch_chunk_mma(const ChunkParams& p, int head_dim, bool fp8, int rows16, bool early, const ChunkItem* items,
                              int n_items, cudaStream_t s);
 // split: one slot of 128 / group tokens per CTA, its tiles taken in turn by two halves; else two slots.
 // prefix_tokens: tokens of k_prefix up to the last one that an item reads, 0 without prefix items.
@@ -92,6 +93,29 @@ cudaError_t launch_draft_verify(const ChunkParams& p, const ChunkVerify* work, i
                                 int32_t* token, cudaStream_t s);
 
 #ifdef __CUDACC__
+// Programmatic dependent launch, within one call: its first kernel is launched in plain stream order (its work
+// list may still be on its way when it is enqueued, by a copy, which griddepcontrol.wait does not cover); a
+// later one may start early, reads its work list, then waits for the grid ahead, and everything after that
+// wait is as in plain stream order.  What a grid ahead may have written is read past L1's read-only path.
+__device__ __forceinline__ void grid_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void grid_release() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+
+template <class... KArgs, class... Args>
+cudaError_t launch_early(bool early, void (*kernel)(KArgs...), dim3 grid, int threads, size_t smem, cudaStream_t s,
+                         Args... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = s;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = early ? 1 : 0;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, static_cast<KArgs>(args)...);
+}
+
 // Multiplier that turns an e4m3 code whose bits sit where bf16 has its exponent and upper
 // mantissa (so that it reads as value * 2^-120) into code * 2^k, as a bf16 pattern: 2^(120 + k),
 // with k = byte - 127.  Byte 0 stands for a group of zeros, 255 for one that holds a NaN.

@@ -32,7 +32,7 @@ __global__ void __launch_bounds__(kThreads) chunk_append_kernel(const __grid_con
   constexpr int L = D / 8;  // lanes of a group
   const ChunkPages w = work[blockIdx.x];
   int32_t* entry = p.page_table + (int64_t)w.event * p.max_pages + w.column;
-  const int page = w.page >= 0 ? w.page : __ldg(entry);
+  const int page = w.page >= 0 ? w.page : __ldcg(entry);
   const int groups = w.count * p.h_kv * 2, lanes = (groups * L + 31) / 32 * 32, c = threadIdx.x % L;
   constexpr int U = 4;  // groups of a thread under way together
 #pragma unroll 1
@@ -114,7 +114,7 @@ __global__ void __launch_bounds__(kThreads) chunk_read_kernel(const __grid_const
   __syncthreads();
   const int pos = (b - mine.span0) * kReadTokens, count = min(kReadTokens, mine.count - pos);
   if ((int)threadIdx.x < count) {
-    const int col = (pos + (int)threadIdx.x) >> p.page_shift, pg = p.page_table[(int64_t)event * p.max_pages + col];
+    const int col = (pos + (int)threadIdx.x) >> p.page_shift, pg = __ldcg(p.page_table + (int64_t)event * p.max_pages + col);
     pages[threadIdx.x] = pg;
     if ((unsigned)pg >= (unsigned)p.n_pages) pad_set_error(p.header, p.gen, PAD_ERR_DEVICE_BOUNDS, event, col, pg);
   }
@@ -137,12 +137,12 @@ __global__ void __launch_bounds__(kThreads) chunk_read_kernel(const __grid_const
       for (int kv = 0; kv < 2; ++kv) {
         const void* pool = kv ? p.v_pool : p.k_pool;
         if (FP8) {
-          const uint2 v = __ldg(reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(pool) + slot * D) + c);
+          const uint2 v = __ldcg(reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(pool) + slot * D) + c);
           x[u][kv].x = v.x;
           x[u][kv].y = v.y;
-          sc[u][kv] = __ldg((kv ? p.v_scale : p.k_scale) + slot);
+          sc[u][kv] = __ldcg((kv ? p.v_scale : p.k_scale) + slot);
         } else {
-          x[u][kv] = __ldg(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(pool) + slot * D) + c);
+          x[u][kv] = __ldcg(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(pool) + slot * D) + c);
         }
       }
     }
@@ -167,14 +167,13 @@ __global__ void __launch_bounds__(kThreads) chunk_read_kernel(const __grid_const
 template <int D, bool FP8>
 cudaError_t append(const ChunkParams& p, const ChunkPages* work, int n, const void* k_new, const void* v_new,
                    int64_t stride, void* k_pool, void* v_pool, uint8_t* ks, uint8_t* vs, cudaStream_t s) {
-  chunk_append_kernel<D, FP8><<<n, kThreads, 0, s>>>(p, work, static_cast<const __nv_bfloat16*>(k_new),
-                                                     static_cast<const __nv_bfloat16*>(v_new), stride, k_pool, v_pool, ks, vs);
-  return cudaGetLastError();
+  return launch_early(false, chunk_append_kernel<D, FP8>, dim3(n), kThreads, 0, s, p, work, static_cast<const __nv_bfloat16*>(k_new),
+                      static_cast<const __nv_bfloat16*>(v_new), stride, k_pool, v_pool, ks, vs);
 }
 template <int D, bool FP8>
 cudaError_t read(const ChunkParams& p, const ChunkRead* work, int n_events, int n, void* k_out, void* v_out, cudaStream_t s) {
-  chunk_read_kernel<D, FP8><<<n, kThreads, 0, s>>>(p, work, n_events, static_cast<__nv_bfloat16*>(k_out), static_cast<__nv_bfloat16*>(v_out));
-  return cudaGetLastError();
+  return launch_early(false, chunk_read_kernel<D, FP8>, dim3(n), kThreads, 0, s, p, work, n_events, static_cast<__nv_bfloat16*>(k_out),
+                      static_cast<__nv_bfloat16*>(v_out));
 }
 
 }  // namespace

@@ -53,7 +53,9 @@ struct Ring {
   static constexpr int kScale = 2 * kBlk * kPitch;        // scale bytes: of K, then of V
   static constexpr int kMask = kScale + 2 * kBlk;         // which keys are there
   static constexpr int kStage = kMask + 16;
-  static constexpr int kStages = FP8 && NB == 1 ? 4 : 3;
+  // (three CTAs per SM at 16 rows, two at 32: 16 sequences x 1 token over 295k cached tokens, 28/4 heads, take 106 us
+  // in 8 bits with two CTAs of three stages, 91 with three of two; bf16 122 and 119)
+  static constexpr int kStages = MT == 1 ? 2 : FP8 ? 4 : 3;
   static constexpr int kWarpBytes = kStages * kStage;
 };
 
@@ -112,7 +114,7 @@ __device__ __forceinline__ bool not_finite2(uint32_t v) {  // either half's expo
 
 // FP8: of paged items; items of the prefix take the bf16 instance.
 template <int D, bool FP8, int MT>
-__global__ void __launch_bounds__(kThreads) chunk_mma_kernel(const __grid_constant__ ChunkParams p,
+__global__ void __launch_bounds__(kThreads, MT == 1 ? 3 : 2) chunk_mma_kernel(const __grid_constant__ ChunkParams p,
                                                              const ChunkItem* __restrict__ items) {
   using R = Ring<D, FP8, MT>;
   constexpr int kRows = 16 * MT, NB = R::NB, kBlk = R::kBlk;
@@ -124,6 +126,11 @@ __global__ void __launch_bounds__(kThreads) chunk_mma_kernel(const __grid_consta
   uint8_t* ring = smem + warp * R::kWarpBytes;
   const uint32_t ring_at = smem_u32(ring);
   const int n_rows = it.ntok * G;
+
+  // (beside the tcgen05 grid of the same call, which was launched in plain stream order: what the items here read is
+  // complete, and that grid is waited for at the end, so that the join's wait covers both)
+  if (!p.beside) grid_wait();
+  grid_release();
 
   const int n_blocks = it.key1 > it.key0 ? (it.key1 - it.key0 + kBlk - 1) / kBlk : 0;
   const int mine = n_blocks > warp ? (n_blocks - warp + kWarps - 1) / kWarps : 0;
@@ -137,7 +144,7 @@ __global__ void __launch_bounds__(kThreads) chunk_mma_kernel(const __grid_consta
   // page of this lane's key (one lane each) of the warp's i-th block
   auto page_of = [&](int i) -> int {
     const int key = it.key0 + (warp + kWarps * i) * kBlk + lane;
-    return it.paged && i < mine && lane < kBlk && key < it.key1 ? __ldg(table + (key >> p.page_shift)) : 0;
+    return it.paged && i < mine && lane < kBlk && key < it.key1 ? __ldcg(table + (key >> p.page_shift)) : 0;
   };
   auto issue = [&](int i, int page, int stage) {
     if (i >= mine) return;
@@ -196,7 +203,7 @@ __global__ void __launch_bounds__(kThreads) chunk_mma_kernel(const __grid_consta
         uint32_t top = 0u;
 #pragma unroll
         for (int j = 0; j < D / 16; ++j) {
-          x[j] = on ? __ldg(reinterpret_cast<const uint2*>(src + 16 * j + 4 * t4)) : make_uint2(0u, 0u);
+          x[j] = on ? __ldcg(reinterpret_cast<const uint2*>(src + 16 * j + 4 * t4)) : make_uint2(0u, 0u);
           top = max(max(max(top, x[j].x & 0x7fffu), max((x[j].x >> 16) & 0x7fffu, x[j].y & 0x7fffu)), (x[j].y >> 16) & 0x7fffu);
         }
         top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
@@ -215,8 +222,8 @@ __global__ void __launch_bounds__(kThreads) chunk_mma_kernel(const __grid_consta
         qs[m][u] = p.scale_log2;
 #pragma unroll
         for (int j = 0; j < D / 16; ++j) {
-          qf[m][j][u] = on ? __ldg(reinterpret_cast<const uint32_t*>(src + 16 * j + 2 * t4)) : 0u;
-          qf[m][j][2 + u] = on ? __ldg(reinterpret_cast<const uint32_t*>(src + 16 * j + 2 * t4 + 8)) : 0u;
+          qf[m][j][u] = on ? __ldcg(reinterpret_cast<const uint32_t*>(src + 16 * j + 2 * t4)) : 0u;
+          qf[m][j][2 + u] = on ? __ldcg(reinterpret_cast<const uint32_t*>(src + 16 * j + 2 * t4 + 8)) : 0u;
         }
       }
     }
@@ -554,6 +561,7 @@ __global__ void __launch_bounds__(kThreads) chunk_mma_kernel(const __grid_consta
       if (c == 0 && p.lse != nullptr) p.lse[row] = l_all == 0.f ? kNegInf : (m_all + log2f(l_all)) * kLn2;
     }
   }
+  if (p.beside) grid_wait();
 }
 
 // The split key ranges of one (token, query head) joined: weights 2^(m_s - max m), O and l added up in a fixed
@@ -565,6 +573,8 @@ __global__ void __launch_bounds__(128) chunk_merge_kernel(const __grid_constant_
   constexpr int V = D / 32, ROWS = 4 / WARPS;  // columns of a lane, rows of a CTA
   __shared__ float red[4][D + 1];
   const ChunkMerge w = work[blockIdx.x];
+  grid_wait();
+  grid_release();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, part = warp % WARPS;
   const int head = min((int)blockIdx.y * ROWS + warp / WARPS, p.h_q - 1);  // (a row too many is done twice)
   const int n = w.pre_n + w.page_n;
@@ -641,7 +651,7 @@ __global__ void __launch_bounds__(128) chunk_merge_kernel(const __grid_constant_
 }
 
 template <int D, bool FP8, int MT>
-cudaError_t launch(const ChunkParams& p, const ChunkItem* items, int n, cudaStream_t s) {
+cudaError_t launch(const ChunkParams& p, bool early, const ChunkItem* items, int n, cudaStream_t s) {
   static bool configured[64] = {};
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
@@ -652,34 +662,28 @@ cudaError_t launch(const ChunkParams& p, const ChunkItem* items, int n, cudaStre
     if (dev >= 0 && dev < 64) configured[dev] = true;
   }
   if ((int64_t)n * p.h_kv > INT32_MAX) return cudaErrorInvalidValue;
-  chunk_mma_kernel<D, FP8, MT><<<n * p.h_kv, kThreads, smem_bytes<D, FP8, MT>(), s>>>(p, items);
-  return cudaGetLastError();
+  return launch_early(early, chunk_mma_kernel<D, FP8, MT>, dim3(n * p.h_kv), kThreads, smem_bytes<D, FP8, MT>(), s, p, items);
 }
 
 }  // namespace
 
-cudaError_t launch_chunk_mma(const ChunkParams& p, int head_dim, bool fp8, int rows16, const ChunkItem* items,
+cudaError_t launch_chunk_mma(const ChunkParams& p, int head_dim, bool fp8, int rows16, bool early, const ChunkItem* items,
                              int n_items, cudaStream_t s) {
   if (head_dim == 128) {
-    if (rows16 == 1) return fp8 ? launch<128, true, 1>(p, items, n_items, s) : launch<128, false, 1>(p, items, n_items, s);
-    return fp8 ? launch<128, true, 2>(p, items, n_items, s) : launch<128, false, 2>(p, items, n_items, s);
+    if (rows16 == 1) return fp8 ? launch<128, true, 1>(p, early, items, n_items, s) : launch<128, false, 1>(p, early, items, n_items, s);
+    return fp8 ? launch<128, true, 2>(p, early, items, n_items, s) : launch<128, false, 2>(p, early, items, n_items, s);
   }
-  if (rows16 == 1) return fp8 ? launch<64, true, 1>(p, items, n_items, s) : launch<64, false, 1>(p, items, n_items, s);
-  return fp8 ? launch<64, true, 2>(p, items, n_items, s) : launch<64, false, 2>(p, items, n_items, s);
+  if (rows16 == 1) return fp8 ? launch<64, true, 1>(p, early, items, n_items, s) : launch<64, false, 1>(p, early, items, n_items, s);
+  return fp8 ? launch<64, true, 2>(p, early, items, n_items, s) : launch<64, false, 2>(p, early, items, n_items, s);
 }
 
 cudaError_t launch_chunk_merge(const ChunkParams& p, int head_dim, int most, const ChunkMerge* work, int n_work, cudaStream_t s) {
   // four warps to a row where it has more splits than one of them keeps under way
   const bool many = most > 8;
   const dim3 grid(n_work, many ? p.h_q : (p.h_q + 3) / 4);
-  if (head_dim == 128) {
-    if (many) chunk_merge_kernel<128, 4><<<grid, 128, 0, s>>>(p, work);
-    else chunk_merge_kernel<128, 1><<<grid, 128, 0, s>>>(p, work);
-  } else {
-    if (many) chunk_merge_kernel<64, 4><<<grid, 128, 0, s>>>(p, work);
-    else chunk_merge_kernel<64, 1><<<grid, 128, 0, s>>>(p, work);
-  }
-  return cudaGetLastError();
+  auto* kernel = head_dim == 128 ? (many ? chunk_merge_kernel<128, 4> : chunk_merge_kernel<128, 1>)
+                                 : (many ? chunk_merge_kernel<64, 4> : chunk_merge_kernel<64, 1>);
+  return launch_early(true, kernel, grid, 128, 0, s, p, work);
 }
 
 }  // namespace pad

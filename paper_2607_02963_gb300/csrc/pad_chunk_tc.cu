@@ -201,6 +201,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   const ChunkItem it = items[(int)blockIdx.x / p.h_kv];
   const int kvh = (int)blockIdx.x % p.h_kv, G = p.group, tps = 128 / G;
+  grid_release();  // (what starts beside this grid is behind all that this grid was behind)
   const int key0 = it.key0, key1 = it.key1;
   // (as a warp-uniform value: the issuers' loops, and with them the MMAs' descriptors, stay in uniform registers)
   const int n_tiles = __shfl_sync(0xffffffffu, key1 > key0 ? (key1 - key0 + kBN - 1) / kBN : 0, 0);
@@ -256,7 +257,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   const int32_t* table = p.page_table + (paged ? it.src * p.max_pages : 0);
   auto page_of = [&](int t) -> int {
     const int key = key0 + t * kBN + 32 * w + lane;
-    return paged && t < n_tiles && key < key1 ? __ldg(table + (key >> p.page_shift)) : 0;
+    return paged && t < n_tiles && key < key1 ? __ldcg(table + (key >> p.page_shift)) : 0;
   };
   // The rows that are there.  A row lies `idx` x mul (+ its slot within the page) from the base: idx is its
   // page, or of a prefix its token.
@@ -293,7 +294,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   // By TMA: lane L's page of a tile holds keys L x page size on; the pages that are there.
   auto tile_page = [&](int t) -> int {
     const int key = key0 + t * kBN + (lane << p.page_shift);
-    return paged && t < n_tiles && lane < (kBN >> p.page_shift) && key < key1 ? __ldg(table + (key >> p.page_shift)) : 0;
+    return paged && t < n_tiles && lane < (kBN >> p.page_shift) && key < key1 ? __ldcg(table + (key >> p.page_shift)) : 0;
   };
   auto tile_pages = [&](int t, int page) -> uint32_t {
     const int key = key0 + t * kBN + (lane << p.page_shift);
@@ -900,18 +901,18 @@ __global__ void __launch_bounds__(kThreads, 1)
         // the values that were left out, of the keys that this row sees
 #pragma unroll 1
         for (int key = max(itv.key0, itv.lim0); key < itv.key0 + lim; ++key) {
-          const int pg = __ldg(p.page_table + itv.src * p.max_pages + (key >> p.page_shift));
+          const int pg = __ldcg(p.page_table + itv.src * p.max_pages + (key >> p.page_shift));
           if ((unsigned)pg >= (unsigned)p.n_pages) continue;
           const int64_t slot = ((int64_t)pg * p.h_kv + kvh) * p.page_size + (key & (p.page_size - 1));
           if (FP8) {
-            if (__ldg(p.v_scale + slot) == 255)
+            if (__ldcg(p.v_scale + slot) == 255)
 #pragma unroll
               for (int i = 0; i < 32; ++i) r[i] = 0x7fc00000u;
           } else {
             const uint32_t* v = reinterpret_cast<const uint32_t*>(static_cast<const __nv_bfloat16*>(p.v_pool) + slot * D + c0);
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-              const uint32_t x = __ldg(v + i);
+              const uint32_t x = __ldcg(v + i);
               if (!odd2(x)) continue;
               if ((x & 0x7f80u) == 0x7f80u) r[2 * i] = __float_as_uint(__uint_as_float(r[2 * i]) + __uint_as_float(x << 16));
               if ((x & 0x7f800000u) == 0x7f800000u)
@@ -1017,8 +1018,7 @@ cudaError_t launch(const ChunkParams& p, int64_t prefix_tokens, const ChunkItem*
   }
   if (prefix_tokens > 0 && !prefix_tensor_maps(p.k_prefix, p.v_prefix, D, p.h_kv, prefix_tokens, &maps.k_prefix, &maps.v_prefix))
     return cudaErrorInvalidValue;
-  chunk_tc_kernel<D, FP8, SPLIT><<<n * p.h_kv, kThreads, Cfg<D, FP8>::kSmemBytes, s>>>(p, maps, items);
-  return cudaGetLastError();
+  return launch_early(false, chunk_tc_kernel<D, FP8, SPLIT>, dim3(n * p.h_kv), kThreads, Cfg<D, FP8>::kSmemBytes, s, p, maps, items);
 }
 
 }  // namespace

@@ -48,9 +48,8 @@ __device__ __forceinline__ int64_t warp_sum(int64_t v) {
 template <class T>
 __global__ void __cluster_dims__(kCtas, 1, 1) __launch_bounds__(kThreads)
     draft_verify_kernel(const __grid_constant__ ChunkParams pr, const ChunkVerify* __restrict__ work, int vocab,
-                        const T* __restrict__ p, int64_t p_stride, const T* __restrict__ q, int64_t q_stride,
-                        const int32_t* __restrict__ draft, const float* __restrict__ u_accept,
-                        const float* __restrict__ u_pick, int32_t* __restrict__ accepted, int32_t* __restrict__ token) {
+                        const T* p, int64_t p_stride, const T* q, int64_t q_stride,
+                        const int32_t* draft, const float* u_accept, const float* u_pick, int32_t* __restrict__ accepted, int32_t* __restrict__ token) {
   __shared__ int first_bad;
   __shared__ int64_t part[kWarps];       // sums of each warp's entries
   __shared__ int64_t sums[2][kCtas];     // of each CTA's: first round, second round
@@ -166,9 +165,8 @@ template <class T>
 cudaError_t launch(const ChunkParams& p, const ChunkVerify* work, int n, int vocab, const void* tp, int64_t ps,
                    const void* dq, int64_t qs, const int32_t* draft, const float* ua, const float* up, int32_t* acc,
                    int32_t* tok, cudaStream_t s) {
-  draft_verify_kernel<T><<<n * kCtas, kThreads, 0, s>>>(p, work, vocab, static_cast<const T*>(tp), ps, static_cast<const T*>(dq),
-                                                        qs, draft, ua, up, acc, tok);
-  return cudaGetLastError();
+  return launch_early(false, draft_verify_kernel<T>, dim3(n * kCtas), kThreads, 0, s, p, work, vocab, static_cast<const T*>(tp), ps,
+                      static_cast<const T*>(dq), qs, draft, ua, up, acc, tok);
 }
 
 }  // namespace
