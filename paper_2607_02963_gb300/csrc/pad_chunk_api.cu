@@ -137,44 +137,71 @@ void cut_mma(std::vector<Segment>& segs, int paged, const pad_problem& prob, int
     if (!s.tc && s.paged == paged) split_by(s, len, kSplitUnit);
 }
 
-// The tcgen05 kernel: one CTA per SM at a time, so its time is that of its waves: a CTA's start and end, and
-// its tiles one after the other.  Both forms and the key ranges' length (in tiles) are costed with what was
-// measured on GB300 (us), the partial states with their way out and in again.
-constexpr double kTcCta = 5.0, kTcFirst = 4.0, kPairTile = 1.55, kSplitTile = 1.8, kPartialRate = 3e6;  // bytes per us
+// CTAs of a kernel that runs one per SM, the longest first: the time until the last ends.  Loads are kept as
+// (load, SMs that have it); CTAs of one length are dealt out together.
+double makespan(std::vector<std::pair<double, int64_t>>& ctas, int sms) {
+  std::sort(ctas.begin(), ctas.end(), [](auto& x, auto& y) { return x.first > y.first; });
+  std::vector<std::pair<double, int64_t>> load{{0.0, sms}};  // ascending
+  double last = 0;
+  for (auto [len, n] : ctas) {
+    while (n > 0) {
+      // (more CTAs of one length than can matter one by one: whole rounds at once)
+      const int64_t k = std::min(n, load[0].second);
+      const double at = load[0].first + len;
+      n -= k;
+      load[0].second -= k;
+      if (load[0].second == 0) load.erase(load.begin());
+      auto it = std::lower_bound(load.begin(), load.end(), at, [](auto& x, double v) { return x.first < v; });
+      if (it != load.end() && it->first == at) it->second += k;
+      else load.insert(it, {at, k});
+      last = std::max(last, at);
+    }
+  }
+  return last;
+}
+
+// The tcgen05 kernel: both of its forms and the length of the key ranges (in tiles) are costed with what was
+// measured on GB300 (us): a CTA's start and end, a tile of each form, the partial states' way out and in
+// again.
+constexpr double kTcCta = 7.0, kPairTile = 1.48, kSplitTile = 0.95, kPartialRate = 4e6;  // bytes per us
 void cut_tc(std::vector<Segment>& segs, const pad_problem& prob, int sms, bool& split) {
   const int tps = 128 / (prob.h_q / prob.h_kv);
-  double best = 1e300;
-  int64_t best_len = 0;
   auto tiles_of = [](const Segment& s) { return ((int64_t)s.keys + 127) / 128; };
   int64_t longest = 0;
-  for (const Segment& s : segs)
-    if (s.tc) longest = std::max(longest, tiles_of(s));
+  double total = 0;
+  for (const Segment& s : segs) {
+    if (!s.tc) continue;
+    longest = std::max(longest, tiles_of(s));
+    total += (double)tiles_of(s) * (double)((s.ntok + tps - 1) / tps) * prob.h_kv;
+  }
   if (longest == 0) return;
+  double best = 1e300;
+  int64_t best_len = longest;
+  std::vector<std::pair<double, int64_t>> ctas;
   for (int form = 0; form < 2; ++form) {
     const int tpc = form ? tps : 2 * tps;
     const double tile = form ? kSplitTile : kPairTile;
-    for (int64_t len = longest;; len = len > 16 ? std::max<int64_t>(16, len * 7 / 8) : len - 1) {
-      double ctas = 0, work = 0, bytes = 0;
-      int64_t most = 0;
+    // (ranges much shorter than an SM's share of the work only add starts)
+    const int64_t least = std::max<int64_t>(1, (int64_t)(total / sms / 12));
+    for (int64_t len = longest;;) {
+      ctas.clear();
+      double bytes = 0;
       for (const Segment& s : segs) {
         if (!s.tc) continue;
         const int64_t tiles = tiles_of(s), n = (tiles + len - 1) / len, each = (tiles + n - 1) / n;
-        const double rows = (double)((s.ntok + tpc - 1) / tpc) * prob.h_kv;
-        ctas += rows * (double)n;
-        work += rows * (double)tiles;
-        most = std::max(most, each);
-        if (n > 1) bytes += 2.0 * (double)n * s.ntok * prob.h_q * (prob.head_dim + 2) * 4;
+        ctas.push_back({kTcCta + tile * (double)each, (int64_t)((s.ntok + tpc - 1) / tpc) * prob.h_kv * n});
+        if (n > 1 || !s.paged) bytes += 2.0 * (double)n * s.ntok * prob.h_q * (prob.head_dim + 2) * 4;
       }
-      const double waves = std::ceil(ctas / sms);
-      // few waves are as long as their longest CTAs; many even out
-      const double t = kTcFirst + bytes / kPartialRate +
-                       (waves <= 4 ? waves * (kTcCta + tile * (double)most) : (ctas * kTcCta + work * tile) / sms + tile * (double)most);
+      const double t = makespan(ctas, sms) + bytes / kPartialRate;
       if (t < best) {
         best = t;
         best_len = len;
         split = form != 0;
       }
-      if (len <= 1) break;
+      if (len <= least) break;
+      // the next length that changes the longest one's count of ranges (in steps of an eighth where that is slow)
+      const int64_t n = (longest + len - 1) / len;
+      len = std::max<int64_t>(least, std::min(len - 1, std::min((longest + n) / (n + 1), n > 8 ? len * 15 / 16 : len)));
     }
   }
   for (Segment& s : segs)

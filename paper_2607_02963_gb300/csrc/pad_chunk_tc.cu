@@ -201,6 +201,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   const ChunkItem it = items[(int)blockIdx.x / p.h_kv];
   const int kvh = (int)blockIdx.x % p.h_kv, G = p.group, tps = 128 / G;
+  const int inv_g = 65536 / G + 1;  // row / G = row * inv_g >> 16 for rows below 128
   grid_release();  // (what starts beside this grid is behind all that this grid was behind)
   const int key0 = it.key0, key1 = it.key1;
   // (as a warp-uniform value: the issuers' loops, and with them the MMAs' descriptors, stay in uniform registers)
@@ -343,14 +344,22 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (!wide) issue_bf16(k_base, sbase + C::kOffK, 0, idx, there);
     }
   } else {
-    // Q of the slots by the others: row = token * G + head; what has no token is zero
-    constexpr int CH = D / 8;
-    for (int i = threadIdx.x; i < (SPLIT ? 1 : 2) * 128 * CH; i += 384) {
-      const int c = i % CH, r = i / CH, g = r >> 7, row = r & 127, tl = row / G, tok = g * tps + tl;
-      uint4 v = make_uint4(0u, 0u, 0u, 0u);
-      if (tl < tps && tok < it.ntok)
-        v = __ldcg(reinterpret_cast<const uint4*>(p.q + (it.tok0 + tok) * p.q_stride + (int64_t)(kvh * G + row - tl * G) * D) + c);
-      sts128(sbase + g * C::kTileBytes + (c >> 3) * C::kBoxBytes + row * 128 + (((c & 7) ^ (row & 7)) << 4), v);
+    // Q of the slots by the others: row = token * G + head; what has no token is zero.  All of a thread's
+    // chunks are under way together.
+    constexpr int CH = D / 8, N = (SPLIT ? 1 : 2) * 128 * CH, PER = (N + 383) / 384;
+    uint4 v[PER];
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+      const int i = (int)threadIdx.x + 384 * k, c = i % CH, r = i / CH, g = r >> 7, row = r & 127;
+      const int tl = row * inv_g >> 16, tok = g * tps + tl;
+      v[k] = make_uint4(0u, 0u, 0u, 0u);
+      if (i < N && tl < tps && tok < it.ntok)
+        v[k] = __ldcg(reinterpret_cast<const uint4*>(p.q + (it.tok0 + tok) * p.q_stride + (int64_t)(kvh * G + row - tl * G) * D) + c);
+    }
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+      const int i = (int)threadIdx.x + 384 * k, c = i % CH, r = i / CH, g = r >> 7, row = r & 127;
+      if (i < N) sts128(sbase + g * C::kTileBytes + (c >> 3) * C::kBoxBytes + row * 128 + (((c & 7) ^ (row & 7)) << 4), v[k]);
     }
     proxy_fence();
   }
@@ -733,7 +742,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int g = (warp - 4) >> 2;             // slot
     const int wrow = 32 * (warp & 3);          // TMEM lanes wrow .. wrow + 31
     const int row = wrow + lane;               // row of the slot: token row / G, head row % G
-    const int tl = row / G;
+    const int tl = row * inv_g >> 16;
     const int tok = (SPLIT ? 0 : g * tps) + tl;  // of the item
     const bool active = tl < tps && tok < it.ntok;
     const int lim = active ? min(it.lim0 + (paged ? tok : 0), key1) - key0 : 0x7fffffff;  // keys of the item it sees
@@ -977,14 +986,15 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
         }
         __syncwarp();
-#pragma unroll 1
-        for (int i = lane; i < 32 * kCh / (SPLIT && bf16 ? 2 : 1); i += 32) {
-          const int r = SPLIT && bf16 ? i / (kCh / 2) : i / kCh;
-          const int c = SPLIT && bf16 ? g * (kCh / 2) + i % (kCh / 2) : i % kCh;
-          const int rr = wrow + r, rt = rr / G, rtok = (SPLIT ? 0 : g * tps) + rt;
+        // (rows of kCh chunks, or of the half that this slot writes: `per` lanes a row)
+        const bool half = SPLIT && bf16;
+        const int per = half ? kCh / 2 : kCh, cl = (half ? g * (kCh / 2) : 0) + lane % per, rows = 32 / per;
+#pragma unroll 4
+        for (int k = lane / per; k < 32; k += rows) {
+          const int rr = wrow + k, rt = rr * inv_g >> 16, rtok = (SPLIT ? 0 : g * tps) + rt;
           if (rt < tps && rtok < ntok) {
-            const uint4 v = *reinterpret_cast<const uint4*>(stg + r * (2 * D) + ((c ^ (r & (kCh - 1))) << 4));
-            const int64_t o = (row0 + (int64_t)rtok * p.h_q + kvh * G + (rr - rt * G)) * D * esz + (int64_t)ps * (2 * D) + 16 * c;
+            const uint4 v = *reinterpret_cast<const uint4*>(stg + k * (2 * D) + ((cl ^ (k & (kCh - 1))) << 4));
+            const int64_t o = (row0 + (int64_t)rtok * p.h_q + kvh * G + (rr - rt * G)) * D * esz + (int64_t)ps * (2 * D) + 16 * cl;
             *reinterpret_cast<uint4*>(base + o) = v;
           }
         }
