@@ -52,7 +52,7 @@ struct ChunkVerify {
 struct ChunkParams {
   int32_t h_q, h_kv, group, page_size, page_shift, max_pages, n_pages;
   int32_t out_bf16;
-  int32_t beside;   // the warp-level kernel runs beside the tcgen05 kernel of the same call
+  int32_t beside;   // the tcgen05 kernel runs beside the warp-level kernel of the same call
   float scale_log2;
   uint64_t gen;
   PadDevHeader* header;

@@ -617,16 +617,17 @@ pad_status pad_chunk_attn(const pad_chunk_t* c, const void* q, int64_t q_stride,
   p.lse = lse;
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   cudaError_t e = cudaSuccess;
-  if (!c->L.tc.empty())
-    e = launch_chunk_tc(p, c->prob.head_dim, c->kv_format == PAD_KV_FP8, c->L.tc_split, c->L.prefix_tokens, list<ChunkItem>(c, c->L.off_tc),
-                        (int)c->L.tc.size(), s);
-  if (e == cudaSuccess && !c->L.pre.empty())
-    e = launch_chunk_mma(p, c->prob.head_dim, false, c->L.pre_rows16, !c->L.tc.empty(), list<ChunkItem>(c, c->L.off_pre), (int)c->L.pre.size(), s);
-  p.beside = !c->L.tc.empty() && c->L.pre.empty();
+  // the warp-level kernel first: its CTAs are short and share an SM, those of the other take one each
+  const bool fp8 = c->kv_format == PAD_KV_FP8;
+  if (!c->L.pre.empty())
+    e = launch_chunk_mma(p, c->prob.head_dim, false, c->L.pre_rows16, false, list<ChunkItem>(c, c->L.off_pre), (int)c->L.pre.size(), s);
   if (e == cudaSuccess && !c->L.page.empty())
-    e = launch_chunk_mma(p, c->prob.head_dim, c->kv_format == PAD_KV_FP8, c->L.page_rows16,
-                         !c->L.tc.empty() || !c->L.pre.empty(), list<ChunkItem>(c, c->L.off_page),
+    e = launch_chunk_mma(p, c->prob.head_dim, fp8, c->L.page_rows16, !c->L.pre.empty(), list<ChunkItem>(c, c->L.off_page),
                          (int)c->L.page.size(), s);
+  p.beside = !c->L.pre.empty() || !c->L.page.empty();
+  if (e == cudaSuccess && !c->L.tc.empty())
+    e = launch_chunk_tc(p, c->prob.head_dim, fp8, c->L.tc_split, c->L.prefix_tokens, list<ChunkItem>(c, c->L.off_tc),
+                        (int)c->L.tc.size(), s);
   if (e == cudaSuccess && !c->L.merge.empty())
     e = launch_chunk_merge(p, c->prob.head_dim, c->L.pre_splits + c->L.page_splits, list<ChunkMerge>(c, c->L.off_merge), (int)c->L.merge.size(), s);
   return e == cudaSuccess ? PAD_OK : cuda_fail(e, "chunk attention launch");

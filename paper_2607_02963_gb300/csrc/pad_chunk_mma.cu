@@ -127,9 +127,7 @@ __global__ void __launch_bounds__(kThreads, MT == 1 ? 3 : 2) chunk_mma_kernel(co
   const uint32_t ring_at = smem_u32(ring);
   const int n_rows = it.ntok * G;
 
-  // (beside the tcgen05 grid of the same call, which was launched in plain stream order: what the items here read is
-  // complete, and that grid is waited for at the end, so that the join's wait covers both)
-  if (!p.beside) grid_wait();
+  grid_wait();
   grid_release();
 
   const int n_blocks = it.key1 > it.key0 ? (it.key1 - it.key0 + kBlk - 1) / kBlk : 0;
@@ -561,7 +559,6 @@ __global__ void __launch_bounds__(kThreads, MT == 1 ? 3 : 2) chunk_mma_kernel(co
       if (c == 0 && p.lse != nullptr) p.lse[row] = l_all == 0.f ? kNegInf : (m_all + log2f(l_all)) * kLn2;
     }
   }
-  if (p.beside) grid_wait();
 }
 
 // The split key ranges of one (token, query head) joined: weights 2^(m_s - max m), O and l added up in a fixed

@@ -202,12 +202,15 @@ __global__ void __launch_bounds__(kThreads, 1)
   const ChunkItem it = items[(int)blockIdx.x / p.h_kv];
   const int kvh = (int)blockIdx.x % p.h_kv, G = p.group, tps = 128 / G;
   const int inv_g = 65536 / G + 1;  // row / G = row * inv_g >> 16 for rows below 128
-  grid_release();  // (what starts beside this grid is behind all that this grid was behind)
+  // (beside the warp-level grid of the same call, which was launched in plain stream order: what the items here read is
+  // complete, and that grid is waited for at the end, so that the join's wait covers both)
+  grid_release();
   const int key0 = it.key0, key1 = it.key1;
   // (as a warp-uniform value: the issuers' loops, and with them the MMAs' descriptors, stay in uniform registers)
   const int n_tiles = __shfl_sync(0xffffffffu, key1 > key0 ? (key1 - key0 + kBN - 1) / kBN : 0, 0);
 
   if (n_tiles == 0 || (sbase & 1023u)) {
+    if (p.beside) grid_wait();
     if (sbase & 1023u) {  // the swizzle atoms need 1024-byte alignment (never expected)
       if (threadIdx.x == 0) pad_set_error(p.header, p.gen, PAD_ERR_UNSUPPORTED, (int)blockIdx.x, (int)sbase, 0);
     }
@@ -455,6 +458,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       __syncwarp();
       fence_after();
       asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
+      if (p.beside) grid_wait();
     }
   } else if (warp >= 12) {
     // ------------------------------------------------------------ loaders
@@ -1028,7 +1032,7 @@ cudaError_t launch(const ChunkParams& p, int64_t prefix_tokens, const ChunkItem*
   }
   if (prefix_tokens > 0 && !prefix_tensor_maps(p.k_prefix, p.v_prefix, D, p.h_kv, prefix_tokens, &maps.k_prefix, &maps.v_prefix))
     return cudaErrorInvalidValue;
-  return launch_early(false, chunk_tc_kernel<D, FP8, SPLIT>, dim3(n * p.h_kv), kThreads, Cfg<D, FP8>::kSmemBytes, s, p, maps, items);
+  return launch_early(p.beside, chunk_tc_kernel<D, FP8, SPLIT>, dim3(n * p.h_kv), kThreads, Cfg<D, FP8>::kSmemBytes, s, p, maps, items);
 }
 
 }  // namespace
