@@ -19,7 +19,7 @@ namespace pad {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kReadTokens = 64;  // of a span
+constexpr int kReadTokens = 32;  // of a span
 
 // 16 lanes of 8 bf16 values (8 at head_dim 64) hold one group.
 template <int D, bool FP8>

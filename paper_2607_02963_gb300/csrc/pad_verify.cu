@@ -32,11 +32,22 @@ constexpr int kWarps = kThreads / 32;
 __device__ __forceinline__ float value(float x) { return x; }
 __device__ __forceinline__ float value(__nv_bfloat16 x) { return __bfloat162float(x); }
 
-// floor(2^38 min(r, 1)), 0 for a NaN: the 24-bit mantissa shifted (a 64-bit conversion takes longer).
+// floor(2^38 min(r, 1)), 0 for a NaN, as its upper and lower 19 bits, each in the low bits of a float's pattern
+// (above those of 2^23): adding 2^23 with rounding down leaves the floor there, and what it cuts off is
+// exact in fp32.  (Patterns are added as they are; 64-bit shifts or conversions take twice the instructions.)
+struct Halves {
+  uint32_t hi, lo;
+};
+constexpr uint32_t kBase = 0x4b000000u;  // the pattern of 2^23
+__device__ __forceinline__ Halves halves(float r) {
+  const float x = fminf(fmaxf(r, 0.f), 1.f) * 524288.f;  // 2^19; fmaxf(NaN, 0) = 0
+  const float t = __fadd_rd(x, 8388608.f);
+  const float rest = x - (t - 8388608.f);
+  return {__float_as_uint(t), __float_as_uint(__fmaf_rd(rest, 524288.f, 8388608.f))};
+}
 __device__ __forceinline__ int64_t weight(float r) {
-  const uint32_t b = r > 0.f ? __float_as_uint(fminf(r, 1.f)) : 0u;
-  const uint64_t m = (uint64_t)((b & 0x7fffffu) | (b >= 0x800000u ? 0x800000u : 0u)) << 15;  // 2^38 at r = 1
-  return (int64_t)(m >> min(127u - (b >> 23), 63u));  // (a subnormal, far below 2^-38, becomes 0)
+  const Halves h = halves(r);
+  return ((int64_t)(h.hi - kBase) << 19) + (int64_t)(h.lo - kBase);
 }
 
 __device__ __forceinline__ int64_t warp_sum(int64_t v) {
@@ -87,7 +98,7 @@ __global__ void __cluster_dims__(kCtas, 1, 1) __launch_bounds__(kThreads)
   bool take = sub;
   int64_t total = 0, before = 0, mine = 0;
   for (int round = 0;; ++round) {
-    int64_t s = 0;
+    uint32_t hi32 = 0, lo32 = 0, n = 0;  // (a thread adds up at most 2^12 + 8 entries: its sums stay below 2^32)
     constexpr int U = 8;
     for (int i0 = lo + lane; i0 < hi; i0 += 32 * U) {
       float x[U], y[U];
@@ -100,9 +111,14 @@ __global__ void __cluster_dims__(kCtas, 1, 1) __launch_bounds__(kThreads)
         }
       }
 #pragma unroll
-      for (int j = 0; j < U; ++j) s += weight(x[j] - y[j]);
+      for (int j = 0; j < U; ++j) {
+        const Halves h = halves(x[j] - y[j]);
+        hi32 += h.hi;
+        lo32 += h.lo;
+      }
+      n += U;
     }
-    s = warp_sum(s);
+    const int64_t s = warp_sum(((int64_t)(hi32 - n * kBase) << 19) + (int64_t)(lo32 - n * kBase));
     if (lane == 0) part[warp] = s;
     __syncthreads();
     if (round == 0) cl.barrier_wait();

@@ -520,3 +520,64 @@ def test_refusals():
         B.pad_chunk_plan(plan.problem, None, [16], [0], [4], [2], page_table=c.dt, n_pages=c.n_pages, kv_format=B.KV_FP8,
                          workspace=c.ws[16:])
     B.pad_chunk_status(plan)
+
+
+# ------------------------------------------------------------------------------ the steps together
+
+
+@pytest.mark.parametrize("kv_format", [B.KV_BF16, B.KV_FP8])
+def test_speculative_steps_together(kv_format):
+    """Drafts written, attended, verified and partly taken back, step after step: the cache holds exactly the kept
+    tokens, in the lowest pages, and a step's attention is that over them."""
+    from paper_2607_02963_gb300.speculative import BranchCache
+    events, page, hq, hk, d, vocab = 3, 4, 8, 2, 64, 50
+    g = torch.Generator().manual_seed(3)
+    cache = BranchCache(hq, hk, d, events, n_pages=40, max_pages=12, page_size=page, kv_format=kv_format,
+                        prefix_len=[20], event_video=[0] * events, out_dtype=0)
+    k_pre, v_pre = torch.randn(20, hk, d, generator=g).bfloat16(), torch.randn(20, hk, d, generator=g).bfloat16()
+    held = [[np.zeros((0, hk, d))] * 2 for _ in range(events)]
+
+    def stored(x):
+        x = x.double().numpy()
+        return oracle.kv8_decode(*oracle.kv8_encode(x)) if kv_format == B.KV_FP8 else x
+
+    for step in range(4):
+        news = np.array([1 + step, 4, 6 - step])
+        plan = cache.plan(news)
+        n, nd = int(news.sum()), int((news - 1).sum())
+        q, k, v = (torch.randn(n, h, d, generator=g).bfloat16() for h in (hq, hk, hk))
+        cache.append(plan, k.cuda(), v.cuda())
+        lse = torch.empty(n, hq, device="cuda")
+        out = cache.attend(plan, q.cuda(), k_pre.cuda(), v_pre.cuda(), lse=lse)
+        p = _tables(g, n, vocab, torch.float32)
+        has = torch.cat([torch.arange(m) < m - 1 for m in news])
+        dq = torch.softmax(torch.log(p[has] + 1e-9) + 0.8 * torch.randn(nd, vocab, generator=g), -1)
+        draft = torch.multinomial(dq, 1, generator=g)[:, 0].to(torch.int32)
+        ua, up = torch.rand(nd, generator=g), torch.rand(events, generator=g)
+        acc, tok = cache.verify(plan, p.cuda(), dq.cuda(), draft.cuda(), ua.cuda(), up.cuda())
+        B.pad_chunk_status(plan)
+        out, lse, at, dat = out.double().cpu().numpy(), lse.double().cpu().numpy(), 0, 0
+        lens = cache.commit(plan, acc)
+        for e, m in enumerate(int(x) for x in news):
+            kk = np.concatenate([k_pre.double().numpy(), held[e][0], stored(k[at:at + m])])
+            vv = np.concatenate([v_pre.double().numpy(), held[e][1], stored(v[at:at + m])])
+            o, l, mag = oracle.chunk_attention(q[at:at + m].double().numpy(), kk, vv, 20 + len(held[e][0]) + 1, d ** -0.5)
+            assert np.all(np.abs(out[at:at + m] - o) <= (2.0 ** -8 + 1e-4) * mag) and np.all(np.abs(lse[at:at + m] - l) <= 1e-4)
+            a, t = oracle.draft_verify(p[at:at + m].numpy(), dq[dat:dat + m - 1].numpy(), draft[dat:dat + m - 1].tolist(),
+                                       ua[dat:dat + m - 1].numpy(), float(up[e]))
+            assert (a, t) == (int(acc[e]), int(tok[e]))
+            held[e] = [np.concatenate([held[e][i], stored(x[at:at + a + 1])]) for i, x in enumerate((k, v))]
+            assert lens[e] == len(held[e][0])
+            at, dat = at + m, dat + m - 1
+        in_use = cache.pages.n_pages - cache.pages.free_count
+        assert in_use == sum((int(x) + page - 1) // page for x in lens)
+    plan = cache.plan([0] * events)
+    k, v = cache.read(plan)
+    assert np.array_equal(k.double().cpu().numpy(), np.concatenate([h[0] for h in held]))
+    assert np.array_equal(v.double().cpu().numpy(), np.concatenate([h[1] for h in held]))
+
+
+def test_the_example_runs():
+    from paper_2607_02963_gb300 import speculative
+    kept, cache = speculative.example(events=3, drafts=3, steps=3, prefix=200, vocab=500, h_q=8, h_kv=2)
+    assert np.array_equal(cache.event_len, np.sum(kept, axis=0)) and all(1 <= k <= 4 for row in kept for k in row)
