@@ -576,14 +576,23 @@ def pad_chunk_plan(problem: Problem, cache, prefix_len, event_video, event_len, 
     return ChunkPlan(h, problem, ne, int(kv_format), int(n_pages), (page_table, workspace))
 
 
+# (The per-layer calls check their tensors in line, by attribute: a helper call for each would be a quarter of a
+# small call's time on the host.  What does not pass goes through the helpers, which say why.)
+
+
 def pad_chunk_append(plan: ChunkPlan, k_new, v_new, k_pool, v_pool, k_scale=None, v_scale=None, stream=None):
     """Write the new tokens' K/V into the branches' pages (quantised in an 8-bit cache)."""
-    kn, ks = _rows(k_new, "k_new", plan._new_shape, plan._bf16)
-    vn, vs = _rows(v_new, "v_new", plan._new_shape, plan._bf16)
-    if ks != vs:
-        raise ValueError("k_new and v_new must have the same token stride")
+    shape, bf16 = plan._new_shape, plan._bf16
+    if (k_new.shape == shape and v_new.shape == shape and k_new.dtype is bf16 and v_new.dtype is bf16
+            and k_new.is_contiguous() and v_new.is_contiguous()):
+        kn, vn, ks = k_new.data_ptr(), v_new.data_ptr(), 0
+    else:
+        kn, ks = _rows(k_new, "k_new", shape, bf16)
+        vn, vs = _rows(v_new, "v_new", shape, bf16)
+        if ks != vs:
+            raise ValueError("k_new and v_new must have the same token stride")
     kp, vp, ksc, vsc = plan._pools(k_pool, v_pool, k_scale, v_scale)
-    st = lib().pad_chunk_append(plan._h, kn, vn, ks, kp, vp, ksc, vsc, _stream_handle(stream))
+    st = (_lib or lib()).pad_chunk_append(plan._h, kn, vn, ks, kp, vp, ksc, vsc, _stream_handle(stream))
     if st:
         _check(st)
 
@@ -591,8 +600,12 @@ def pad_chunk_append(plan: ChunkPlan, k_new, v_new, k_pool, v_pool, k_scale=None
 def pad_chunk_read(plan: ChunkPlan, k_pool, v_pool, k_out, v_out, k_scale=None, v_scale=None, stream=None):
     """Copy every branch's cached tokens out as contiguous bf16 [n_cached, h_kv, head_dim]."""
     kp, vp, ksc, vsc = plan._pools(k_pool, v_pool, k_scale, v_scale)
-    ko, vo = (_dev(k_out, "k_out", plan._read_shape, plan._bf16), _dev(v_out, "v_out", plan._read_shape, plan._bf16))
-    st = lib().pad_chunk_read(plan._h, kp, vp, ksc, vsc, ko, vo, _stream_handle(stream))
+    shape, bf16 = plan._read_shape, plan._bf16
+    if not (k_out.shape == shape and v_out.shape == shape and k_out.dtype is bf16 and v_out.dtype is bf16
+            and k_out.is_contiguous() and v_out.is_contiguous()):
+        _dev(k_out, "k_out", shape, bf16)
+        _dev(v_out, "v_out", shape, bf16)
+    st = (_lib or lib()).pad_chunk_read(plan._h, kp, vp, ksc, vsc, k_out.data_ptr(), v_out.data_ptr(), _stream_handle(stream))
     if st:
         _check(st)
 
@@ -600,14 +613,26 @@ def pad_chunk_read(plan: ChunkPlan, k_pool, v_pool, k_out, v_out, k_scale=None, 
 def pad_chunk_attn(plan: ChunkPlan, q, k_prefix, v_prefix, k_pool, v_pool, out, lse=None, k_scale=None, v_scale=None,
                    stream=None):
     """Attention of the step's new tokens over their video's prefix and their branch's cached tokens."""
-    qp, qs = _rows(q, "q", plan._q_shape, plan._bf16)
+    shape = plan._q_shape
+    if q.shape == shape and q.dtype is plan._bf16 and q.is_contiguous():
+        qp, qs = q.data_ptr(), 0
+    else:
+        qp, qs = _rows(q, "q", shape, plan._bf16)
+    if not (out.shape == shape and out.dtype is plan._out_type and out.is_contiguous()):
+        _dev(out, "out", shape, plan._out_type)
+    if lse is None:
+        lp = None
+    else:
+        if not (lse.shape == plan._lse_shape and lse.dtype is plan._f32 and lse.is_contiguous()):
+            _dev(lse, "lse", plan._lse_shape, plan._f32)
+        lp = lse.data_ptr()
     kp, vp, ksc, vsc = plan._pools(k_pool, v_pool, k_scale, v_scale)
     kx, vx = None, None
     if k_prefix is not None:
         kx = _dev(k_prefix, "k_prefix", (k_prefix.shape[0],) + plan._new_shape[1:], plan._bf16)
         vx = _dev(v_prefix, "v_prefix", k_prefix.shape, plan._bf16)
-    st = lib().pad_chunk_attn(plan._h, qp, qs, kx, vx, kp, vp, ksc, vsc, _dev(out, "out", plan._q_shape, plan._out_type),
-                              _dev(lse, "lse", plan._lse_shape, plan._f32), _stream_handle(stream))
+    st = (_lib or lib()).pad_chunk_attn(plan._h, qp, qs, kx, vx, kp, vp, ksc, vsc, out.data_ptr(), lp,
+                                        _stream_handle(stream))
     if st:
         _check(st)
 
@@ -617,14 +642,25 @@ def pad_draft_verify(plan: ChunkPlan, p, q, draft, u_accept, u_pick, accepted, t
     the draft's q [n_drafts, vocab] (fp32 or bf16), and draw each branch's next token."""
     bf16 = p.dtype is plan._bf16
     kind = plan._bf16 if bf16 else plan._f32
-    vocab = int(p.shape[1])
-    pp, ps = _rows(p, "p", (plan.n_tokens, vocab), kind)
-    qp, qs = _rows(q, "q", (plan.n_drafts, vocab), kind)
-    nd, ne = (plan.n_drafts,), (plan.n_events,)
-    st = lib().pad_draft_verify(plan._h, vocab, 1 if bf16 else 0, pp, ps, qp, qs, _dev(draft, "draft", nd, plan._i32),
-                                _dev(u_accept, "u_accept", nd, plan._f32), _dev(u_pick, "u_pick", ne, plan._f32),
-                                _dev(accepted, "accepted", ne, plan._i32), _dev(token, "token", ne, plan._i32),
-                                _stream_handle(stream))
+    vocab = p.shape[1]
+    p_shape, q_shape, nd, ne = (plan.n_tokens, vocab), (plan.n_drafts, vocab), (plan.n_drafts,), (plan.n_events,)
+    if (p.shape == p_shape and q.shape == q_shape and p.dtype is kind and q.dtype is kind and p.is_contiguous()
+            and q.is_contiguous()):
+        pp, qp, ps, qs = p.data_ptr(), q.data_ptr(), 0, 0
+    else:
+        pp, ps = _rows(p, "p", p_shape, kind)
+        qp, qs = _rows(q, "q", q_shape, kind)
+    i32, f32 = plan._i32, plan._f32
+    if not (draft.shape == nd and u_accept.shape == nd and u_pick.shape == ne and accepted.shape == ne
+            and token.shape == ne and draft.dtype is i32 and u_accept.dtype is f32 and u_pick.dtype is f32
+            and accepted.dtype is i32 and token.dtype is i32 and draft.is_contiguous() and u_accept.is_contiguous()
+            and u_pick.is_contiguous() and accepted.is_contiguous() and token.is_contiguous()):
+        for t, name, shape, dt in ((draft, "draft", nd, i32), (u_accept, "u_accept", nd, f32),
+                                   (u_pick, "u_pick", ne, f32), (accepted, "accepted", ne, i32), (token, "token", ne, i32)):
+            _dev(t, name, shape, dt)
+    st = (_lib or lib()).pad_draft_verify(plan._h, vocab, 1 if bf16 else 0, pp, ps, qp, qs, draft.data_ptr(),
+                                          u_accept.data_ptr(), u_pick.data_ptr(), accepted.data_ptr(),
+                                          token.data_ptr(), _stream_handle(stream))
     if st:
         _check(st)
 
