@@ -332,6 +332,21 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     __syncwarp();
   };
+  // The tile's mask, before its K is fetched: the softmax reads it once S is there, and all of a warp's lanes have to
+  // read the same.
+  auto note_tile = [&](int t, uint32_t pages) {
+    const bool whole = key0 + (t + 1) * kBN <= key1 && (!paged || pages == (uint32_t)((1ull << (kBN >> p.page_shift)) - 1ull));
+    uint32_t mine = 0xffffffffu;  // lane's word
+    if (!whole) {
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const uint32_t m = __ballot_sync(0xffffffffu, key_there(t, 32 * u + lane, pages));
+        if (lane == u) mine = m;
+      }
+    }
+    if (lane < 4) bars->mask[t % kMasks][lane] = mine;
+    __syncwarp();
+  };
   uint32_t idx = 0, there = 0;
   if (warp >= 12) {
     // the first K tile goes out before the CTA has met (by cp.async: its arrival after)
@@ -340,6 +355,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int page = tile_page(0);
         there = tile_pages(0, page);
         __syncwarp();
+        note_tile(0, there);
         fetch_tile(&maps.k_pool, &maps.k_prefix, sbase + C::kOffK, 0, page, there, &bars->kfull[0]);
       }
     } else {
@@ -504,18 +520,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (kph > 0) ok = cwait_warp(&bars->kfree[ks], (uint32_t)((kph - 1) & 1), bars, p, 1);
             if (!ok) break;
           }
-          uint32_t mine = 0u;  // lane's word of the mask
-          if (key0 + (t + 1) * kBN <= key1 && (!paged || there == every)) {
-            mine = 0xffffffffu;
-          } else {
-#pragma unroll
-            for (int u = 0; u < 4; ++u) {
-              const uint32_t m = __ballot_sync(0xffffffffu, key_there(t, 32 * u + lane, there));
-              if (lane == u) mine = m;
-            }
-          }
-          if (lane < 4) bars->mask[t % kMasks][lane] = mine;
-          __syncwarp();
+          if (t > 0) note_tile(t, there);
           if (t > 0) fetch_tile(&maps.k_pool, &maps.k_prefix, sbase + C::kOffK + (uint32_t)ks * C::kTileBytes, t, page, there, &bars->kfull[ks]);
           page = tile_page(t + 1);
           issued = t + 1;
@@ -823,6 +828,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(H ? &bars->phi[g] : &bars->plo[g]);
+        __syncwarp();
         if (H == 0) load(kLoGroups, std::integral_constant<int, 4 - kLoGroups>{});
 #pragma unroll
         for (int u = 0; u < 4; ++u) acc[u] = fadd2(acc[u], sum[u]);
@@ -843,7 +849,9 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       fence_after();
       const uint4 mk = lds128(smem_u32(bars->mask[t % kMasks]));
-      ok = t < n_full && (mk.x & mk.y & mk.z & mk.w) == 0xffffffffu ? tile(t, std::false_type{}) : tile(t, std::true_type{});
+      // (one decision for the warp: what follows is full of warp-wide instructions)
+      const bool plain = __all_sync(0xffffffffu, t < n_full && (mk.x & mk.y & mk.z & mk.w) == 0xffffffffu) != 0;
+      ok = plain ? tile(t, std::false_type{}) : tile(t, std::true_type{});
     }
     const volatile ChunkItem& itv = bars->item;
     const int mine = SPLIT ? (n_tiles + 1 - g) >> 1 : n_tiles;  // tiles of this slot

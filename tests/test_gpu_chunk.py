@@ -581,3 +581,23 @@ def test_the_example_runs():
     from paper_2607_02963_gb300 import speculative
     kept, cache = speculative.example(events=3, drafts=3, steps=3, prefix=200, vocab=500, h_q=8, h_kv=2)
     assert np.array_equal(cache.event_len, np.sum(kept, axis=0)) and all(1 <= k <= 4 for row in kept for k in row)
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+def test_many_launches_in_a_row_agree(fp8):
+    """Calls queued back to back, two batches in turn: every pass gives what the first one gave."""
+    cases = [Case(40 + i, [30, 200, 3], [5, 40, 1], [400 + 37 * i], [0, 0, 0], 28, 4, 128, 16, fp8).store().device() for i in range(2)]
+    plans = [c.plan(out_dtype=1) for c in cases]
+    first = [c.attend(p) for c, p in zip(cases, plans)]
+    q = [c.q.cuda() for c in cases]
+    pre = [(c.k_pre.cuda(), c.v_pre.cuda()) for c in cases]
+    outs = [[torch.full_like(o, 7.0) for o in f] for f in first]
+    differ = torch.zeros(2, dtype=torch.int64, device="cuda")
+    for i in range(600):
+        b = i % 2
+        B.pad_chunk_attn(plans[b], q[b], *pre[b], *cases[b].dp, *outs[b], *cases[b].ds)
+        if i % 50 >= 48:
+            differ[b] += (outs[b][0] != first[b][0]).sum() + (outs[b][1] != first[b][1]).sum()
+    assert differ.tolist() == [0, 0]
+    for p in plans:
+        B.pad_chunk_status(p)
