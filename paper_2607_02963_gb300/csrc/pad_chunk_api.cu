@@ -161,10 +161,15 @@ double makespan(std::vector<std::pair<double, int64_t>>& ctas, int sms) {
 }
 
 // The tcgen05 kernel: both of its forms and the length of the key ranges (in tiles) are costed with what was
-// measured on GB300 (us): a CTA's start and end, a tile of each form, the partial states' way out and in
-// again.
-constexpr double kTcCta = 7.0, kPairTile = 1.48, kSplitTile = 0.95, kPartialRate = 4e6;  // bytes per us
-void cut_tc(std::vector<Segment>& segs, const pad_problem& prob, int sms, bool& split) {
+// measured on GB300 (us; 152 CTAs at work, from 4096 and 12288 keys, pages of 16): a CTA's start and end, a tile
+// of each form by head_dim and by where its keys are, the partial states' way out and in again.
+// With one form for everything (us): 129 tokens over 32768, 28/4 heads, two slots 81.5, one slot 75;
+// 2048 tokens over 30720 in pages, 640 and 800; 8-bit chunks of head_dim 64, 177 and 280.
+constexpr double kTcCta = 7.0, kPartialRate = 4e6;  // bytes per us
+constexpr double kTile[2][2][3] = {  // [one slot per CTA][head_dim 64][prefix, bf16 pages, 8-bit pages]
+    {{1.49, 1.53, 2.55}, {1.30, 1.22, 1.60}},
+    {{0.69, 1.01, 2.17}, {0.61, 0.78, 1.38}}};
+void cut_tc(std::vector<Segment>& segs, const pad_problem& prob, bool fp8, int sms, bool& split) {
   const int tps = 128 / (prob.h_q / prob.h_kv);
   auto tiles_of = [](const Segment& s) { return ((int64_t)s.keys + 127) / 128; };
   int64_t longest = 0;
@@ -180,7 +185,7 @@ void cut_tc(std::vector<Segment>& segs, const pad_problem& prob, int sms, bool& 
   std::vector<std::pair<double, int64_t>> ctas;
   for (int form = 0; form < 2; ++form) {
     const int tpc = form ? tps : 2 * tps;
-    const double tile = form ? kSplitTile : kPairTile;
+    const double* tile = kTile[form][prob.head_dim == 64];
     // (ranges much shorter than an SM's share of the work only add starts)
     const int64_t least = std::max<int64_t>(1, (int64_t)(total / sms / 12));
     for (int64_t len = longest;;) {
@@ -189,7 +194,7 @@ void cut_tc(std::vector<Segment>& segs, const pad_problem& prob, int sms, bool& 
       for (const Segment& s : segs) {
         if (!s.tc) continue;
         const int64_t tiles = tiles_of(s), n = (tiles + len - 1) / len, each = (tiles + n - 1) / n;
-        ctas.push_back({kTcCta + tile * (double)each, (int64_t)((s.ntok + tpc - 1) / tpc) * prob.h_kv * n});
+        ctas.push_back({kTcCta + tile[s.paged + (fp8 && s.paged)] * (double)each, (int64_t)((s.ntok + tpc - 1) / tpc) * prob.h_kv * n});
         if (n > 1 || !s.paged) bytes += 2.0 * (double)n * s.ntok * prob.h_q * (prob.head_dim + 2) * 4;
       }
       const double t = makespan(ctas, sms) + bytes / kPartialRate;
@@ -271,7 +276,7 @@ void build(const Batch& b, const int64_t* prefix_offset, Lists& L) {
     if (prob.flags & (PAD_FLAG_PREFIX_MMA | PAD_FLAG_PREFIX_TC)) s.tc = (prob.flags & PAD_FLAG_PREFIX_TC) != 0;
     else s.tc = !s.paged || (int64_t)s.ntok * G > kMmaRows;
   }
-  cut_tc(segs, prob, sms, L.tc_split);
+  cut_tc(segs, prob, b.kv_format == PAD_KV_FP8, sms, L.tc_split);
   cut_mma(segs, 0, prob, sms, L.pre_rows16);
   cut_mma(segs, 1, prob, sms, L.page_rows16);
   for (const Segment& s : segs) {

@@ -16,10 +16,14 @@
 // power of two to below 2^15 (exact down to 2^-29 of their largest value), weights go in as p 2^(k - r + 15)
 // with r the largest V scale so far; where a block's scales lie more than 2^12 below that, they go in as
 // bf16, whose range is fp32's, and so do the codes.
-// (Widened to bf16 throughout, four to five integer instructions a pair: 129 us for 295k cached tokens, 28/4 heads,
+// (Widened to bf16 throughout, four to five integer instructions a pair: 129 us for 333k cached tokens, 28/4 heads,
 // no faster than the bf16 cache.)
 //
-// P goes into P.V rounded to bf16 (2^-8 of each weight at most, as in every kernel of this library); the row sum is that of the unrounded fp32 weights, and all states are fp32.
+// P goes into P.V rounded to bf16 (2^-8 of each weight at most, as in every kernel of this library); the row sum
+// is that of the unrounded fp32 weights, and all states are fp32.
+//
+// 16 sequences x 1 token over 333k cached tokens, 28/4 heads: bf16 120 us, 5.6 TB/s, bound by memory; 8 bits 90 us,
+// 3.8 TB/s, bound by the instructions that widen the codes and their latency.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <algorithm>
@@ -53,7 +57,7 @@ struct Ring {
   static constexpr int kScale = 2 * kBlk * kPitch;        // scale bytes: of K, then of V
   static constexpr int kMask = kScale + 2 * kBlk;         // which keys are there
   static constexpr int kStage = kMask + 16;
-  // (three CTAs per SM at 16 rows, two at 32: 16 sequences x 1 token over 295k cached tokens, 28/4 heads, take 106 us
+  // (three CTAs per SM at 16 rows, two at 32: 16 sequences x 1 token over 333k cached tokens, 28/4 heads, take 106 us
   // in 8 bits with two CTAs of three stages, 91 with three of two; bf16 122 and 119)
   static constexpr int kStages = MT == 1 ? 2 : FP8 ? 4 : 3;
   static constexpr int kWarpBytes = kStages * kStage;

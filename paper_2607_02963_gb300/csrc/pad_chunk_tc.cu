@@ -15,8 +15,8 @@
 //                swizzle atom: 16-byte cp.async, 32 rows a warp, arrival left to the hardware, the
 //                issuers fence the proxies.  8 bits: codes by cp.async, each thread widening those it has
 //                copied itself.  (Through registers instead, the fence behind a tile's stores waited for
-//                the next tile's loads: 2300 cycles per K or V tile.  bf16 by cp.async throughout: 838 us for
-//                2048 new tokens over 30720, 28/4 heads; the pages' boxes take 701 us.)
+//                the next tile's loads: 2300 cycles per K or V tile.  bf16 by cp.async throughout:
+//                838 us for 2048 new tokens over 30720, 28/4 heads, where the pages' boxes took 701.)
 //   warp 0       S issuer: S_g(k) = Q_g K(k)^T
 //   warp 1       TMEM allocation (512 columns) and deallocation, P.V issuer: O_g += P_g(k) V(k), P read
 //                back from TMEM, 96 keys and then the last 32
@@ -29,6 +29,11 @@
 // are; a hidden V value would meet a weight of 0, which is not enough for a NaN, so in the tiles that some
 // row does not see in full the values past the first row's last key are looked at, and those that are not
 // finite are left out of P.V and added to the rows that see them at the end.
+//
+// Bound by the chain S -> softmax -> P.V of a slot where the other slot's MMAs do not cover it; in 8 bits by
+// the shared memory's bandwidth (per tile of 128 keys: operands of the MMAs 2048 cycles, codes in and out
+// 512, their widened form 512).  2048 new tokens over 30720, 28/4 heads, bf16: 607 to 670 us, 1390 to 1535
+// TFLOP/s; 6 chunks of 130 to 1501 tokens over up to 7001, 14/2 heads, head_dim 64, 8 bits: 178 us, 620 TFLOP/s.
 //
 // Every wait is bounded (about one second); one that runs out records PAD_ERR_DEVICE_TIMEOUT, raises
 // a CTA-wide flag, lets what was started drain, frees TMEM and returns.
@@ -710,7 +715,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         for (int i = 0; i < NI; ++i) {
           const int row = i * RPI + r0, r = 32 * w + row;
           const uint32_t ml = __shfl_sync(0xffffffffu, mult, row);
-          const uint32_t in[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+          const int flip = D == 128 ? c >> 2 : 0;
+          const uint32_t in[4] = {flip ? x[i].z : x[i].x, flip ? x[i].w : x[i].y, flip ? x[i].x : x[i].z, flip ? x[i].y : x[i].w};
           uint4 o[2];
 #pragma unroll
           for (int u = 0; u < 2; ++u) {
@@ -721,12 +727,10 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
           // chunks 2 c and 2 c + 1 of the row: the upper half of the row's lanes writes them in the other
           // order, so that one store's lanes touch distinct banks (the two boxes lie on the same ones)
-          const int flip = D == 128 ? c >> 2 : 0;
 #pragma unroll
           for (int u = 0; u < 2; ++u) {
             const int ch = 2 * c + (u ^ flip);
-            *reinterpret_cast<uint4*>(smem + tile + (ch >> 3) * C::kBoxBytes + r * 128 + (((ch & 7) ^ (r & 7)) << 4)) =
-                flip ? o[u ^ 1] : o[u];
+            *reinterpret_cast<uint4*>(smem + tile + (ch >> 3) * C::kBoxBytes + r * 128 + (((ch & 7) ^ (r & 7)) << 4)) = o[u];
           }
         }
         proxy_fence();
