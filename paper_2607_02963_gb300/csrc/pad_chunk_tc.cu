@@ -30,10 +30,11 @@
 // row does not see in full the values past the first row's last key are looked at, and those that are not
 // finite are left out of P.V and added to the rows that see them at the end.
 //
-// Bound by the chain S -> softmax -> P.V of a slot where the other slot's MMAs do not cover it; in 8 bits by
-// the shared memory's bandwidth (per tile of 128 keys: operands of the MMAs 2048 cycles, codes in and out
-// 512, their widened form 512).  2048 new tokens over 30720, 28/4 heads, bf16: 607 to 670 us, 1390 to 1535
-// TFLOP/s; 6 chunks of 130 to 1501 tokens over up to 7001, 14/2 heads, head_dim 64, 8 bits: 178 us, 620 TFLOP/s.
+// Bound by the chain S -> softmax -> P.V of a slot where the other slot's MMAs do not cover it; over pages one
+// slot alone by the boxes of a tile, in 8 bits by the warps that widen (one per scheduler: 1.1 us per K or V
+// tile at head_dim 128, 0.7 at 64).  2048 new tokens over 30720, 28/4 heads, bf16: 640 to 673 us, 1385 to
+// 1456 TFLOP/s; 129 over a prefix of 32768: 74 us; 6 chunks of 130 to 1501 tokens over up to 7001, 14/2 heads,
+// head_dim 64, 8 bits: 178 us, 620 TFLOP/s.
 //
 // Every wait is bounded (about one second); one that runs out records PAD_ERR_DEVICE_TIMEOUT, raises
 // a CTA-wide flag, lets what was started drain, frees TMEM and returns.

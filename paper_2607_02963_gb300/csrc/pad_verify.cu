@@ -11,8 +11,8 @@
 // Bound by bytes: one row of p and one of q per event.  A cluster of eight CTAs takes an event; each sums
 // an eighth of the rows, warp by warp over consecutive entries, hands its sum to the others through
 // distributed shared memory, and the CTA that holds the point goes through the one warp's part it lies
-// in again (a 128th of the row, from L2).  32 branches, vocabulary 150001, fp32: 12 us, 3.2 TB/s, of which some
-// five are the chain ahead of the row's loads (work entry, draft, its probabilities) and the clusters' meetings.
+// in again (a 128th of the row, from L2).  32 branches, vocabulary 150001, fp32: 12 us, 3.2 TB/s; one branch,
+// vocabulary 32768: 7 us, which is the launch and the chain ahead of the row's loads (work entry, draft, its probabilities).
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
 #include <algorithm>
