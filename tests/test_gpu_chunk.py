@@ -601,3 +601,49 @@ def test_many_launches_in_a_row_agree(fp8):
     assert differ.tolist() == [0, 0]
     for p in plans:
         B.pad_chunk_status(p)
+
+
+@pytest.mark.parametrize("sms", [1, 0])
+@pytest.mark.parametrize("fp8", [False, True])
+@pytest.mark.parametrize("d,h_q,h_kv,page", [(128, 28, 4, 16), (64, 14, 2, 64), (128, 16, 1, 4), (64, 6, 2, 8)])
+@pytest.mark.parametrize("what", [0.0, float("nan"), float("inf")])
+def test_both_forms_of_the_tcgen05_kernel(what, d, h_q, h_kv, page, fp8, sms):
+    # planned for one SM, where fewer CTAs are better, two slots of tokens share a CTA
+    lens, news, prefix, video = [700, 2, 0, 129], [70, 150, 0, 43], [301, 5], [0, 0, 1, 1]
+    c = Case(31 + d + page, lens, news, prefix, video, h_q, h_kv, d, page, fp8)
+    at = 2 + 120  # a private token of branch 1 that its first 120 new tokens do not see
+    if what != 0.0:
+        c.v[1][at, 0, 3] = what
+    c.store().device()
+    prob = B.make_problem(h_q, h_kv, d, page, num_sms=sms, flags=B.FLAG_PREFIX_TC)
+    fmt = B.KV_FP8 if fp8 else B.KV_BF16
+    c.ws = torch.zeros(B.pad_chunk_workspace_size(prob, prefix, video, lens, news, kv_format=fmt), dtype=torch.uint8, device="cuda")
+    plan = B.pad_chunk_plan(prob, None, prefix, video, lens, news, page_table=c.dt, n_pages=c.n_pages, kv_format=fmt, workspace=c.ws)
+    if sms == 1:
+        per = 2 * (128 // (h_q // h_kv))
+        assert plan.info()["tc_items"] == sum(-(-n // per) for n in (70, 150, 43, 70 + 150, 43))
+    out, lse = c.attend(plan)
+    B.pad_chunk_status(plan)
+    if what != 0.0:
+        rows, group = slice(70 + 120, 70 + 150), h_q // h_kv
+        bad = out[rows, :group].float() if fp8 else out[rows, :group, 3].float()
+        assert not torch.isfinite(bad).any()
+        keep = torch.ones_like(out, dtype=torch.bool)
+        if fp8:
+            keep[rows, :group] = False  # (a group that holds it reads back as NaN throughout)
+        else:
+            keep[rows, :group, 3] = False
+        assert torch.isfinite(out[keep]).all()
+        c.v[1][at, 0, 3] = 0.0
+        if fp8:
+            return
+        o = out.clone()
+        o[~keep] = 0.0
+        for e in (0, 1, 3):
+            a, want, l, mag = c.want(e)
+            n = news[e]
+            k = keep[a:a + n].cpu().numpy()
+            assert np.all((np.abs(o[a:a + n].double().cpu().numpy() - want) <= (2.0 ** -8 + 1e-4) * mag) | ~k)
+            assert np.all(np.abs(lse[a:a + n].double().cpu().numpy() - l) <= 1e-4)
+        return
+    c.check(out, lse)
