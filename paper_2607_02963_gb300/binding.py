@@ -450,7 +450,11 @@ def _rows(t, name, shape, dtype):
         if n != 1 and st != want:
             raise ValueError(f"{name}: the rows of tensors passed to libpad must be contiguous")
         want *= n
-    return t.data_ptr(), (int(t.stride(0)) if t.shape[0] > 1 else 0)
+    if t.shape[0] <= 1:
+        return t.data_ptr(), 0
+    if t.stride(0) < want:  # (a broadcast one's is 0, which the library takes for packed rows)
+        raise ValueError(f"{name}: the rows of tensors passed to libpad must not overlap (row stride {t.stride(0)}, {want} elements)")
+    return t.data_ptr(), int(t.stride(0))
 
 
 class ChunkPlan:

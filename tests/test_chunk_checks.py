@@ -1,0 +1,82 @@
+"""What the binding of the multi-token step refuses before anything is launched.  No GPU: plans without a workspace,
+which the library itself does not launch, and tensors that only claim to be on one."""
+import pytest
+import torch
+
+from paper_2607_02963_gb300 import binding as B
+
+
+class OnGpu(torch.Tensor):
+    """A host tensor that passes for one in device memory."""
+    is_cuda = True
+
+
+def _zeros(*shape, dtype=torch.bfloat16):
+    return torch.zeros(*shape, dtype=dtype).as_subclass(OnGpu)
+
+
+def _plan(news=(3, 2), lens=(5, 0), **kw):
+    prob = B.make_problem(8, 2, 64, 16, num_sms=152)
+    table = torch.full((len(news), 4), -1, dtype=torch.int32)
+    return B.pad_chunk_plan(prob, None, kw.pop("prefix_len", None), kw.pop("event_video", None), lens, news, page_table=table,
+                            n_pages=9, **kw)
+
+
+def _pools():
+    return _zeros(9, 2, 16, 64), _zeros(9, 2, 16, 64)
+
+
+def _attn(plan, q=None, k_prefix=None, v_prefix=None, pools=None, out=None, **kw):
+    n = plan.n_tokens
+    B.pad_chunk_attn(plan, _zeros(n, 8, 64) if q is None else q, k_prefix, v_prefix, *(pools or _pools()),
+                     _zeros(n, 8, 64, dtype=torch.float32) if out is None else out, stream=0, **kw)
+
+
+def _verify(plan, p=None, q=None, **kw):
+    a = dict(draft=_zeros(plan.n_drafts, dtype=torch.int32), u_accept=_zeros(plan.n_drafts, dtype=torch.float32),
+             u_pick=_zeros(plan.n_events, dtype=torch.float32), accepted=_zeros(plan.n_events, dtype=torch.int32),
+             token=_zeros(plan.n_events, dtype=torch.int32)) | kw
+    B.pad_draft_verify(plan, _zeros(plan.n_tokens, 50, dtype=torch.float32) if p is None else p,
+                       _zeros(plan.n_drafts, 50, dtype=torch.float32) if q is None else q, stream=0, **a)
+
+
+def test_what_passes_reaches_the_library(padlib):
+    """The checks' other side: the same calls with nothing wrong end in the library's own refusal of a host-only plan."""
+    plan = _plan()
+    for call in (lambda: _attn(plan), lambda: _verify(plan)):
+        with pytest.raises(B.PadError, match="host-only"):
+            call()
+
+
+@pytest.mark.parametrize("rows", [1, 2])
+def test_rows_that_overlap_are_refused(padlib, rows):
+    """A broadcast tensor has a row stride of 0, which stands for packed rows in the library: n rows would be read
+    from the memory of one."""
+    plan = _plan()
+    n, nd = plan.n_tokens, plan.n_drafts
+
+    def lap(*shape, dtype=torch.bfloat16):
+        """Rows that start 0 elements apart, or one."""
+        wide = _zeros(4 * shape[0] * max(shape), *shape[1:], dtype=dtype)
+        return wide.as_strided(shape, (rows - 1,) + wide.stride()[1:])
+
+    with pytest.raises(ValueError, match="q: .*overlap"):
+        _attn(plan, q=lap(n, 8, 64))
+    x = _zeros(n, 2, 64)
+    with pytest.raises(ValueError, match="k_new: .*overlap"):
+        B.pad_chunk_append(plan, lap(n, 2, 64), x, *_pools(), stream=0)
+    with pytest.raises(ValueError, match="v_new: .*overlap"):
+        B.pad_chunk_append(plan, x, lap(n, 2, 64), *_pools(), stream=0)
+    for dtype in (torch.float32, torch.bfloat16):
+        with pytest.raises(ValueError, match="p: .*overlap"):
+            _verify(plan, p=lap(n, 50, dtype=dtype), q=_zeros(nd, 50, dtype=dtype))
+        with pytest.raises(ValueError, match="q: .*overlap"):
+            _verify(plan, p=_zeros(n, 50, dtype=dtype), q=lap(nd, 50, dtype=dtype))
+
+
+def test_one_row_may_be_broadcast(padlib):
+    """A single row has no next one."""
+    plan = _plan(news=(1,), lens=(5,))
+    q = _zeros(1, 8, 64)
+    with pytest.raises(B.PadError, match="host-only"):
+        _attn(plan, q=q.expand(1, 8, 64).as_strided((1, 8, 64), (0, 64, 1)))
