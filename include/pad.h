@@ -564,6 +564,7 @@ typedef struct {
   int32_t page_splits;     /* most key ranges that a branch's own tokens are split into */
   int32_t tc_items;        /* work items of the tcgen05 kernel, */
   int32_t mma_items;       /* and of the warp-level kernel (times h_kv CTAs each) */
+  int32_t prefix_tokens;   /* tokens that k_prefix and v_prefix hold at least: up to the last one that is read */
 } pad_chunk_info;
 pad_status pad_chunk_get_info(const pad_chunk_t* chunk, pad_chunk_info* info);
 /* The pages taken: for i < n_new_pages, page[i] became column column[i] of event[i]'s row of the
@@ -584,7 +585,8 @@ pad_status pad_chunk_read(const pad_chunk_t* chunk, const void* k_pool, const vo
                           const uint8_t* v_scale, void* k_out, void* v_out, pad_stream_t stream);
 
 /* Attention of the new tokens; their K/V are read from the pools (pad_chunk_append first).
- * k_prefix / v_prefix may be NULL when no video has a prefix; lse may be NULL.  q_stride: elements
+ * k_prefix / v_prefix [prefix_tokens at least, h_kv, head_dim] (pad_chunk_info) may be NULL when no video has a
+ * prefix; lse may be NULL.  q_stride: elements
  * from one token of q to the next, a multiple of 8, 0 = h_q * head_dim.  A page id outside the pool
  * hides its tokens and is recorded; a row that then sees nothing gets 0 and an lse of -infinity.  What
  * lies in cache slots past a branch's last token is never used in arithmetic. */

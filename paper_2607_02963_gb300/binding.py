@@ -58,7 +58,7 @@ class PlanInfo(ctypes.Structure):
 class ChunkInfo(ctypes.Structure):
     _fields_ = [("n_tokens", c_int64), ("n_cached", c_int64), ("n_drafts", c_int64), ("workspace_bytes", c_int64),
                 ("partial_rows", c_int64), ("n_new_pages", c_int32), ("prefix_splits", c_int32),
-                ("page_splits", c_int32), ("tc_items", c_int32), ("mma_items", c_int32)]
+                ("page_splits", c_int32), ("tc_items", c_int32), ("mma_items", c_int32), ("prefix_tokens", c_int32)]
 
 
 _I32P = POINTER(c_int32)
@@ -469,6 +469,7 @@ class ChunkPlan:
         self._keep = keep  # device memory that the plan points to
         i = self.info()
         self.n_tokens, self.n_cached, self.n_drafts = i["n_tokens"], i["n_cached"], i["n_drafts"]
+        self._prefix_tokens = i["prefix_tokens"]
         # what every call's tensors are checked against
         import torch
         hq, hk, d = problem.h_q, problem.h_kv, problem.head_dim
@@ -633,6 +634,8 @@ def pad_chunk_attn(plan: ChunkPlan, q, k_prefix, v_prefix, k_pool, v_pool, out, 
     kp, vp, ksc, vsc = plan._pools(k_pool, v_pool, k_scale, v_scale)
     kx, vx = None, None
     if k_prefix is not None:
+        if k_prefix.shape[0] < plan._prefix_tokens:
+            raise ValueError(f"k_prefix: {k_prefix.shape[0]} tokens, the plan reads {plan._prefix_tokens}")
         kx = _dev(k_prefix, "k_prefix", (k_prefix.shape[0],) + plan._new_shape[1:], plan._bf16)
         vx = _dev(v_prefix, "v_prefix", k_prefix.shape, plan._bf16)
     st = (_lib or lib()).pad_chunk_attn(plan._h, qp, qs, kx, vx, kp, vp, ksc, vsc, out.data_ptr(), lp,

@@ -10,6 +10,8 @@
 
 #include "pad_chunk.h"
 
+static_assert(sizeof(pad_chunk_info) == 64, "prefix_tokens takes what was padding: the struct keeps its size");
+
 using namespace pad;
 
 namespace {
@@ -541,6 +543,7 @@ pad_status pad_chunk_get_info(const pad_chunk_t* c, pad_chunk_info* info) {
   info->page_splits = c->L.page_splits;
   info->tc_items = (int32_t)c->L.tc.size();
   info->mma_items = (int32_t)(c->L.pre.size() + c->L.page.size());
+  info->prefix_tokens = (int32_t)c->L.prefix_tokens;
   return PAD_OK;
 }
 

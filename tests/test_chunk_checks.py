@@ -80,3 +80,25 @@ def test_one_row_may_be_broadcast(padlib):
     q = _zeros(1, 8, 64)
     with pytest.raises(B.PadError, match="host-only"):
         _attn(plan, q=q.expand(1, 8, 64).as_strided((1, 8, 64), (0, 64, 1)))
+
+
+def test_a_prefix_shorter_than_the_plans_is_refused(padlib):
+    """The kernels read k_prefix as far as the plan's last prefix token, whatever the tensor holds."""
+    def pre(n):
+        return _zeros(n, 2, 64)
+
+    for kw, need in ((dict(prefix_len=[40], event_video=[0, 0]), 40), (dict(prefix_len=[40, 7], event_video=[0, 1]), 47),
+                     (dict(prefix_len=[40, 7], event_video=[0, 1], prefix_offset=[100, 3]), 140),
+                     # a video whose branches bring no token is not read
+                     (dict(prefix_len=[40, 7], event_video=[0, 1], news=(3, 0)), 40),
+                     (dict(prefix_len=[0, 0], event_video=[0, 1]), 0)):
+        plan = _plan(**kw)
+        assert plan.info()["prefix_tokens"] == need
+        for n in (need, need + 5):
+            with pytest.raises(B.PadError, match="host-only"):
+                _attn(plan, k_prefix=pre(n), v_prefix=pre(n))
+        for n in {0, need - 1} - {-1, need}:
+            with pytest.raises(ValueError, match=f"k_prefix: {n} tokens, the plan reads {need}"):
+                _attn(plan, k_prefix=pre(n), v_prefix=pre(n))
+            with pytest.raises(ValueError, match="v_prefix"):
+                _attn(plan, k_prefix=pre(need), v_prefix=pre(n))
