@@ -428,6 +428,11 @@ def pad_device_status(plan: Plan, stream=None):
     _check(lib().pad_device_status(plan.handle, _stream(stream)))
 
 
+def _on_gpu(t, name):
+    if not t.is_cuda and not t.is_pinned():
+        raise ValueError(f"{name}: tensors passed to libpad must be in device memory (or page-locked)")
+
+
 def _dev(t, name, shape, dtype):
     """Device address of a contiguous tensor of this shape and type (None -> NULL)."""
     if t is None:
@@ -436,6 +441,7 @@ def _dev(t, name, shape, dtype):
         raise ValueError(f"{name}: {tuple(t.shape)} {t.dtype}, expected {tuple(shape)} {dtype}")
     if not t.is_contiguous():
         raise ValueError(f"{name}: tensors passed to libpad must be contiguous")
+    _on_gpu(t, name)
     return t.data_ptr()
 
 
@@ -443,6 +449,7 @@ def _rows(t, name, shape, dtype):
     """Device address and row stride (elements; 0 = packed) of a tensor whose rows are contiguous."""
     if t.shape != shape or t.dtype is not dtype:
         raise ValueError(f"{name}: {tuple(t.shape)} {t.dtype}, expected {tuple(shape)} {dtype}")
+    _on_gpu(t, name)
     if t.is_contiguous():
         return t.data_ptr(), 0
     want = 1
@@ -512,13 +519,13 @@ class ChunkPlan:
     def _pools(self, k_pool, v_pool, k_scale, v_scale):
         ps, pt = self._pool_shape, self._pool_type
         if (k_pool.shape == ps and v_pool.shape == ps and k_pool.dtype is pt and v_pool.dtype is pt
-                and k_pool.is_contiguous() and v_pool.is_contiguous()):
+                and k_pool.is_contiguous() and k_pool.is_cuda and v_pool.is_contiguous() and v_pool.is_cuda):
             if k_scale is None and v_scale is None:
                 return k_pool.data_ptr(), v_pool.data_ptr(), None, None
             ss, u8 = self._scale_shape, self._u8
             if (k_scale is not None and v_scale is not None and k_scale.shape == ss and v_scale.shape == ss
-                    and k_scale.dtype is u8 and v_scale.dtype is u8 and k_scale.is_contiguous()
-                    and v_scale.is_contiguous()):
+                    and k_scale.dtype is u8 and v_scale.dtype is u8 and k_scale.is_contiguous() and k_scale.is_cuda
+                    and v_scale.is_contiguous() and v_scale.is_cuda):
                 return k_pool.data_ptr(), v_pool.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr()
         return (_dev(k_pool, "k_pool", ps, pt), _dev(v_pool, "v_pool", ps, pt),
                 _dev(k_scale, "k_scale", self._scale_shape, self._u8), _dev(v_scale, "v_scale", self._scale_shape, self._u8))
@@ -572,6 +579,10 @@ def pad_chunk_plan(problem: Problem, cache, prefix_len, event_video, event_len, 
         max_pages = int(page_table.shape[1])
     if cache is not None and n_pages == 0:
         n_pages = cache.n_pages
+    if workspace is not None:
+        _on_gpu(workspace, "workspace")
+        if page_table is not None:
+            _on_gpu(page_table, "page_table")
     ws_bytes = int(workspace.numel() * workspace.element_size()) if workspace is not None else 0
     strm = _stream(stream) if workspace is not None else c_void_p(0)
     h = c_void_p()
@@ -589,7 +600,7 @@ def pad_chunk_append(plan: ChunkPlan, k_new, v_new, k_pool, v_pool, k_scale=None
     """Write the new tokens' K/V into the branches' pages (quantised in an 8-bit cache)."""
     shape, bf16 = plan._new_shape, plan._bf16
     if (k_new.shape == shape and v_new.shape == shape and k_new.dtype is bf16 and v_new.dtype is bf16
-            and k_new.is_contiguous() and v_new.is_contiguous()):
+            and k_new.is_contiguous() and k_new.is_cuda and v_new.is_contiguous() and v_new.is_cuda):
         kn, vn, ks = k_new.data_ptr(), v_new.data_ptr(), 0
     else:
         kn, ks = _rows(k_new, "k_new", shape, bf16)
@@ -607,7 +618,7 @@ def pad_chunk_read(plan: ChunkPlan, k_pool, v_pool, k_out, v_out, k_scale=None, 
     kp, vp, ksc, vsc = plan._pools(k_pool, v_pool, k_scale, v_scale)
     shape, bf16 = plan._read_shape, plan._bf16
     if not (k_out.shape == shape and v_out.shape == shape and k_out.dtype is bf16 and v_out.dtype is bf16
-            and k_out.is_contiguous() and v_out.is_contiguous()):
+            and k_out.is_contiguous() and k_out.is_cuda and v_out.is_contiguous() and v_out.is_cuda):
         _dev(k_out, "k_out", shape, bf16)
         _dev(v_out, "v_out", shape, bf16)
     st = (_lib or lib()).pad_chunk_read(plan._h, kp, vp, ksc, vsc, k_out.data_ptr(), v_out.data_ptr(), _stream_handle(stream))
@@ -619,16 +630,16 @@ def pad_chunk_attn(plan: ChunkPlan, q, k_prefix, v_prefix, k_pool, v_pool, out, 
                    stream=None):
     """Attention of the step's new tokens over their video's prefix and their branch's cached tokens."""
     shape = plan._q_shape
-    if q.shape == shape and q.dtype is plan._bf16 and q.is_contiguous():
+    if q.shape == shape and q.dtype is plan._bf16 and q.is_contiguous() and q.is_cuda:
         qp, qs = q.data_ptr(), 0
     else:
         qp, qs = _rows(q, "q", shape, plan._bf16)
-    if not (out.shape == shape and out.dtype is plan._out_type and out.is_contiguous()):
+    if not (out.shape == shape and out.dtype is plan._out_type and out.is_contiguous() and out.is_cuda):
         _dev(out, "out", shape, plan._out_type)
     if lse is None:
         lp = None
     else:
-        if not (lse.shape == plan._lse_shape and lse.dtype is plan._f32 and lse.is_contiguous()):
+        if not (lse.shape == plan._lse_shape and lse.dtype is plan._f32 and lse.is_contiguous() and lse.is_cuda):
             _dev(lse, "lse", plan._lse_shape, plan._f32)
         lp = lse.data_ptr()
     kp, vp, ksc, vsc = plan._pools(k_pool, v_pool, k_scale, v_scale)
@@ -651,8 +662,8 @@ def pad_draft_verify(plan: ChunkPlan, p, q, draft, u_accept, u_pick, accepted, t
     kind = plan._bf16 if bf16 else plan._f32
     vocab = p.shape[1]
     p_shape, q_shape, nd, ne = (plan.n_tokens, vocab), (plan.n_drafts, vocab), (plan.n_drafts,), (plan.n_events,)
-    if (p.shape == p_shape and q.shape == q_shape and p.dtype is kind and q.dtype is kind and p.is_contiguous()
-            and q.is_contiguous()):
+    if (p.shape == p_shape and q.shape == q_shape and p.dtype is kind and q.dtype is kind and p.is_contiguous() and p.is_cuda
+            and q.is_contiguous() and q.is_cuda):
         pp, qp, ps, qs = p.data_ptr(), q.data_ptr(), 0, 0
     else:
         pp, ps = _rows(p, "p", p_shape, kind)
@@ -660,8 +671,9 @@ def pad_draft_verify(plan: ChunkPlan, p, q, draft, u_accept, u_pick, accepted, t
     i32, f32 = plan._i32, plan._f32
     if not (draft.shape == nd and u_accept.shape == nd and u_pick.shape == ne and accepted.shape == ne
             and token.shape == ne and draft.dtype is i32 and u_accept.dtype is f32 and u_pick.dtype is f32
-            and accepted.dtype is i32 and token.dtype is i32 and draft.is_contiguous() and u_accept.is_contiguous()
-            and u_pick.is_contiguous() and accepted.is_contiguous() and token.is_contiguous()):
+            and accepted.dtype is i32 and token.dtype is i32 and draft.is_contiguous() and draft.is_cuda
+            and u_accept.is_contiguous() and u_accept.is_cuda and u_pick.is_contiguous() and u_pick.is_cuda
+            and accepted.is_contiguous() and accepted.is_cuda and token.is_contiguous() and token.is_cuda):
         for t, name, shape, dt in ((draft, "draft", nd, i32), (u_accept, "u_accept", nd, f32),
                                    (u_pick, "u_pick", ne, f32), (accepted, "accepted", ne, i32), (token, "token", ne, i32)):
             _dev(t, name, shape, dt)

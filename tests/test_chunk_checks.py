@@ -102,3 +102,45 @@ def test_a_prefix_shorter_than_the_plans_is_refused(padlib):
                 _attn(plan, k_prefix=pre(n), v_prefix=pre(n))
             with pytest.raises(ValueError, match="v_prefix"):
                 _attn(plan, k_prefix=pre(need), v_prefix=pre(n))
+
+
+def test_host_tensors_are_refused(padlib):
+    """A host tensor's address is not for the kernels: every tensor of every call."""
+    plan = _plan(prefix_len=[20], event_video=[0, 0])
+    n, nd, ne, f32, i32 = plan.n_tokens, plan.n_drafts, plan.n_events, torch.float32, torch.int32
+    t = dict(q=_zeros(n, 8, 64), k_prefix=_zeros(20, 2, 64), v_prefix=_zeros(20, 2, 64), k_pool=_pools()[0], v_pool=_pools()[1],
+             out=_zeros(n, 8, 64, dtype=f32), lse=_zeros(n, 8, dtype=f32), k_new=_zeros(n, 2, 64), v_new=_zeros(n, 2, 64),
+             k_out=_zeros(plan.n_cached, 2, 64), v_out=_zeros(plan.n_cached, 2, 64), p=_zeros(n, 50, dtype=f32),
+             dq=_zeros(nd, 50, dtype=f32), draft=_zeros(nd, dtype=i32), u_accept=_zeros(nd, dtype=f32),
+             u_pick=_zeros(ne, dtype=f32), accepted=_zeros(ne, dtype=i32), token=_zeros(ne, dtype=i32))
+    calls = {"attn": (B.pad_chunk_attn, ("q", "k_prefix", "v_prefix", "k_pool", "v_pool", "out", "lse")),
+             "append": (B.pad_chunk_append, ("k_new", "v_new", "k_pool", "v_pool")),
+             "read": (B.pad_chunk_read, ("k_pool", "v_pool", "k_out", "v_out")),
+             "verify": (B.pad_draft_verify, ("p", "dq", "draft", "u_accept", "u_pick", "accepted", "token"))}
+    for call, names in calls.values():
+        with pytest.raises(B.PadError, match="host-only"):
+            call(plan, *(t[x] for x in names), stream=0)
+        for bad in names:
+            host = torch.zeros(t[bad].shape, dtype=t[bad].dtype)
+            with pytest.raises(ValueError, match=f"{'q' if bad == 'dq' else bad}: .*device memory"):
+                call(plan, *(host if x == bad else t[x] for x in names), stream=0)
+    # rows of a wider tensor, and the 8-bit cache's scales
+    wide = torch.zeros(n, 1024, dtype=torch.bfloat16)[:, :512].unflatten(1, (8, 64))
+    with pytest.raises(ValueError, match="q: .*device memory"):
+        _attn(plan, q=wide, k_prefix=t["k_prefix"], v_prefix=t["v_prefix"])
+    plan = _plan(kv_format=B.KV_FP8)
+    pools, u8 = [_zeros(9, 2, 16, 64, dtype=torch.uint8) for _ in range(2)], torch.uint8
+    for bad in range(2):
+        scales = [torch.zeros(9, 2, 16, dtype=u8) if i == bad else _zeros(9, 2, 16, dtype=u8) for i in range(2)]
+        with pytest.raises(ValueError, match="[kv]_scale: .*device memory"):
+            B.pad_chunk_append(plan, t["k_new"], t["v_new"], *pools, *scales, stream=0)
+
+
+def test_host_workspaces_and_page_tables_are_refused(padlib):
+    prob = B.make_problem(8, 2, 64, 16, num_sms=152)
+    size = B.pad_chunk_workspace_size(prob, None, None, [5], [3])
+    ws, table = torch.zeros(size + 256, dtype=torch.uint8), torch.full((1, 4), -1, dtype=torch.int32)
+    with pytest.raises(ValueError, match="workspace: .*device memory"):
+        B.pad_chunk_plan(prob, None, None, None, [5], [3], page_table=table.as_subclass(OnGpu), n_pages=4, workspace=ws, stream=0)
+    with pytest.raises(ValueError, match="page_table: .*device memory"):
+        B.pad_chunk_plan(prob, None, None, None, [5], [3], page_table=table, n_pages=4, workspace=ws.as_subclass(OnGpu), stream=0)
