@@ -12,8 +12,8 @@
 //                128-byte swizzle, warp 12 those of K, warp 13 of V, a lane looking up and fetching one page;
 //                V tiles that some row does not see in full are looked over before they count as loaded
 //                (warps 13-15): slots past the last token hold anything.  Pages of four tokens, which are half a
-//                swizzle atom: 16-byte cp.async, 32 rows a warp, arrival left to the hardware, the
-//                issuers fence the proxies.  8 bits: codes by cp.async, each thread widening those it has
+//                swizzle atom: 16-byte cp.async, 32 rows a warp, arrival left to the hardware (the mask's
+//                word by an arrival of its own), the issuers fence the proxies.  8 bits: codes by cp.async, each thread widening those it has
 //                copied itself.  (Through registers instead, the fence behind a tile's stores waited for
 //                the next tile's loads: 2300 cycles per K or V tile.  bf16 by cp.async throughout:
 //                838 us for 2048 new tokens over 30720, 28/4 heads, where the pages' boxes took 701.)
@@ -91,7 +91,9 @@ struct ChunkMaps {
 };
 
 struct Bars {
-  uint64_t kfull[4], kfree[4];  // (full: one arrival with the bytes; by cp.async one of every loader thread)
+  // (full: one arrival with the bytes; by cp.async one of every loader thread, and for bf16 K tiles one of every warp,
+  // which publishes the tile's mask: the arrivals of copies order no other store)
+  uint64_t kfull[4], kfree[4];
   uint64_t vfull[4], vfree[4];
   uint64_t sfull[2];
   uint64_t plo[2], phi[2];
@@ -232,7 +234,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   const bool bulk = !wide && (!paged || maps.pages);  // tiles by TMA
   if (threadIdx.x == 384) {  // (of the warp that fetches the first tile)
     for (int s = 0; s < 4; ++s) {
-      mbar_init(&bars->kfull[s], bulk ? 1 : 128);
+      mbar_init(&bars->kfull[s], bulk ? 1 : wide ? 128 : 132);
       mbar_init(&bars->kfree[s], 1);
       mbar_init(&bars->vfull[s], bulk ? 1 : 128);
       mbar_init(&bars->vfree[s], 1);
@@ -611,6 +613,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           note(t);
           issue_bf16(k_base, sbase + C::kOffK + (uint32_t)ks * C::kTileBytes, t, idx, there);
         }
+        if (lane == 0) mbar_arrive(&bars->kfull[ks]);  // (lane 0 wrote the mask's word)
         mbar_arrive_copies(&bars->kfull[ks]);
         const uint32_t vt = C::kOffV + (uint32_t)vs * C::kTileBytes;
         if (vph > 0) ok = cwait_warp(&bars->vfree[vs], (uint32_t)((vph - 1) & 1), bars, p, 2);
