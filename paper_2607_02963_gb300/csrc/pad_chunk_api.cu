@@ -70,7 +70,7 @@ pad_status check_batch(const Batch& b) {
     return api_fail(PAD_ERR_INVALID_ARG, "an event array is NULL");
   for (int v = 0; v < b.n_videos; ++v)
     if (b.prefix_len[v] < 0 || b.prefix_len[v] > kMaxLen) return api_fail(PAD_ERR_INVALID_ARG, "prefix_len[%d]=%d", v, b.prefix_len[v]);
-  int64_t tokens = 0, cached = 0;
+  int64_t tokens = 0, spans = 0;  // (a read's grid is one CTA per span)
   for (int e = 0; e < b.n_events; ++e) {
     if (b.event_len[e] < 0 || b.n_new[e] < 0 || (int64_t)b.event_len[e] + b.n_new[e] > kMaxLen)
       return api_fail(PAD_ERR_INVALID_ARG, "event_len[%d]=%d, n_new[%d]=%d", e, b.event_len[e], e, b.n_new[e]);
@@ -80,9 +80,9 @@ pad_status check_batch(const Batch& b) {
         return api_fail(PAD_ERR_INVALID_ARG, "event_video[%d]=%d: non-decreasing within [0, %d)", e, v, b.n_videos);
     }
     tokens += b.n_new[e];
-    cached += (int64_t)b.event_len[e] + b.n_new[e];
+    spans += ((int64_t)b.event_len[e] + b.n_new[e] + chunk_read_tokens() - 1) / chunk_read_tokens();
   }
-  if (tokens > kMaxTokens || cached > (int64_t)64 * INT32_MAX / 2) return api_fail(PAD_ERR_UNSUPPORTED, "too many tokens");
+  if (tokens > kMaxTokens || spans > INT32_MAX) return api_fail(PAD_ERR_UNSUPPORTED, "too many tokens");
   return PAD_OK;
 }
 

@@ -144,3 +144,15 @@ def test_host_workspaces_and_page_tables_are_refused(padlib):
         B.pad_chunk_plan(prob, None, None, None, [5], [3], page_table=table.as_subclass(OnGpu), n_pages=4, workspace=ws, stream=0)
     with pytest.raises(ValueError, match="page_table: .*device memory"):
         B.pad_chunk_plan(prob, None, None, None, [5], [3], page_table=table, n_pages=4, workspace=ws.as_subclass(OnGpu), stream=0)
+
+
+def test_more_cached_tokens_than_a_read_has_ctas_for_are_refused(padlib):
+    """pad_chunk_read copies spans of 32 tokens, a CTA each: 2^31 of them and more are no grid."""
+    prob = B.make_problem(1, 1, 64, 64, num_sms=152)
+    most = [1 << 30] * 63 + [(1 << 30) - 32]           # 2^31 - 1 spans
+    assert B.pad_chunk_plan(prob, None, None, None, most, [0] * 64).n_cached == 2 ** 36 - 32
+    lens = [1 << 30] * 63 + [(1 << 30) - 64] + [1] * 31  # fewer tokens, more spans
+    for call in (lambda: B.pad_chunk_plan(prob, None, None, None, lens, [0] * 95),
+                 lambda: B.pad_chunk_workspace_size(prob, None, None, lens, [0] * 95)):
+        with pytest.raises(B.PadError, match="too many tokens"):
+            call()
