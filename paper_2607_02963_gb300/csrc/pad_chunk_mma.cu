@@ -602,24 +602,26 @@ __global__ void __launch_bounds__(128) chunk_merge_kernel(const __grid_constant_
         const int64_t row = row_of(s);
         const float2 ml = p.part_ml[row];
         const float* src = p.part_o + row * D + V * lane;
-        if constexpr (V == 4) {
-          const float4 t = *reinterpret_cast<const float4*>(src);
-          x[u][0] = t.x, x[u][1] = t.y, x[u][2] = t.z, x[u][3] = t.w;
-        } else {
-          const float2 t = *reinterpret_cast<const float2*>(src);
-          x[u][0] = t.x, x[u][1] = t.y;
-        }
-        if (ml.y != 0.f) {  // (l = 0: nothing was visible there, and its O may not have been written; a NaN passes)
+        // (l = 0: nothing was visible there, and its O may not have been written; a NaN passes.  A weight that
+        // underflows to 0 multiplies all the same: what is not finite in its O stays so.)
+        const bool seen = ml.y != 0.f;
+        if (seen) {
           ws[u] = ex2(ml.x - m_all);
           l += ws[u] * ml.y;
+        }
+        if constexpr (V == 4) {
+          const float4 t = *reinterpret_cast<const float4*>(src);
+          x[u][0] = seen ? t.x : 0.f, x[u][1] = seen ? t.y : 0.f, x[u][2] = seen ? t.z : 0.f, x[u][3] = seen ? t.w : 0.f;
+        } else {
+          const float2 t = *reinterpret_cast<const float2*>(src);
+          x[u][0] = seen ? t.x : 0.f, x[u][1] = seen ? t.y : 0.f;
         }
       }
     }
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
-      for (int v = 0; v < V; ++v)
-        if (ws[u] != 0.f) acc[v] += ws[u] * x[u][v];
+      for (int v = 0; v < V; ++v) acc[v] += ws[u] * x[u][v];
   }
   if constexpr (WARPS > 1) {
 #pragma unroll

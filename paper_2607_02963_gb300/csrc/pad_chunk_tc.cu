@@ -923,7 +923,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           const float a[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
           for (int u = 0; u < 4; ++u)
-            r[4 * j + u] = __float_as_uint(mine > 0 && wgt != 0.f ? fmaf(__uint_as_float(r[4 * j + u]), wgt, a[u]) : a[u]);
+            r[4 * j + u] = __float_as_uint(mine > 0 ? fmaf(__uint_as_float(r[4 * j + u]), wgt, a[u]) : a[u]);
         }
       }
       if (dirty && active && itv.paged) {
