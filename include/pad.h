@@ -580,7 +580,8 @@ pad_status pad_chunk_append(const pad_chunk_t* chunk, const void* k_new, const v
                             void* k_pool, void* v_pool, uint8_t* k_scale, uint8_t* v_scale, pad_stream_t stream);
 
 /* Copy the cached tokens of every event, positions 0 .. event_len + n_new - 1, event after event,
- * into k_out / v_out [n_cached, h_kv, head_dim] bf16 (exact in either format). */
+ * into k_out / v_out [n_cached, h_kv, head_dim] bf16 (exact in either format).  The tokens of a page id outside
+ * the pool come out as zeros, and it is recorded (pad_chunk_status). */
 pad_status pad_chunk_read(const pad_chunk_t* chunk, const void* k_pool, const void* v_pool, const uint8_t* k_scale,
                           const uint8_t* v_scale, void* k_out, void* v_out, pad_stream_t stream);
 

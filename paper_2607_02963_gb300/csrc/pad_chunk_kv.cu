@@ -132,9 +132,11 @@ __global__ void __launch_bounds__(kThreads) chunk_read_kernel(const __grid_const
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int i = i0 + u * kThreads, g = i / L, h = g % p.h_kv, t = g / p.h_kv;
+      to[u] = i < n ? ((mine.out + pos + t) * p.h_kv + h) * D + 8 * c : -1;
+      x[u][0] = x[u][1] = make_uint4(0u, 0u, 0u, 0u);
+      sc[u][0] = sc[u][1] = 0u;
       const int pg = i < n ? pages[t] : -1;
-      to[u] = (unsigned)pg < (unsigned)p.n_pages ? ((mine.out + pos + t) * p.h_kv + h) * D + 8 * c : -1;
-      if (to[u] < 0) continue;
+      if ((unsigned)pg >= (unsigned)p.n_pages) continue;  // (its tokens are zeros)
       const int64_t slot = ((int64_t)pg * p.h_kv + h) * p.page_size + ((pos + t) & (p.page_size - 1));
 #pragma unroll
       for (int kv = 0; kv < 2; ++kv) {
