@@ -499,7 +499,12 @@ pad_status pad_prefill_status(pad_stream_t stream);
  *   pad_chunk_commit  host: the branches' new lengths; pages past them go back.
  * pad_chunk_read copies the branches' cached tokens out as contiguous bf16 (the layout of
  * k_prefix / v_prefix).  All device work is asynchronous on the stream given; calls on
- * another stream than the plan's must be ordered after it by the caller.
+ * another stream than the plan's must be ordered after it by the caller.  The calls after the plan may be
+ * captured into a graph and replayed with other contents in the same buffers.
+ *
+ * What the one-token step has and this one has not: rotary positions (pad_plan_set_rope: q and k_new come rotated
+ * here), and the modes PAD_G_SELF and PAD_BRANCH_CAUSAL.  Its weights go into P.V as one bf16 number each, 2^-8 of
+ * themselves at most off, at head_dim 64 too, where the one-token step's prefix pass keeps them in two parts.
  *
  * Layouts (row-major, bf16 unless stated); N = sum of n_new, tokens packed event by event:
  *   q      [N, h_q, head_dim]   k_new / v_new [N, h_kv, head_dim]   (token strides may be larger)

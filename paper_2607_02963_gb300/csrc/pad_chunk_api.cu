@@ -170,6 +170,10 @@ double makespan(std::vector<std::pair<double, int64_t>>& ctas, int sms) {
 // of each form by head_dim and by where its keys are, the partial states' way out and in again.
 // With one form for everything (us): 129 tokens over 32768, 28/4 heads, two slots 81.5, one slot 75;
 // 2048 tokens over 30720 in pages, 640 and 800; 8-bit chunks of head_dim 64, 177 and 280.
+// The costs are those of pages of 16.  Two slots and one on other pages (us, 1024 tokens over 8192, where two are taken;
+// head_dim 128, 28/4 heads | 64, 14/2 heads): pages of 4, 148 and 177 | 71 and 72; of 8, 130 and 197 | 69 and 86; of 16,
+// 122 and 152 | 71 and 68; of 32, 122 and 132 | 70 and 62; of 64, 120 and 124 | 71 and 58.  In 8 bits the page size makes no
+// difference: 175 and 242 to 246 | 77 and 104.
 constexpr double kTcCta = 7.0, kPartialRate = 4e6;  // bytes per us
 constexpr double kTile[2][2][3] = {  // [one slot per CTA][head_dim 64][prefix, bf16 pages, 8-bit pages]
     {{1.49, 1.53, 2.55}, {1.30, 1.22, 1.60}},

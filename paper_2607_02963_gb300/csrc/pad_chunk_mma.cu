@@ -19,8 +19,9 @@
 // (Widened to bf16 throughout, four to five integer instructions a pair: 129 us for 333k cached tokens, 28/4 heads,
 // no faster than the bf16 cache.)
 //
-// P goes into P.V rounded to bf16 (2^-8 of each weight at most, as in every kernel of this library); the row sum
-// is that of the unrounded fp32 weights, and all states are fp32.
+// P goes into P.V rounded to bf16 (2^-8 of each weight at most; f16, 2^-11, with 8-bit keys, unless their scales lie far
+// apart), at head_dim 64 too, where the one-token step's kernels keep more of it (two bf16 parts, or 32 bits up to 8
+// rows); the row sum is that of the unrounded fp32 weights, and all states are fp32.
 //
 // 16 sequences x 1 token over 333k cached tokens, 28/4 heads: bf16 120 us, 5.6 TB/s, bound by memory; 8 bits 90 us,
 // 3.8 TB/s, bound by the instructions that widen the codes and their latency.

@@ -25,6 +25,9 @@
 //
 // TMEM columns: S_0 at 0, S_1 at 128, O_g at 256 + D g; P_g goes over S_g.
 //
+// P goes into P.V rounded to bf16, one number each at either head_dim (2^-8 of a weight at most); the row sum is that of
+// the unrounded fp32 weights.
+//
 // What is not finite stays with the rows that see it: scores of hidden keys are replaced, whatever they
 // are; a hidden V value would meet a weight of 0, which is not enough for a NaN, so in the tiles that some
 // row does not see in full the values past the first row's last key are looked at, and those that are not
@@ -58,7 +61,7 @@ constexpr int kThreads = 512;
 constexpr int kLoGroups = 3;    // 32-key groups of a tile whose P is released first
 constexpr float kRescaleSum = 256.0f;  // a part of a row whose P sum to more is redone on a new maximum
 constexpr float kNegInf = -__builtin_huge_valf();
-constexpr int kMasks = 8;       // tiles whose key masks are kept (five can be between loader and softmax)
+constexpr int kMasks = 8;       // tiles whose key masks are kept (as many can be between loader and softmax: 8 bits, D 64, one slot)
 
 template <int D, bool FP8>
 struct Cfg {
