@@ -486,14 +486,14 @@ pad_status pad_prefill_status(pad_stream_t stream);
 
 /* ---------------------------------------------------------------------------
  * Steps of several tokens per branch: drafted tokens to be verified, chunks of a prompt, or
- * single tokens over a cache held in 8 bits.  The paper's step (Eq. 3) is the case of one
+ * single tokens over a cache held in 8 or 4 bits.  The paper's step (Eq. 3) is the case of one
  * token per branch; the mask is its own (Sec. 3.4) applied to every chunk token: token t of
  * event e attends to the shared prefix of its video and to its own branch's tokens up to and
  * including itself.  A step is, in stream order,
  *   pad_chunk_plan    host: validate, allocate pages, build the work lists and copy them to
  *                     the workspace; one plan serves every layer of the model;
  *   pad_chunk_append  write the new tokens' K/V into the branches' pages (quantised where the
- *                     cache is held in 8 bits) and the new page-table entries;
+ *                     cache is held in 8 or 4 bits) and the new page-table entries;
  *   pad_chunk_attn    attention of the new tokens;
  *   pad_draft_verify  accept or reject the drafted tokens and draw the next one;
  *   pad_chunk_commit  host: the branches' new lengths; pages past them go back.
@@ -512,6 +512,8 @@ pad_status pad_prefill_status(pad_stream_t stream);
  *   pools  kv_format PAD_KV_BF16: as above, bf16 [n_pages, h_kv, page_size, head_dim]
  *          kv_format PAD_KV_FP8:  codes uint8 [n_pages, h_kv, page_size, head_dim] and scales
  *          uint8 [n_pages, h_kv, page_size], one scale for the head_dim codes of a token and head
+ *          kv_format PAD_KV_FP4:  codes uint8 [n_pages, h_kv, page_size, head_dim / 2], byte i holding value
+ *          2 i in its lower half and value 2 i + 1 in its upper, and scales uint8 [n_pages, h_kv, page_size, head_dim / 16]
  *
  * 8-bit groups: with a = max|x| over the head_dim values, k is the smallest integer with
  * a <= 448 * 2^k, kept in [-120, 7]; a code is x / 2^k in e4m3, rounded to nearest even, values
@@ -520,10 +522,21 @@ pad_status pad_prefill_status(pad_stream_t stream);
  * are 0; the codes 0x7f and 0xff do not occur).  A power
  * of two costs e4m3 no accuracy (its relative spacing is the same everywhere) and makes code
  * times scale exact in bf16: what the attention multiplies is what pad_chunk_read returns.
+ *
+ * 4-bit groups: 16 consecutive values of a token and head.  With a = max|x|, the scale s is a / 6 rounded to nearest even
+ * as an unsigned number of 5 exponent bits (bias 15) and 3 mantissa bits, its byte: 2^(e - 15) (1 + m / 8), below 2^-14
+ * m 2^-17; at most 10240 (byte 226).  A code is x / s in e2m1 (0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives), rounded
+ * to nearest even, saturated (a > 61440).  Byte 255 stands for a group that holds a NaN or an infinity, which reads back
+ * as NaN throughout (its codes are 0); bytes 227 to 254 do not occur.  Code times scale has six significant bits at
+ * most: it is exact in bf16, and attention multiplies it as it is.
+ * In attention over 4-bit pages a weight is off by 2^-11 of itself at most, or by 2^-40 of the largest of its row's piece of
+ * keys where that is more (weights below 2^-29 of it); sequences with many new query rows are widened to bf16 pages in the
+ * workspace first, where the bf16 cache's 2^-8 holds.
  * --------------------------------------------------------------------------- */
 typedef struct pad_chunk_t pad_chunk_t;
 #define PAD_KV_BF16 0
 #define PAD_KV_FP8 1
+#define PAD_KV_FP4 4
 
 /* Bytes of device workspace pad_chunk_plan needs (host arrays, same meaning as there); 0 on
  * invalid arguments.  A caller that keeps one workspace for many steps takes the largest. */
@@ -534,7 +547,7 @@ size_t pad_chunk_workspace_size(const pad_problem* prob, int32_t kv_format, int3
 /* Plan one step.
  *   prob           layer shape; flags: PAD_FLAG_PREFIX_MMA forces the warp-level kernel for
  *                  everything, PAD_FLAG_PREFIX_TC the tcgen05 kernel, other prefix flags are refused
- *   kv_format      PAD_KV_BF16 or PAD_KV_FP8 (the prefix is bf16 either way)
+ *   kv_format      PAD_KV_BF16, PAD_KV_FP8 or PAD_KV_FP4 (the prefix is bf16 in each)
  *   cache          page bookkeeping: every page that the new tokens start is taken from it, the
  *                  lowest-numbered free ones, events in ascending order; NULL: page_table already
  *                  lists the pages of all event_len + n_new tokens

@@ -1,10 +1,12 @@
-"""fp64 definitions of the multi-token step (test infrastructure only, like pad_oracle.py): 8-bit groups,
+"""fp64 definitions of the multi-token step (test infrastructure only, like pad_oracle.py): 8-bit and 4-bit groups,
 attention of chunk tokens, verification of drafted tokens.
 
 An 8-bit group is the head_dim values of one token and kv-head: codes are e4m3 (four exponent bits,
 bias 7, three mantissa bits, largest value 448) of x / 2^k to nearest even, k the smallest integer with
 max|x| <= 448 * 2^k, kept in [-120, 7]; the scale byte is k + 127, 0 for zeros, 255 where a value is not
-finite.  Chunk token t of an event sees its video's prefix and its branch's tokens up to itself
+finite.  A 4-bit group is 16 consecutive values: the scale is max|x| / 6 to nearest even as an unsigned number of five
+exponent bits (bias 15) and three mantissa bits, 10240 at most, codes are e2m1 of x / scale to nearest even, saturated;
+byte 255 and codes of 0 where a value is not finite.  Chunk token t of an event sees its video's prefix and its branch's tokens up to itself
 (Sec. 3.4).  Verification keeps drafted token i while u_i q_i(x_i) < p_i(x_i) and draws the next token
 from integer weights floor(2^38 min(r, 1)).
 """
@@ -55,6 +57,44 @@ def kv8_encode(x: np.ndarray):
 def kv8_decode(codes: np.ndarray, byte: np.ndarray) -> np.ndarray:
     scale = np.where(byte == 255, np.nan, np.where(byte == 0, 0.0, 2.0 ** (np.clip(byte.astype(np.float64), 7, 134) - 127)))
     return e4m3_values()[codes] * scale[..., None]
+
+
+def _nearest(y: np.ndarray, grid: np.ndarray) -> np.ndarray:
+    """Index of the entry of the ascending grid nearest to each y, ties to the even index."""
+    y = np.minimum(y, grid[-1])
+    hi = np.clip(np.searchsorted(grid, y), 0, len(grid) - 1)
+    lo = np.maximum(hi - 1, 0)
+    dh, dl = grid[hi] - y, y - grid[lo]
+    return np.where(dh < dl, hi, np.where(dl < dh, lo, np.where(lo % 2 == 0, lo, hi)))
+
+
+def kv4_scales() -> np.ndarray:
+    """The value of each scale byte up to 226."""
+    b = np.arange(227)
+    return np.where(b < 8, b * 2.0 ** -17, (8 + b % 8) * 2.0 ** (b // 8 - 18.0))
+
+
+_E2M1 = np.array([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0])
+
+
+def kv4_encode(x: np.ndarray):
+    """x [..., d] float64 -> (codes uint8 [..., d / 2], the even value's in the lower half, scale bytes uint8 [..., d / 16])."""
+    g = np.asarray(x, dtype=np.float64).reshape(x.shape[:-1] + (x.shape[-1] // 16, 16))
+    fine = np.all(np.isfinite(g), axis=-1)
+    g = np.where(fine[..., None], g, 0.0)
+    byte = _nearest(np.abs(g).max(-1) / 6.0, kv4_scales())
+    scale = kv4_scales()[byte][..., None]
+    y = np.divide(g, scale, out=np.zeros_like(g), where=scale > 0)
+    code = (_nearest(np.abs(y), _E2M1) + 8 * np.signbit(g)).astype(np.uint8) * fine[..., None]
+    code = code.reshape(x.shape)
+    return (code[..., 0::2] + 16 * code[..., 1::2]).astype(np.uint8), np.where(fine, byte, 255).astype(np.uint8)
+
+
+def kv4_decode(codes: np.ndarray, byte: np.ndarray) -> np.ndarray:
+    c = np.stack([codes & 15, codes >> 4], -1).reshape(byte.shape + (16,))
+    v = np.where(c > 7, -1.0, 1.0) * _E2M1[c & 7]
+    scale = np.where(byte == 255, np.nan, kv4_scales()[np.minimum(byte, 226)])
+    return (v * scale[..., None]).reshape(codes.shape[:-1] + (2 * codes.shape[-1],))
 
 
 def chunk_attention(q, k, v, first_limit: int, scale: float):

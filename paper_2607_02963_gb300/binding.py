@@ -32,6 +32,7 @@ BRANCH_OWN = 0
 BRANCH_CAUSAL = 1
 KV_BF16 = 0
 KV_FP8 = 1
+KV_FP4 = 4
 
 
 class PadError(RuntimeError):
@@ -482,10 +483,10 @@ class ChunkPlan:
         hq, hk, d = problem.h_q, problem.h_kv, problem.head_dim
         self._q_shape, self._lse_shape = (self.n_tokens, hq, d), (self.n_tokens, hq)
         self._new_shape, self._read_shape = (self.n_tokens, hk, d), (self.n_cached, hk, d)
-        self._scale_shape = (n_pages, hk, problem.page_size)
-        self._pool_shape = self._scale_shape + (d,)
+        self._scale_shape = (n_pages, hk, problem.page_size) + ((d // 16,) if kv_format == KV_FP4 else ())
+        self._pool_shape = (n_pages, hk, problem.page_size, d // 2 if kv_format == KV_FP4 else d)
         self._bf16, self._f32, self._i32, self._u8 = torch.bfloat16, torch.float32, torch.int32, torch.uint8
-        self._pool_type = torch.uint8 if kv_format == KV_FP8 else torch.bfloat16
+        self._pool_type = torch.bfloat16 if kv_format == KV_BF16 else torch.uint8
         self._out_type = torch.bfloat16 if problem.out_dtype == 1 else torch.float32
 
     @property
@@ -597,7 +598,7 @@ def pad_chunk_plan(problem: Problem, cache, prefix_len, event_video, event_len, 
 
 
 def pad_chunk_append(plan: ChunkPlan, k_new, v_new, k_pool, v_pool, k_scale=None, v_scale=None, stream=None):
-    """Write the new tokens' K/V into the branches' pages (quantised in an 8-bit cache)."""
+    """Write the new tokens' K/V into the branches' pages (quantised in an 8-bit or 4-bit cache)."""
     shape, bf16 = plan._new_shape, plan._bf16
     if (k_new.shape == shape and v_new.shape == shape and k_new.dtype is bf16 and v_new.dtype is bf16
             and k_new.is_contiguous() and k_new.is_cuda and v_new.is_contiguous() and v_new.is_cuda):

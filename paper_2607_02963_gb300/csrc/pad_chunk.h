@@ -7,6 +7,8 @@
 //   part_o       float[partial_rows * head_dim]  (unnormalised O)
 #pragma once
 
+#include <cuda_fp16.h>
+
 #include "pad_internal.h"
 
 namespace pad {
@@ -45,6 +47,12 @@ struct ChunkRead {
   int32_t count;          // tokens
 };
 
+// A sequence held in 4 bits that is widened to bf16 pages of the plan's own, in spans as above.
+struct ChunkWiden {
+  int32_t event, page0;   // row of the page table; the first of its pages
+  int32_t span0, count;   // spans of the sequences before it; tokens
+};
+
 struct ChunkVerify {
   int32_t tok0, n_draft, draft0;  // first row of p, drafted tokens and the first of them; n_draft -1: no new token
 };
@@ -72,15 +80,22 @@ struct ChunkParams {
 };
 
 // Launchers; they return the launch error.
-cudaError_t launch_chunk_append(const ChunkParams& p, int head_dim, bool fp8, const ChunkPages* work, int n_work,
+cudaError_t launch_chunk_append(const ChunkParams& p, int head_dim, int kv_format, const ChunkPages* work, int n_work,
                                 const void* k_new, const void* v_new, int64_t stride, void* k_pool, void* v_pool,
                                 uint8_t* k_scale, uint8_t* v_scale, cudaStream_t s);
-cudaError_t launch_chunk_read(const ChunkParams& p, int head_dim, bool fp8, const ChunkRead* work, int n_events,
+cudaError_t launch_chunk_read(const ChunkParams& p, int head_dim, int kv_format, const ChunkRead* work, int n_events,
                               int n_spans, void* k_out, void* v_out, cudaStream_t s);
 int chunk_read_tokens();
+// The 4-bit tokens of `n_events` sequences into bf16 pages of the plan's own (row e of `table`, `columns` wide, lists
+// them; an entry whose page is not in the pool becomes -1).
+cudaError_t launch_chunk_widen(const ChunkParams& p, int head_dim, const ChunkWiden* work, int n_events, int n_spans,
+                               void* k_out, void* v_out, int32_t* table, int columns, cudaStream_t s);
 // rows16: 16-row groups that the items' rows take, 1 or 2.  early: not the call's first kernel.
 cudaError_t launch_chunk_mma(const ChunkParams& p, int head_dim, bool fp8, int rows16, bool early, const ChunkItem* items,
                              int n_items, cudaStream_t s);
+// The same over 4-bit pages; rows8: groups of eight rows, 1 to 4.
+cudaError_t launch_chunk_mma4(const ChunkParams& p, int head_dim, int rows8, bool early, const ChunkItem* items, int n_items,
+                              cudaStream_t s);
 // split: one slot of 128 / group tokens per CTA, its tiles taken in turn by two halves; else two slots.
 // prefix_tokens: tokens of k_prefix up to the last one that an item reads, 0 without prefix items.
 cudaError_t launch_chunk_tc(const ChunkParams& p, int head_dim, bool fp8, bool split, int64_t prefix_tokens,
@@ -129,6 +144,23 @@ __device__ __forceinline__ uint32_t scale_mult(uint32_t byte) {
 __device__ __forceinline__ uint32_t e4m3_pair(uint32_t x, uint32_t mult) {
   const uint32_t b = ((x >> 4) & 0x07f007f0u) | (x & 0x80008000u);
   const __nv_bfloat162 r = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&b), *reinterpret_cast<const __nv_bfloat162*>(&mult));
+  return *reinterpret_cast<const uint32_t*>(&r);
+}
+
+// The eight e2m1 codes of x as four f16 pairs, exactly: pair j holds the codes 2 j (its lower half) and 2 j + 1.
+__device__ __forceinline__ void f16_of_e2m1(uint32_t x, uint32_t (&h)[4]) {
+  asm("{\n .reg .b8 a, b, c, d;\n mov.b32 {a, b, c, d}, %4;\n"
+      " cvt.rn.f16x2.e2m1x2 %0, a;\n cvt.rn.f16x2.e2m1x2 %1, b;\n cvt.rn.f16x2.e2m1x2 %2, c;\n cvt.rn.f16x2.e2m1x2 %3, d;\n}\n"
+      : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3]) : "r"(x));
+}
+__device__ __forceinline__ uint32_t f16_times(uint32_t a, uint32_t b) {
+  const __half2 r = __hmul2(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
+  return *reinterpret_cast<const uint32_t*>(&r);
+}
+// (six significant bits at most: exact)
+__device__ __forceinline__ uint32_t bf16_of_f16(uint32_t h) {
+  const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h));
+  const __nv_bfloat162 r = __floats2bfloat162_rn(f.x, f.y);
   return *reinterpret_cast<const uint32_t*>(&r);
 }
 #endif

@@ -4,6 +4,7 @@
 #include <cmath>
 #include <cstring>
 #include <exception>
+#include <stdexcept>
 #include <vector>
 
 #include <nvtx3/nvToolsExt.h>
@@ -30,6 +31,9 @@ constexpr int kMinSplit = 256;
 // Rows of a branch (tokens x group) up to which the warp-level kernel takes it: two 16-row groups.  13 branches
 // of 35 rows over a prefix of 8219 take 25.4 us with this limit, 29.7 with 48 or 64, where they go in pieces.
 constexpr int kMmaRows = 32;
+// The same over 4-bit pages, which the warp-level kernel takes in pieces of 32 rows that each widen the keys again; beyond
+// it they are widened once, to bf16 pages in the workspace, for the tcgen05 kernel.
+constexpr int kMma4Rows = 192;
 
 size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
@@ -61,8 +65,8 @@ pad_status check_batch(const Batch& b) {
   if (st != PAD_OK) return st;
   if (b.prob->flags & ~(PAD_FLAG_PREFIX_MMA | PAD_FLAG_PREFIX_TC))
     return api_fail(PAD_ERR_UNSUPPORTED, "flags 0x%x: a multi-token step takes PAD_FLAG_PREFIX_MMA or PAD_FLAG_PREFIX_TC", b.prob->flags);
-  if (b.kv_format != PAD_KV_BF16 && b.kv_format != PAD_KV_FP8)
-    return api_fail(PAD_ERR_INVALID_ARG, "kv_format=%d (0 = bf16, 1 = 8 bits)", b.kv_format);
+  if (b.kv_format != PAD_KV_BF16 && b.kv_format != PAD_KV_FP8 && b.kv_format != PAD_KV_FP4)
+    return api_fail(PAD_ERR_INVALID_ARG, "kv_format=%d (0 = bf16, 1 = 8 bits, 4 = 4 bits)", b.kv_format);
   if (b.n_videos < 0 || b.n_events < 0) return api_fail(PAD_ERR_INVALID_ARG, "negative count");
   if (b.n_events > (1 << 20) || b.n_videos > (1 << 20)) return api_fail(PAD_ERR_UNSUPPORTED, "more than 2^20 events or videos");
   if (b.n_videos > 0 && !b.prefix_len) return api_fail(PAD_ERR_INVALID_ARG, "prefix_len is NULL");
@@ -91,16 +95,20 @@ struct Lists {
   std::vector<ChunkItem> tc;             // items of the tcgen05 kernel
   std::vector<ChunkItem> pre, page;      // items of the warp-level kernel: of the prefixes, of the pages
   bool tc_split = false, has_prefix = false;
-  int pre_rows16 = 1, page_rows16 = 1;
+  int pre_rows = 1, page_rows = 1;       // rows of the warp-level kernels' tiles, in 16s (4-bit pages: in 8s)
+  int pre_tokens = 1, page_tokens = 1;   // tokens of their items
   std::vector<ChunkMerge> merge;
   std::vector<ChunkPages> pages;
   std::vector<ChunkRead> read;
   std::vector<ChunkVerify> verify;
+  std::vector<ChunkWiden> widen;
   int64_t n_tokens = 0, n_cached = 0, n_drafts = 0, partial_rows = 0;
   int64_t prefix_tokens = 0;             // of k_prefix, up to the last one read
+  int64_t widen_pages = 0;
+  int32_t widen_spans = 0, widen_columns = 0;
   int32_t n_spans = 0, pre_splits = 0, page_splits = 0;
-  size_t off_tc = 0, off_pre = 0, off_page = 0, off_merge = 0, off_pages = 0, off_read = 0, off_verify = 0, image_bytes = 0;
-  size_t off_ml = 0, off_o = 0, total = 0;
+  size_t off_tc = 0, off_pre = 0, off_page = 0, off_merge = 0, off_pages = 0, off_read = 0, off_verify = 0, off_widen = 0, image_bytes = 0;
+  size_t off_ml = 0, off_o = 0, off_wtable = 0, off_wk = 0, off_wv = 0, total = 0;
 };
 
 // Consecutive chunk tokens that attend to one sequence of keys.
@@ -126,13 +134,20 @@ void split_by(Segment& s, int64_t len, int64_t unit) {
 // SM), and key ranges are cut so that there are some eight CTAs for each SM, no shorter than
 // kMinSplit keys.  (16 x 1 token over 333k cached tokens, 28/4 heads: 121 us in bf16 and 91 in 8 bits; with four CTAs
 // for each SM 127 and 98, with sixteen 133 and 110.  128 or 512 keys make no difference beyond a short call's noise.)
-void cut_mma(std::vector<Segment>& segs, int paged, const pad_problem& prob, int sms, int& rows16) {
+// 4-bit pages: tiles of eight rows, up to four; a branch of more rows in pieces of about as many tokens.
+void cut_mma(std::vector<Segment>& segs, int paged, const pad_problem& prob, bool fp4, int sms, int& rows, int& tpt) {
   const int G = prob.h_q / prob.h_kv;
-  int longest = 0;
+  int longest = 1;
   for (const Segment& s : segs)
     if (!s.tc && s.paged == paged) longest = std::max(longest, s.ntok);
-  rows16 = (int64_t)longest * G <= 16 ? 1 : 2;
-  const int tpt = 16 * rows16 / G;
+  if (fp4) {
+    const int pieces = (longest + 32 / G - 1) / (32 / G);
+    tpt = (longest + pieces - 1) / pieces;
+    rows = (tpt * G + 7) / 8;
+  } else {
+    rows = (int64_t)longest * G <= 16 ? 1 : 2;
+    tpt = 16 * rows / G;
+  }
   double work = 0;
   for (const Segment& s : segs)
     if (!s.tc && s.paged == paged) work += (double)((s.ntok + tpt - 1) / tpt) * s.keys * prob.h_kv;
@@ -245,6 +260,7 @@ void build(const Batch& b, const int64_t* prefix_offset, Lists& L) {
   const int ps = prob.page_size, span = chunk_read_tokens();
   const int sms = prob.num_sms > 0 ? prob.num_sms : api_num_sms();
   const int G = prob.h_q / prob.h_kv;
+  const bool fp4 = b.kv_format == PAD_KV_FP4;
   std::vector<Segment> segs;
   std::vector<int32_t> pre_of(b.n_events, -1), own_of(b.n_events, -1);
   int32_t open = -1;  // the video whose prefix segment is growing
@@ -283,11 +299,11 @@ void build(const Batch& b, const int64_t* prefix_offset, Lists& L) {
   }
   for (Segment& s : segs) {
     if (prob.flags & (PAD_FLAG_PREFIX_MMA | PAD_FLAG_PREFIX_TC)) s.tc = (prob.flags & PAD_FLAG_PREFIX_TC) != 0;
-    else s.tc = !s.paged || (int64_t)s.ntok * G > kMmaRows;
+    else s.tc = !s.paged || (int64_t)s.ntok * G > (fp4 ? kMma4Rows : kMmaRows);
   }
   cut_tc(segs, prob, b.kv_format == PAD_KV_FP8, sms, L.tc_split);
-  cut_mma(segs, 0, prob, sms, L.pre_rows16);
-  cut_mma(segs, 1, prob, sms, L.page_rows16);
+  cut_mma(segs, 0, prob, false, sms, L.pre_rows, L.pre_tokens);
+  cut_mma(segs, 1, prob, fp4, sms, L.page_rows, L.page_tokens);
   for (const Segment& s : segs) {
     int32_t& most = s.paged ? L.page_splits : L.pre_splits;
     most = std::max(most, s.n_splits);
@@ -319,13 +335,22 @@ void build(const Batch& b, const int64_t* prefix_offset, Lists& L) {
       }
     }
   for (Segment& s : segs) {
+    if (s.paged && s.tc && fp4) {
+      const int32_t columns = (s.keys + ps - 1) / ps;
+      L.widen.push_back({(int32_t)s.src, (int32_t)L.widen_pages, L.widen_spans, s.keys});
+      s.src = (int64_t)L.widen.size() - 1;
+      L.widen_pages += columns;
+      if (L.widen_pages > INT32_MAX) throw std::length_error("too many cached tokens to widen");
+      L.widen_spans += (s.keys + span - 1) / span;
+      L.widen_columns = std::max(L.widen_columns, columns);
+    }
     if (!s.paged) {
       s.src = off[s.src];
       L.has_prefix = true;
       L.prefix_tokens = std::max(L.prefix_tokens, s.src + s.keys);
     }
     if (s.tc) items_of(s, prob, (L.tc_split ? 1 : 2) * (128 / G), L.tc);
-    else items_of(s, prob, 16 * (s.paged ? L.page_rows16 : L.pre_rows16) / G, s.paged ? L.page : L.pre);
+    else items_of(s, prob, s.paged ? L.page_tokens : L.pre_tokens, s.paged ? L.page : L.pre);
   }
   // the longest first: what is left at the end of the grid is short
   auto longer = [](const ChunkItem& x, const ChunkItem& y) { return x.key1 - x.key0 > y.key1 - y.key0; };
@@ -343,12 +368,20 @@ void build(const Batch& b, const int64_t* prefix_offset, Lists& L) {
   place(L.off_pages, L.pages.size() * sizeof(ChunkPages));
   place(L.off_read, L.read.size() * sizeof(ChunkRead));
   place(L.off_verify, L.verify.size() * sizeof(ChunkVerify));
+  place(L.off_widen, L.widen.size() * sizeof(ChunkWiden));
   L.image_bytes = at - sizeof(PadDevHeader);
   at = align_up(at, 256);
   L.off_ml = at;
   at = align_up(at + (size_t)L.partial_rows * sizeof(float2), 256);
   L.off_o = at;
   at = align_up(at + (size_t)L.partial_rows * prob.head_dim * sizeof(float), 256);
+  const size_t wide = (size_t)L.widen_pages * prob.h_kv * ps * prob.head_dim * 2;
+  L.off_wtable = at;
+  at = align_up(at + L.widen.size() * (size_t)L.widen_columns * sizeof(int32_t), 256);
+  L.off_wk = at;
+  at = align_up(at + wide, 256);
+  L.off_wv = at;
+  at = align_up(at + wide, 256);
   L.total = at;
 }
 
@@ -402,8 +435,9 @@ pad_status check_launch(const pad_chunk_t* c, bool pages) {
 pad_status check_pools(const pad_chunk_t* c, const void* k_pool, const void* v_pool, const void* k_scale, const void* v_scale) {
   if (!k_pool || !v_pool) return api_fail(PAD_ERR_INVALID_ARG, "NULL pool");
   if (!aligned(k_pool, 16) || !aligned(v_pool, 16)) return api_fail(PAD_ERR_INVALID_ARG, "pools must be 16-byte aligned");
-  if (c->kv_format == PAD_KV_FP8) {
-    if (!k_scale || !v_scale) return api_fail(PAD_ERR_INVALID_ARG, "an 8-bit cache needs its scale pools");
+  if (c->kv_format != PAD_KV_BF16) {
+    if (!k_scale || !v_scale)
+      return api_fail(PAD_ERR_INVALID_ARG, "%s cache needs its scale pools", c->kv_format == PAD_KV_FP8 ? "an 8-bit" : "a 4-bit");
     if (!aligned(k_scale, 16) || !aligned(v_scale, 16)) return api_fail(PAD_ERR_INVALID_ARG, "scale pools must be 16-byte aligned");
   } else if (k_scale || v_scale) {
     return api_fail(PAD_ERR_INVALID_ARG, "a bf16 cache has no scale pools");
@@ -517,6 +551,7 @@ pad_status pad_chunk_plan(const pad_problem* prob, int32_t kv_format, pad_cache_
       put(c->L.off_pages, c->L.pages.data(), c->L.pages.size() * sizeof(ChunkPages));
       put(c->L.off_read, c->L.read.data(), c->L.read.size() * sizeof(ChunkRead));
       put(c->L.off_verify, c->L.verify.data(), c->L.verify.size() * sizeof(ChunkVerify));
+      put(c->L.off_widen, c->L.widen.data(), c->L.widen.size() * sizeof(ChunkWiden));
       if (!image.empty()) {
         cudaError_t e = api_copy_in(c->workspace + sizeof(PadDevHeader), image.data(), image.size(),
                                     reinterpret_cast<cudaStream_t>(stream));
@@ -578,7 +613,7 @@ pad_status pad_chunk_append(const pad_chunk_t* c, const void* k_new, const void*
   if (st != PAD_OK) return st;
   if (!k_new || !v_new || !aligned(k_new, 16) || !aligned(v_new, 16))
     return api_fail(PAD_ERR_INVALID_ARG, "k_new and v_new must be 16-byte aligned tensors");
-  cudaError_t e = launch_chunk_append(params_of(c), c->prob.head_dim, c->kv_format == PAD_KV_FP8,
+  cudaError_t e = launch_chunk_append(params_of(c), c->prob.head_dim, c->kv_format,
                                       list<ChunkPages>(c, c->L.off_pages), (int)c->L.pages.size(), k_new, v_new, new_stride,
                                       k_pool, v_pool, k_scale, v_scale, reinterpret_cast<cudaStream_t>(stream));
   return e == cudaSuccess ? PAD_OK : cuda_fail(e, "chunk append launch");
@@ -599,7 +634,7 @@ pad_status pad_chunk_read(const pad_chunk_t* c, const void* k_pool, const void* 
   p.v_pool = v_pool;
   p.k_scale = k_scale;
   p.v_scale = v_scale;
-  cudaError_t e = launch_chunk_read(p, c->prob.head_dim, c->kv_format == PAD_KV_FP8, list<ChunkRead>(c, c->L.off_read),
+  cudaError_t e = launch_chunk_read(p, c->prob.head_dim, c->kv_format, list<ChunkRead>(c, c->L.off_read),
                                     c->n_events, c->L.n_spans, k_out, v_out, reinterpret_cast<cudaStream_t>(stream));
   return e == cudaSuccess ? PAD_OK : cuda_fail(e, "chunk read launch");
 }
@@ -633,12 +668,27 @@ pad_status pad_chunk_attn(const pad_chunk_t* c, const void* q, int64_t q_stride,
   cudaStream_t s = reinterpret_cast<cudaStream_t>(stream);
   cudaError_t e = cudaSuccess;
   // the warp-level kernel first: its CTAs are short and share an SM, those of the other take one each
-  const bool fp8 = c->kv_format == PAD_KV_FP8;
-  if (!c->L.pre.empty())
-    e = launch_chunk_mma(p, c->prob.head_dim, false, c->L.pre_rows16, false, list<ChunkItem>(c, c->L.off_pre), (int)c->L.pre.size(), s);
-  if (e == cudaSuccess && !c->L.page.empty())
-    e = launch_chunk_mma(p, c->prob.head_dim, fp8, c->L.page_rows16, !c->L.pre.empty(), list<ChunkItem>(c, c->L.off_page),
-                         (int)c->L.page.size(), s);
+  const bool fp8 = c->kv_format == PAD_KV_FP8, fp4 = c->kv_format == PAD_KV_FP4;
+  uint8_t* const ws = c->workspace;
+  if (!c->L.widen.empty())  // (ahead of them all: what follows starts after it has ended)
+    e = launch_chunk_widen(p, c->prob.head_dim, list<ChunkWiden>(c, c->L.off_widen), (int)c->L.widen.size(), c->L.widen_spans,
+                           ws + c->L.off_wk, ws + c->L.off_wv, reinterpret_cast<int32_t*>(ws + c->L.off_wtable),
+                           c->L.widen_columns, s);
+  if (e == cudaSuccess && !c->L.pre.empty())
+    e = launch_chunk_mma(p, c->prob.head_dim, false, c->L.pre_rows, false, list<ChunkItem>(c, c->L.off_pre), (int)c->L.pre.size(), s);
+  if (e == cudaSuccess && !c->L.page.empty()) {
+    const ChunkItem* items = list<ChunkItem>(c, c->L.off_page);
+    const int n = (int)c->L.page.size();
+    e = fp4 ? launch_chunk_mma4(p, c->prob.head_dim, c->L.page_rows, !c->L.pre.empty(), items, n, s)
+            : launch_chunk_mma(p, c->prob.head_dim, fp8, c->L.page_rows, !c->L.pre.empty(), items, n, s);
+  }
+  if (fp4) {  // (the tcgen05 kernel's pages are the widened ones)
+    p.k_pool = ws + c->L.off_wk;
+    p.v_pool = ws + c->L.off_wv;
+    p.page_table = reinterpret_cast<int32_t*>(ws + c->L.off_wtable);
+    p.max_pages = c->L.widen_columns;
+    p.n_pages = (int32_t)c->L.widen_pages;
+  }
   p.beside = !c->L.pre.empty() || !c->L.page.empty();
   if (e == cudaSuccess && !c->L.tc.empty())
     e = launch_chunk_tc(p, c->prob.head_dim, fp8, c->L.tc_split, c->L.prefix_tokens, list<ChunkItem>(c, c->L.off_tc),

@@ -8,12 +8,18 @@
 // there because the readers undo the format's exponent offset and the scale in one bf16 product,
 // 2^(120 + k), which has to be finite.
 //
+// A 4-bit group (16 consecutive values of one token and kv-head): the scale s is max|x| / 6 rounded to 5 exponent
+// and 3 mantissa bits, the upper byte of its f16 pattern without the sign, 10240 at most; codes are e2m1 of x / s to
+// nearest even.  Code times scale has six significant bits at most and is exact in bf16 and in f16 (up to 6 x 10240 = 61440).
+//
 // Bound by memory, one pass each; short ones by the launch.  32768 tokens of 4 heads x 128 written and read back
 // (two calls of 101 MB): 45 us, 4.5 TB/s; 32 branches x 5 tokens written and 9000 read: 12 us.
 #include <cuda_bf16.h>
+#include <cuda_fp16.h>
 #include <cuda_fp8.h>
 #include <algorithm>
 #include <cstdint>
+#include <type_traits>
 
 #include "pad_chunk.h"
 
@@ -24,8 +30,39 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kReadTokens = 32;  // of a span
 
-// 16 lanes of 8 bf16 values (8 at head_dim 64) hold one group.
-template <int D, bool FP8>
+// The 4-bit codes of eight values with scale byte `byte`.  x / s is x times the rounded 1 / s, 2^-22 off at most, rounded
+// to f16 on the way: x has eight significant bits and s four, so that x / s either is a number half way between two
+// codes (three significant bits), which f16 restores, or is 2^-8 of itself away from every one, further than f16 moves it.
+__device__ __forceinline__ uint32_t e2m1_codes(const uint32_t (&x)[4], uint32_t byte) {
+  const float s = (byte >> 3) ? __uint_as_float((byte + 896u) << 20) : (float)byte * 0x1p-17f;
+  const float inv = byte == 0u ? 0.f : 1.f / s;
+  float y[8];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const __half2 h = __floats2half2_rn(__uint_as_float(x[j] << 16) * inv, __uint_as_float(x[j] & 0xffff0000u) * inv);
+    y[2 * j] = __low2float(h);
+    y[2 * j + 1] = __high2float(h);
+  }
+  uint32_t r;
+  asm("{\n .reg .b8 a, b, c, d;\n"
+      " cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n cvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n"
+      " cvt.rn.satfinite.e2m1x2.f32 c, %6, %5;\n cvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n"
+      " mov.b32 %0, {a, b, c, d};\n}\n"
+      : "=r"(r) : "f"(y[0]), "f"(y[1]), "f"(y[2]), "f"(y[3]), "f"(y[4]), "f"(y[5]), "f"(y[6]), "f"(y[7]));
+  return r;
+}
+// The scale byte of a group whose largest magnitude has this bf16 pattern: max / 6 (no tie is moved by that division's
+// rounding: the quotient of an eight-bit number by 3 that lies half way between two scales is exact) to the nearest.
+__device__ __forceinline__ uint32_t e2m1_scale(uint32_t m) {
+  if (m >= 0x7f80u) return 255u;
+  const float s = __fdiv_rn(__uint_as_float(m << 16), 6.f);
+  const uint32_t u = __float_as_uint(s);
+  const uint32_t b = s < 0x1p-14f ? (uint32_t)rintf(s * 0x1p17f) : ((u + 0x7ffffu + ((u >> 20) & 1u)) >> 20) - 896u;
+  return min(b, 226u);
+}
+
+// 16 lanes of 8 bf16 values (8 at head_dim 64) hold a token and head: one 8-bit group, or a 4-bit one for two lanes.
+template <int D, int FMT>
 __global__ void __launch_bounds__(kThreads) chunk_append_kernel(const __grid_constant__ ChunkParams p,
                                                                 const ChunkPages* __restrict__ work,
                                                                 const __nv_bfloat16* __restrict__ k_new,
@@ -61,7 +98,7 @@ __global__ void __launch_bounds__(kThreads) chunk_append_kernel(const __grid_con
       const int g = (i0 + u * kThreads) / L, tok = g / (2 * p.h_kv), r = g % (2 * p.h_kv), h = r >> 1;
       const bool on = g < groups;
       const int64_t slot = ((int64_t)page * p.h_kv + h) * p.page_size + w.slot + tok;
-      if (!FP8) {
+      if (FMT == PAD_KV_BF16) {
         if (on) *(reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>((r & 1) ? v_pool : k_pool) + slot * D) + c) = x[u];
         continue;
       }
@@ -71,7 +108,15 @@ __global__ void __launch_bounds__(kThreads) chunk_append_kernel(const __grid_con
 #pragma unroll
       for (int j = 0; j < 4; ++j) m = max(m, max(xs[j] & 0x7fffu, (xs[j] >> 16) & 0x7fffu));
 #pragma unroll
-      for (int o = L / 2; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
+      for (int o = FMT == PAD_KV_FP4 ? 1 : L / 2; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
+      if (FMT == PAD_KV_FP4) {
+        const uint32_t byte = e2m1_scale(m);
+        if (on) {
+          static_cast<uint32_t*>((r & 1) ? v_pool : k_pool)[slot * (D / 8) + c] = byte == 255u ? 0u : e2m1_codes(xs, byte);
+          if (!(c & 1)) ((r & 1) ? v_scale : k_scale)[slot * (D / 16) + (c >> 1)] = (uint8_t)byte;
+        }
+        continue;
+      }
       // max = f * 2^(e - 127) with f in [1, 2): max <= 448 * 2^k = 1.75 * 2^(k + 8).  (A subnormal's k
       // is below the range in any case.)
       const int e = (int)(m >> 7);
@@ -99,27 +144,34 @@ __global__ void __launch_bounds__(kThreads) chunk_append_kernel(const __grid_con
 }
 
 // One span: up to kReadTokens consecutive tokens of an event, all heads, K and V.  A thread moves 16
-// bytes in bf16, or 8 codes to 16 bytes.
-template <int D, bool FP8>
+// bytes in bf16, or 8 codes to 16 bytes.  Work: ChunkRead for tokens copied out, ChunkWiden for pages in bf16.
+template <int D, int FMT, class Work>
 __global__ void __launch_bounds__(kThreads) chunk_read_kernel(const __grid_constant__ ChunkParams p,
-                                                              const ChunkRead* __restrict__ work, int n_events,
+                                                              const Work* __restrict__ work, int n_events,
                                                               __nv_bfloat16* __restrict__ k_out,
-                                                              __nv_bfloat16* __restrict__ v_out) {
+                                                              __nv_bfloat16* __restrict__ v_out,
+                                                              int32_t* __restrict__ table, int columns) {
   constexpr int L = D / 8;
+  constexpr bool kWiden = std::is_same<Work, ChunkWiden>::value;
   __shared__ int pages[kReadTokens];
-  __shared__ ChunkRead mine;
-  __shared__ int event;
+  __shared__ Work mine;
+  __shared__ int row;
   const int b = (int)blockIdx.x;
   for (int e = threadIdx.x; e < n_events; e += kThreads) {
-    const ChunkRead w = work[e];
-    if (b >= w.span0 && b < w.span0 + (w.count + kReadTokens - 1) / kReadTokens) mine = w, event = e;  // (one event holds it)
+    const Work w = work[e];
+    if (b >= w.span0 && b < w.span0 + (w.count + kReadTokens - 1) / kReadTokens) mine = w, row = e;  // (one event holds it)
   }
   __syncthreads();
+  int event = row;
+  if constexpr (kWiden) event = mine.event;
   const int pos = (b - mine.span0) * kReadTokens, count = min(kReadTokens, mine.count - pos);
   if ((int)threadIdx.x < count) {
     const int col = (pos + (int)threadIdx.x) >> p.page_shift, pg = __ldcg(p.page_table + (int64_t)event * p.max_pages + col);
     pages[threadIdx.x] = pg;
-    if ((unsigned)pg >= (unsigned)p.n_pages) pad_set_error(p.header, p.gen, PAD_ERR_DEVICE_BOUNDS, event, col, pg);
+    const bool there = (unsigned)pg < (unsigned)p.n_pages;
+    if (!there) pad_set_error(p.header, p.gen, PAD_ERR_DEVICE_BOUNDS, event, col, pg);
+    if constexpr (kWiden)
+      if (((pos + (int)threadIdx.x) & (p.page_size - 1)) == 0) table[(int64_t)row * columns + col] = there ? mine.page0 + col : -1;
   }
   __syncthreads();
   const int n = count * p.h_kv * L, c = threadIdx.x % L;
@@ -132,7 +184,10 @@ __global__ void __launch_bounds__(kThreads) chunk_read_kernel(const __grid_const
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int i = i0 + u * kThreads, g = i / L, h = g % p.h_kv, t = g / p.h_kv;
-      to[u] = i < n ? ((mine.out + pos + t) * p.h_kv + h) * D + 8 * c : -1;
+      if constexpr (kWiden)
+        to[u] = i < n ? ((((int64_t)mine.page0 + ((pos + t) >> p.page_shift)) * p.h_kv + h) * p.page_size + ((pos + t) & (p.page_size - 1))) * D + 8 * c : -1;
+      else
+        to[u] = i < n ? ((mine.out + pos + t) * p.h_kv + h) * D + 8 * c : -1;
       x[u][0] = x[u][1] = make_uint4(0u, 0u, 0u, 0u);
       sc[u][0] = sc[u][1] = 0u;
       const int pg = i < n ? pages[t] : -1;
@@ -141,7 +196,10 @@ __global__ void __launch_bounds__(kThreads) chunk_read_kernel(const __grid_const
 #pragma unroll
       for (int kv = 0; kv < 2; ++kv) {
         const void* pool = kv ? p.v_pool : p.k_pool;
-        if (FP8) {
+        if (FMT == PAD_KV_FP4) {
+          x[u][kv].x = __ldcg(static_cast<const uint32_t*>(pool) + slot * L + c);
+          sc[u][kv] = __ldcg((kv ? p.v_scale : p.k_scale) + slot * (D / 16) + (c >> 1));
+        } else if (FMT == PAD_KV_FP8) {
           const uint2 v = __ldcg(reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(pool) + slot * D) + c);
           x[u][kv].x = v.x;
           x[u][kv].y = v.y;
@@ -157,7 +215,14 @@ __global__ void __launch_bounds__(kThreads) chunk_read_kernel(const __grid_const
 #pragma unroll
       for (int kv = 0; kv < 2; ++kv) {
         uint4 o = x[u][kv];
-        if (FP8) {
+        if (FMT == PAD_KV_FP4) {
+          const uint32_t m = (sc[u][kv] << 7) * 0x10001u;  // the scale as f16, twice
+          uint32_t h[4];
+          f16_of_e2m1(x[u][kv].x, h);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) h[j] = bf16_of_f16(f16_times(h[j], m));
+          o = make_uint4(h[0], h[1], h[2], h[3]);
+        } else if (FMT == PAD_KV_FP8) {
           uint32_t m = scale_mult(sc[u][kv]);
           m |= m << 16;
           o = make_uint4(e4m3_pair(__byte_perm(x[u][kv].x, 0u, 0x1404), m), e4m3_pair(__byte_perm(x[u][kv].x, 0u, 0x3424), m),
@@ -169,33 +234,42 @@ __global__ void __launch_bounds__(kThreads) chunk_read_kernel(const __grid_const
   }
 }
 
-template <int D, bool FP8>
+template <int D, int FMT>
 cudaError_t append(const ChunkParams& p, const ChunkPages* work, int n, const void* k_new, const void* v_new,
                    int64_t stride, void* k_pool, void* v_pool, uint8_t* ks, uint8_t* vs, cudaStream_t s) {
-  return launch_early(false, chunk_append_kernel<D, FP8>, dim3(n), kThreads, 0, s, p, work, static_cast<const __nv_bfloat16*>(k_new),
+  return launch_early(false, chunk_append_kernel<D, FMT>, dim3(n), kThreads, 0, s, p, work, static_cast<const __nv_bfloat16*>(k_new),
                       static_cast<const __nv_bfloat16*>(v_new), stride, k_pool, v_pool, ks, vs);
 }
-template <int D, bool FP8>
+template <int D, int FMT>
 cudaError_t read(const ChunkParams& p, const ChunkRead* work, int n_events, int n, void* k_out, void* v_out, cudaStream_t s) {
-  return launch_early(false, chunk_read_kernel<D, FP8>, dim3(n), kThreads, 0, s, p, work, n_events, static_cast<__nv_bfloat16*>(k_out),
-                      static_cast<__nv_bfloat16*>(v_out));
+  return launch_early(false, chunk_read_kernel<D, FMT, ChunkRead>, dim3(n), kThreads, 0, s, p, work, n_events,
+                      static_cast<__nv_bfloat16*>(k_out), static_cast<__nv_bfloat16*>(v_out), nullptr, 0);
 }
 
 }  // namespace
 
 int chunk_read_tokens() { return kReadTokens; }
 
-cudaError_t launch_chunk_append(const ChunkParams& p, int head_dim, bool fp8, const ChunkPages* work, int n_work,
+cudaError_t launch_chunk_append(const ChunkParams& p, int head_dim, int kv_format, const ChunkPages* work, int n_work,
                                 const void* k_new, const void* v_new, int64_t stride, void* k_pool, void* v_pool,
                                 uint8_t* k_scale, uint8_t* v_scale, cudaStream_t s) {
-  auto* f = head_dim == 128 ? (fp8 ? append<128, true> : append<128, false>) : (fp8 ? append<64, true> : append<64, false>);
+  auto* f = head_dim == 128 ? (kv_format == PAD_KV_FP4 ? append<128, PAD_KV_FP4> : kv_format == PAD_KV_FP8 ? append<128, PAD_KV_FP8> : append<128, PAD_KV_BF16>)
+                            : (kv_format == PAD_KV_FP4 ? append<64, PAD_KV_FP4> : kv_format == PAD_KV_FP8 ? append<64, PAD_KV_FP8> : append<64, PAD_KV_BF16>);
   return f(p, work, n_work, k_new, v_new, stride, k_pool, v_pool, k_scale, v_scale, s);
 }
 
-cudaError_t launch_chunk_read(const ChunkParams& p, int head_dim, bool fp8, const ChunkRead* work, int n_events,
+cudaError_t launch_chunk_read(const ChunkParams& p, int head_dim, int kv_format, const ChunkRead* work, int n_events,
                               int n_spans, void* k_out, void* v_out, cudaStream_t s) {
-  auto* f = head_dim == 128 ? (fp8 ? read<128, true> : read<128, false>) : (fp8 ? read<64, true> : read<64, false>);
+  auto* f = head_dim == 128 ? (kv_format == PAD_KV_FP4 ? read<128, PAD_KV_FP4> : kv_format == PAD_KV_FP8 ? read<128, PAD_KV_FP8> : read<128, PAD_KV_BF16>)
+                            : (kv_format == PAD_KV_FP4 ? read<64, PAD_KV_FP4> : kv_format == PAD_KV_FP8 ? read<64, PAD_KV_FP8> : read<64, PAD_KV_BF16>);
   return f(p, work, n_events, n_spans, k_out, v_out, s);
+}
+
+cudaError_t launch_chunk_widen(const ChunkParams& p, int head_dim, const ChunkWiden* work, int n_events, int n_spans,
+                               void* k_out, void* v_out, int32_t* table, int columns, cudaStream_t s) {
+  auto* f = head_dim == 128 ? chunk_read_kernel<128, PAD_KV_FP4, ChunkWiden> : chunk_read_kernel<64, PAD_KV_FP4, ChunkWiden>;
+  return launch_early(false, f, dim3(n_spans), kThreads, 0, s, p, work, n_events, static_cast<__nv_bfloat16*>(k_out),
+                      static_cast<__nv_bfloat16*>(v_out), table, columns);
 }
 
 }  // namespace pad
