@@ -493,8 +493,10 @@ pad_status pad_prefill_status(pad_stream_t stream);
  *   pad_chunk_plan    host: validate, allocate pages, build the work lists and copy them to
  *                     the workspace; one plan serves every layer of the model;
  *   pad_chunk_append  write the new tokens' K/V into the branches' pages (quantised where the
- *                     cache is held in 8 or 4 bits) and the new page-table entries;
+ *                     cache is held in 8 or 4 bits) and the new page-table entries; or
+ *   pad_chunk_append_rope  the same with the rotary positions of the new queries and keys;
  *   pad_chunk_attn    attention of the new tokens;
+ *   pad_chunk_probs   the model's logits turned into probabilities;
  *   pad_draft_verify  accept or reject the drafted tokens and draw the next one;
  *   pad_chunk_commit  host: the branches' new lengths; pages past them go back.
  * pad_chunk_read copies the branches' cached tokens out as contiguous bf16 (the layout of
@@ -502,8 +504,8 @@ pad_status pad_prefill_status(pad_stream_t stream);
  * another stream than the plan's must be ordered after it by the caller.  The calls after the plan may be
  * captured into a graph and replayed with other contents in the same buffers.
  *
- * What the one-token step has and this one has not: rotary positions (pad_plan_set_rope: q and k_new come rotated
- * here), and the modes PAD_G_SELF and PAD_BRANCH_CAUSAL.  Its weights go into P.V as one bf16 number each, 2^-8 of
+ * What the one-token step has and this one has not: rotary positions from a table (pad_plan_set_rope; here
+ * pad_chunk_append_rope turns q and k_new), and the modes PAD_G_SELF and PAD_BRANCH_CAUSAL.  Its weights go into P.V as one bf16 number each, 2^-8 of
  * themselves at most off, at head_dim 64 too, where the one-token step's prefix pass keeps them in two parts.
  *
  * Layouts (row-major, bf16 unless stated); N = sum of n_new, tokens packed event by event:
@@ -597,6 +599,54 @@ pad_status pad_chunk_destroy(pad_chunk_t* chunk);
 pad_status pad_chunk_append(const pad_chunk_t* chunk, const void* k_new, const void* v_new, int64_t new_stride,
                             void* k_pool, void* v_pool, uint8_t* k_scale, uint8_t* v_scale, pad_stream_t stream);
 
+/* Rotary positions: what a model says of them, and the pairs' frequencies that follow.  Pair i of the first rotary_dim
+ * dimensions of a head, (i, i + rotary_dim / 2) or, interleaved, (2 i, 2 i + 1), is turned by position * f_i; the other
+ * dimensions stay as they are.  f_i = theta^(-2 i / rotary_dim), scaled for contexts longer than the trained ones:
+ *   PAD_ROPE_LINEAR  f_i / factor;
+ *   PAD_ROPE_BASE    theta replaced by theta * factor^(rotary_dim / (rotary_dim - 2));
+ *   PAD_ROPE_TURNS   f_i (g + (1 - g) / factor), g = (n_i - low) / (high - low) kept in [0, 1], n_i = original_len f_i / 2 pi,
+ *                    the turns that pair i makes over the trained length;
+ *   PAD_ROPE_INDEX   the same with g = 1 - (i - a) / max(b - a, 0.001) kept in [0, 1], a = floor(I(high)), b = ceil(I(low)), both
+ *                    kept in [0, rotary_dim - 1], I(n) = rotary_dim ln(original_len / (2 pi n)) / (2 ln theta).
+ * Cosine and sine are multiplied by `magnitude`.  Fields that a scaling does not name are not read. */
+typedef struct {
+  int32_t head_dim;          /* 64 or 128 */
+  int32_t rotary_dim;        /* even, 2 to head_dim (PAD_ROPE_BASE: at least 4) */
+  int32_t layout;            /* PAD_ROPE_HALF or PAD_ROPE_INTERLEAVED */
+  int32_t scaling;
+  double theta;              /* > 0 (PAD_ROPE_INDEX: > 1) */
+  double factor;             /* > 0 */
+  double original_len;       /* > 0 */
+  double low, high;          /* low < high (PAD_ROPE_INDEX: 0 < low < high) */
+  double magnitude;          /* finite; 1 for none */
+} pad_rope_spec;
+#define PAD_ROPE_HALF 0
+#define PAD_ROPE_INTERLEAVED 1
+#define PAD_ROPE_NONE 0
+#define PAD_ROPE_LINEAR 1
+#define PAD_ROPE_BASE 2
+#define PAD_ROPE_TURNS 3
+#define PAD_ROPE_INDEX 4
+typedef struct {
+  int32_t head_dim, rotary_dim, layout;
+  float magnitude;
+  uint64_t turn[64];         /* f_i / 2 pi in units of 2^-64: the product with a position, without its upper bits, is the
+                              * pair's angle as a fraction of a turn, however far the position */
+} pad_rope;
+/* Fill `rope` from `spec` (host). */
+pad_status pad_rope_init(const pad_rope_spec* spec, pad_rope* rope);
+
+/* pad_chunk_append with rotary positions: k_new is turned before it is written into the pools (rounded once to bf16, then
+ * quantised where the cache is), v_new is written as it is, and q is turned into q_out.
+ *   position   [N] int32 device, of each new token, any value
+ *   q, q_out   [N, h_q, head_dim] bf16; q_out may be q itself (same stride), and must not overlap q, k_new or v_new otherwise
+ * Angles are exact to 2^-24 of a turn at any position.  Strides are in elements, multiples of 8, 0 = packed.  A page id
+ * outside the pool keeps its keys and values out and is recorded; their queries are turned all the same. */
+pad_status pad_chunk_append_rope(const pad_chunk_t* chunk, const pad_rope* rope, const int32_t* position, const void* q,
+                                 int64_t q_stride, void* q_out, int64_t q_out_stride, const void* k_new, const void* v_new,
+                                 int64_t new_stride, void* k_pool, void* v_pool, uint8_t* k_scale, uint8_t* v_scale,
+                                 pad_stream_t stream);
+
 /* Copy the cached tokens of every event, positions 0 .. event_len + n_new - 1, event after event,
  * into k_out / v_out [n_cached, h_kv, head_dim] bf16 (exact in either format).  The tokens of a page id outside
  * the pool come out as zeros, and it is recorded (pad_chunk_status). */
@@ -612,6 +662,30 @@ pad_status pad_chunk_read(const pad_chunk_t* chunk, const void* k_pool, const vo
 pad_status pad_chunk_attn(const pad_chunk_t* chunk, const void* q, int64_t q_stride, const void* k_prefix,
                           const void* v_prefix, const void* k_pool, const void* v_pool, const uint8_t* k_scale,
                           const uint8_t* v_scale, void* out, float* lse, pad_stream_t stream);
+
+/* Logits turned into the probabilities that pad_draft_verify reads.  Row t of event e:
+ *   x = logit; c = how often the token occurs in the event's history and in its chunk's tokens up to and including t's;
+ *   where c > 0, x = x / r if x > 0, else x * r, and then x = x - (frequency * c + presence);
+ *   x = x + the event's biases of that token; a token whose mask bit is 0 is left out, whatever its logit is;
+ *   p = softmax(x / T) over what is left; with T not above 0 one-hot at the first largest x; zeros where nothing is left
+ *   (every token masked, or at -infinity).  A NaN or +infinity among what is left makes a row with T > 0 NaN; with T not above 0
+ *   a NaN makes it zeros.
+ *   logits       [N, vocab] fp32 or bf16 (logits_dtype 0 or 1), row stride logits_stride elements (0 = vocab)
+ *   p            [N, vocab] fp32 or bf16 (p_dtype), row stride p_stride; may be logits itself (same type and stride)
+ *   params       [n_events, 4] fp32: T, r (> 0), frequency, presence; NULL: 1, 1, 0, 0 for every event
+ *   tokens       [N] int32, the chunk's tokens; NULL: only the history counts
+ *   history      [n_events, history_width] int32, event e's first history_len[e] entries; NULL (with history_len): none
+ *   bias_token   [n_events, bias_width] int32, bias_value the same in fp32, event e's first bias_len[e] entries, in any
+ *                order (a token that occurs again has the sum of its values, added in the order they are in); NULL (all three): none
+ *   mask         [N, mask_stride] int32 words, bit i % 32 of word i / 32 for token i; mask_stride at least
+ *                ceil(vocab / 32), 0 = that; NULL: every token is allowed
+ * All device memory.  Tokens outside [0, vocab) are passed over; lengths are kept within their rows.  Sums are in fp32 in a fixed
+ * order: the same inputs give the same bits.  vocab at most 393216. */
+pad_status pad_chunk_probs(const pad_chunk_t* chunk, int32_t vocab, int32_t logits_dtype, const void* logits, int64_t logits_stride,
+                           const float* params, const int32_t* tokens, const int32_t* history, int32_t history_width,
+                           const int32_t* history_len, const int32_t* bias_token, const float* bias_value, int32_t bias_width,
+                           const int32_t* bias_len, const int32_t* mask, int64_t mask_stride, int32_t p_dtype, void* p,
+                           int64_t p_stride, pad_stream_t stream);
 
 /* Verify drafted tokens: event e has n_new[e] - 1 drafted tokens (none where n_new is 0 or 1), its chunk
  * being its last accepted token followed by them.

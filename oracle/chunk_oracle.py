@@ -119,6 +119,66 @@ def chunk_attention(q, k, v, first_limit: int, scale: float):
     return out, lse, mag
 
 
+def rope_frequencies(rotary, theta, scaling="none", factor=1.0, original_len=0.0, low=1.0, high=4.0):
+    """f_i of each rotary pair, scaled for long contexts."""
+    if scaling == "base":
+        theta = theta * factor ** (rotary / (rotary - 2))
+    f = np.array([theta ** (-2.0 * i / rotary) for i in range(rotary // 2)])
+    if scaling == "linear":
+        return f / factor
+    if scaling == "turns":
+        g = np.clip((original_len * f / (2 * math.pi) - low) / (high - low), 0, 1)
+        return f * (g + (1 - g) / factor)
+    if scaling == "index":
+        def index(n):
+            return rotary * math.log(original_len / (2 * math.pi * n)) / (2 * math.log(theta))
+        a, b = (min(max(x, 0), rotary - 1) for x in (math.floor(index(high)), math.ceil(index(low))))
+        g = 1 - np.clip((np.arange(rotary // 2) - a) / max(b - a, 0.001), 0, 1)
+        return f * (g + (1 - g) / factor)
+    return f
+
+
+def rope_turn(x, position, frequencies, layout="half", magnitude=1.0):
+    """x [n, heads, d] float64 turned at position [n]; also |a| + |b| of each value's pair, 0 for those that stay."""
+    r = 2 * len(frequencies)
+    angle = np.asarray(position, dtype=np.float64)[:, None] * frequencies
+    cos, sin = (magnitude * f(angle)[:, None] for f in (np.cos, np.sin))
+    one, two = (slice(0, r // 2), slice(r // 2, r)) if layout == "half" else (slice(0, r, 2), slice(1, r, 2))
+    a, b = x[..., one], x[..., two]
+    out, size = x.copy(), np.zeros_like(x)
+    out[..., one], out[..., two] = a * cos - b * sin, b * cos + a * sin
+    size[..., one] = size[..., two] = np.abs(a) + np.abs(b)
+    return out, size
+
+
+def logits_to_probs(logits, temperature=1.0, repetition=1.0, frequency=0.0, presence=0.0, context=(), biases=(), allowed=None):
+    """One row [vocab] in 64 bits: penalties for the tokens of ``context``, (token, value) ``biases``, a boolean mask, softmax.
+    Returns p and the largest magnitude that a logit passes through."""
+    x = np.asarray(logits, dtype=np.float64).copy()
+    vocab = len(x)
+    count = np.bincount([t for t in context if 0 <= t < vocab], minlength=vocab).astype(np.float64)
+    size = np.abs(x) * max(repetition, 1 / repetition)
+    x = np.where(count > 0, np.where(x > 0, x / repetition, x * repetition) - (frequency * count + presence), x)
+    size += count * abs(frequency) + abs(presence)
+    for t, v in biases:
+        if 0 <= t < vocab:
+            x[t] += v
+            size[t] += abs(v)
+    if allowed is not None:
+        x[~np.asarray(allowed, bool)] = -np.inf
+    size = float(np.max(np.where(np.isfinite(x) & np.isfinite(size), size, 0)))
+    if not np.isnan(x).any() and x.max() == -np.inf:
+        return np.zeros(vocab), size
+    if not temperature > 0:
+        p = np.zeros(vocab)
+        if not np.isnan(x).any():
+            p[int(np.argmax(x))] = 1.0
+        return p, size
+    with np.errstate(invalid="ignore"):
+        e = np.exp((x - np.max(x)) / temperature)
+    return e / e.sum(), size
+
+
 def draft_verify(p, q, draft, u_accept, u_pick):
     """One event: p [n + 1, V], q [n, V] float32 arrays (bf16 widened), drafted tokens [n], uniforms.
     Returns (accepted, token); Python integers throughout the draw."""

@@ -62,6 +62,16 @@ class ChunkInfo(ctypes.Structure):
                 ("page_splits", c_int32), ("tc_items", c_int32), ("mma_items", c_int32), ("prefix_tokens", c_int32)]
 
 
+class RopeSpec(ctypes.Structure):
+    _fields_ = [("head_dim", c_int32), ("rotary_dim", c_int32), ("layout", c_int32), ("scaling", c_int32)] + [
+        (f, ctypes.c_double) for f in ("theta", "factor", "original_len", "low", "high", "magnitude")]
+
+
+class RopeTurns(ctypes.Structure):
+    _fields_ = [("head_dim", c_int32), ("rotary_dim", c_int32), ("layout", c_int32), ("magnitude", c_float),
+                ("turn", ctypes.c_uint64 * 64)]
+
+
 _I32P = POINTER(c_int32)
 _I64P = POINTER(c_int64)
 
@@ -118,6 +128,11 @@ _SIGNATURES = {
     "pad_chunk_destroy": (c_int32, [c_void_p]),
     "pad_chunk_append": (c_int32, [c_void_p, c_void_p, c_void_p, c_int64, c_void_p, c_void_p, c_void_p, c_void_p,
                                    c_void_p]),
+    "pad_rope_init": (c_int32, [POINTER(RopeSpec), POINTER(RopeTurns)]),
+    "pad_chunk_append_rope": (c_int32, [c_void_p, POINTER(RopeTurns), c_void_p, c_void_p, c_int64, c_void_p, c_int64, c_void_p,
+                                        c_void_p, c_int64] + [c_void_p] * 5),
+    "pad_chunk_probs": (c_int32, [c_void_p, c_int32, c_int32, c_void_p, c_int64, c_void_p, c_void_p, c_void_p, c_int32, c_void_p,
+                                  c_void_p, c_void_p, c_int32, c_void_p, c_void_p, c_int64, c_int32, c_void_p, c_int64, c_void_p]),
     "pad_chunk_read": (c_int32, [c_void_p] * 8),
     "pad_chunk_attn": (c_int32, [c_void_p, c_void_p, c_int64] + [c_void_p] * 9),
     "pad_draft_verify": (c_int32, [c_void_p, c_int32, c_int32, c_void_p, c_int64, c_void_p, c_int64] + [c_void_p] * 6),
@@ -614,6 +629,54 @@ def pad_chunk_append(plan: ChunkPlan, k_new, v_new, k_pool, v_pool, k_scale=None
         _check(st)
 
 
+class Rope:
+    """A model's rotary positions (pad_rope_init): the first ``rotary_dim`` dimensions of a head in pairs (i, i + rotary_dim / 2)
+    ("half") or (2 i, 2 i + 1) ("interleaved"), turned by position * theta^(-2 i / rotary_dim).  ``scaling`` for contexts longer than
+    the trained ones: "none", "linear", "base", "turns" or "index" (see pad.h for their formulas and what each reads)."""
+
+    LAYOUTS = ("half", "interleaved")
+    SCALINGS = ("none", "linear", "base", "turns", "index")
+
+    def __init__(self, head_dim, rotary_dim=None, theta=10000.0, layout="half", scaling="none", factor=1.0, original_len=0.0, low=1.0,
+                 high=4.0, magnitude=1.0):
+        if layout not in self.LAYOUTS:
+            raise ValueError(f"layout {layout!r}, expected one of {self.LAYOUTS}")
+        if scaling not in self.SCALINGS:
+            raise ValueError(f"scaling {scaling!r}, expected one of {self.SCALINGS}")
+        spec = RopeSpec(int(head_dim), int(head_dim if rotary_dim is None else rotary_dim), self.LAYOUTS.index(layout),
+                        self.SCALINGS.index(scaling), theta, factor, original_len, low, high, magnitude)
+        self.turns = RopeTurns()
+        _check(lib().pad_rope_init(ctypes.byref(spec), ctypes.byref(self.turns)))
+        self._ref = ctypes.byref(self.turns)
+
+
+def pad_chunk_append_rope(plan: ChunkPlan, rope: Rope, position, q, q_out, k_new, v_new, k_pool, v_pool, k_scale=None, v_scale=None,
+                          stream=None):
+    """pad_chunk_append with rotary positions: k_new is turned on its way into the pools, q into q_out (which may be q itself).
+    ``position`` [N] int32: of each new token."""
+    shape, qs, bf16 = plan._new_shape, plan._q_shape, plan._bf16
+    if (k_new.shape == shape and v_new.shape == shape and k_new.dtype is bf16 and v_new.dtype is bf16
+            and k_new.is_contiguous() and k_new.is_cuda and v_new.is_contiguous() and v_new.is_cuda):
+        kn, vn, ks = k_new.data_ptr(), v_new.data_ptr(), 0
+    else:
+        kn, ks = _rows(k_new, "k_new", shape, bf16)
+        vn, vs = _rows(v_new, "v_new", shape, bf16)
+        if ks != vs:
+            raise ValueError("k_new and v_new must have the same token stride")
+    if (q.shape == qs and q_out.shape == qs and q.dtype is bf16 and q_out.dtype is bf16 and q.is_contiguous() and q.is_cuda
+            and q_out.is_contiguous() and q_out.is_cuda):
+        qp, op, qst, ost = q.data_ptr(), q_out.data_ptr(), 0, 0
+    else:
+        qp, qst = _rows(q, "q", qs, bf16)
+        op, ost = _rows(q_out, "q_out", qs, bf16)
+    pp = _dev(position, "position", (plan.n_tokens,), plan._i32)
+    kp, vp, ksc, vsc = plan._pools(k_pool, v_pool, k_scale, v_scale)
+    st = (_lib or lib()).pad_chunk_append_rope(plan._h, rope._ref, pp, qp, qst, op, ost, kn, vn, ks, kp, vp, ksc, vsc,
+                                               _stream_handle(stream))
+    if st:
+        _check(st)
+
+
 def pad_chunk_read(plan: ChunkPlan, k_pool, v_pool, k_out, v_out, k_scale=None, v_scale=None, stream=None):
     """Copy every branch's cached tokens out as contiguous bf16 [n_cached, h_kv, head_dim]."""
     kp, vp, ksc, vsc = plan._pools(k_pool, v_pool, k_scale, v_scale)
@@ -652,6 +715,40 @@ def pad_chunk_attn(plan: ChunkPlan, q, k_prefix, v_prefix, k_pool, v_pool, out, 
         vx = _dev(v_prefix, "v_prefix", k_prefix.shape, plan._bf16)
     st = (_lib or lib()).pad_chunk_attn(plan._h, qp, qs, kx, vx, kp, vp, ksc, vsc, out.data_ptr(), lp,
                                         _stream_handle(stream))
+    if st:
+        _check(st)
+
+
+def pad_chunk_probs(plan: ChunkPlan, logits, p, params=None, history=None, history_len=None, tokens=None, bias_token=None,
+                    bias_value=None, bias_len=None, mask=None, stream=None):
+    """The step's logits [n_tokens, vocab] (fp32 or bf16) turned into the probabilities p (fp32 or bf16; may be logits itself) that
+    pad_draft_verify reads.  ``params`` [n_events, 4] fp32: temperature, repetition, frequency, presence.  ``history``
+    [n_events, width] int32 with ``history_len`` [n_events], ``tokens`` [n_tokens] int32: what counts as repeated.  ``bias_token``
+    int32 and ``bias_value`` fp32 [n_events, width] with ``bias_len`` [n_events].  ``mask`` [n_tokens, ceil(vocab / 32)] int32 words."""
+    f32, i32, n, ne = plan._f32, plan._i32, plan.n_tokens, plan.n_events
+    if logits.dim() != 2:
+        raise ValueError(f"logits: {tuple(logits.shape)}, expected [{n}, vocab]")
+    shape = (n, logits.shape[1])
+    lk, pk = (plan._bf16 if t.dtype is plan._bf16 else f32 for t in (logits, p))
+    if (logits.shape == shape and p.shape == shape and logits.dtype is lk and p.dtype is pk and logits.is_contiguous()
+            and logits.is_cuda and p.is_contiguous() and p.is_cuda):
+        lp, pp, ls, ps = logits.data_ptr(), p.data_ptr(), 0, 0
+    else:
+        lp, ls = _rows(logits, "logits", shape, lk)
+        pp, ps = _rows(p, "p", shape, pk)
+    if lp == pp and (lk is not pk or ls != ps):
+        raise ValueError("p: over logits, their types and strides must be the same")
+    hw = 0 if history is None else int(history.shape[-1])
+    bw = 0 if bias_token is None else int(bias_token.shape[-1])
+    hp, hl = _dev(history, "history", (ne, hw), i32), _dev(history_len, "history_len", (ne,), i32)
+    bt, bv = _dev(bias_token, "bias_token", (ne, bw), i32), _dev(bias_value, "bias_value", (ne, bw), f32)
+    bl = _dev(bias_len, "bias_len", (ne,), i32)
+    mp, ms = None, 0
+    if mask is not None:
+        mp, ms = _rows(mask, "mask", (n, -(-shape[1] // 32)), i32)
+    st = (_lib or lib()).pad_chunk_probs(plan._h, shape[1], int(lk is plan._bf16), lp, ls, _dev(params, "params", (ne, 4), f32),
+                                         _dev(tokens, "tokens", (n,), i32), hp, hw, hl, bt, bv, bw, bl, mp, ms,
+                                         int(pk is plan._bf16), pp, ps, _stream_handle(stream))
     if st:
         _check(st)
 

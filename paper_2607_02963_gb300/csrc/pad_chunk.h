@@ -90,6 +90,11 @@ int chunk_read_tokens();
 // them; an entry whose page is not in the pool becomes -1).
 cudaError_t launch_chunk_widen(const ChunkParams& p, int head_dim, const ChunkWiden* work, int n_events, int n_spans,
                                void* k_out, void* v_out, int32_t* table, int columns, cudaStream_t s);
+// Rotates q into q_out and k_new into the pools, v_new goes with it.  most: new tokens of the page that takes the most.
+cudaError_t launch_chunk_rope(const ChunkParams& p, int head_dim, int kv_format, const pad_rope& rope, const ChunkPages* work,
+                              int n_work, int most, int64_t n_tokens, int sms, const int32_t* position, const void* q, int64_t q_stride,
+                              void* q_out, int64_t out_stride, const void* k_new, const void* v_new, int64_t new_stride,
+                              void* k_pool, void* v_pool, uint8_t* k_scale, uint8_t* v_scale, cudaStream_t s);
 // rows16: 16-row groups that the items' rows take, 1 or 2.  early: not the call's first kernel.
 cudaError_t launch_chunk_mma(const ChunkParams& p, int head_dim, bool fp8, int rows16, bool early, const ChunkItem* items,
                              int n_items, cudaStream_t s);
@@ -106,6 +111,26 @@ cudaError_t launch_draft_verify(const ChunkParams& p, const ChunkVerify* work, i
                                 const void* tp, int64_t p_stride, const void* dq, int64_t q_stride,
                                 const int32_t* draft, const float* u_accept, const float* u_pick, int32_t* accepted,
                                 int32_t* token, cudaStream_t s);
+
+// The rows of logits of a plan's new tokens turned into probabilities.
+struct ChunkProbs {
+  const void* logits;
+  void* p;
+  int64_t logits_stride, p_stride;
+  const float* params;         // [n_events][4]: temperature, repetition, frequency, presence; or NULL
+  const int32_t* tokens;       // [n_tokens], or NULL
+  const int32_t* history;      // [n_events][history_width]
+  const int32_t* history_len;
+  const int32_t* bias_token;   // [n_events][bias_width]
+  const float* bias_value;
+  const int32_t* bias_len;
+  const uint32_t* mask;        // [n_tokens][mask_stride] words of 32 tokens, or NULL
+  int64_t mask_stride;
+  int32_t history_width, bias_width, vocab, n_events, longest;  // longest: tokens of the longest chunk
+  int32_t logits_bf16, p_bf16;
+};
+int chunk_probs_max_vocab();
+cudaError_t launch_chunk_probs(const ChunkProbs& a, const ChunkVerify* work, int n_tokens, cudaStream_t s);
 
 #ifdef __CUDACC__
 // Programmatic dependent launch, within one call: its first kernel is launched in plain stream order (its work

@@ -106,6 +106,7 @@ struct Lists {
   int64_t prefix_tokens = 0;             // of k_prefix, up to the last one read
   int64_t widen_pages = 0;
   int32_t widen_spans = 0, widen_columns = 0;
+  int32_t most_in_page = 0, longest = 0;  // new tokens of the page that takes the most, of the branch that brings the most
   int32_t n_spans = 0, pre_splits = 0, page_splits = 0;
   size_t off_tc = 0, off_pre = 0, off_page = 0, off_merge = 0, off_pages = 0, off_read = 0, off_verify = 0, off_widen = 0, image_bytes = 0;
   size_t off_ml = 0, off_o = 0, off_wtable = 0, off_wk = 0, off_wv = 0, total = 0;
@@ -288,10 +289,12 @@ void build(const Batch& b, const int64_t* prefix_offset, Lists& L) {
     for (int i = 0; i < n;) {
       const int pos = len + i, count = std::min(n - i, ps - pos % ps);
       L.pages.push_back({e, pos / ps, -1, tok0 + i, pos % ps, count});
+      L.most_in_page = std::max(L.most_in_page, count);
       i += count;
     }
     L.read.push_back({L.n_cached, L.n_spans, len + n});
     L.n_spans += (int32_t)(((int64_t)len + n + span - 1) / span);
+    L.longest = std::max(L.longest, n);
     L.verify.push_back({tok0, n - 1, (int32_t)L.n_drafts});
     L.n_tokens += n;
     L.n_cached += (int64_t)len + n;
@@ -452,6 +455,15 @@ pad_status check_stride(int64_t& stride, int64_t packed, int64_t unit, const cha
     return api_fail(PAD_ERR_INVALID_ARG, "%s stride %lld: at least %lld, a multiple of %lld", what, (long long)stride,
                     (long long)packed, (long long)unit);
   return PAD_OK;
+}
+
+// Whether `rows` rows of `width` elements at a and of `width_b` at b (bf16, strides in elements) share memory.
+bool overlap(const void* a, int64_t stride, int64_t width, const void* b, int64_t stride_b, int64_t width_b, int64_t rows) {
+  const intptr_t x = reinterpret_cast<intptr_t>(a) / 2, y = reinterpret_cast<intptr_t>(b) / 2;
+  if (x + (rows - 1) * stride + width <= y || y + (rows - 1) * stride_b + width_b <= x) return false;
+  if (stride != stride_b) return true;
+  const int64_t d = ((int64_t)(y - x) % stride + stride) % stride;  // columns of rows that lie one within the other
+  return d < width || d > stride - width_b;
 }
 
 }  // namespace
@@ -617,6 +629,140 @@ pad_status pad_chunk_append(const pad_chunk_t* c, const void* k_new, const void*
                                       list<ChunkPages>(c, c->L.off_pages), (int)c->L.pages.size(), k_new, v_new, new_stride,
                                       k_pool, v_pool, k_scale, v_scale, reinterpret_cast<cudaStream_t>(stream));
   return e == cudaSuccess ? PAD_OK : cuda_fail(e, "chunk append launch");
+}
+
+pad_status pad_rope_init(const pad_rope_spec* spec, pad_rope* rope) {
+  if (!spec || !rope) return api_fail(PAD_ERR_INVALID_ARG, "NULL argument");
+  const pad_rope_spec& s = *spec;
+  const double R = s.rotary_dim, pi = 3.14159265358979323846;
+  auto positive = [](double x) { return x > 0 && std::isfinite(x); };
+  if (s.head_dim != 64 && s.head_dim != 128) return api_fail(PAD_ERR_UNSUPPORTED, "head_dim=%d (supported: 64, 128)", s.head_dim);
+  if (s.rotary_dim < 2 || s.rotary_dim > s.head_dim || s.rotary_dim % 2 != 0)
+    return api_fail(PAD_ERR_INVALID_ARG, "rotary_dim=%d: even, 2 to head_dim=%d", s.rotary_dim, s.head_dim);
+  if (s.layout != PAD_ROPE_HALF && s.layout != PAD_ROPE_INTERLEAVED) return api_fail(PAD_ERR_INVALID_ARG, "layout=%d", s.layout);
+  if (s.scaling < PAD_ROPE_NONE || s.scaling > PAD_ROPE_INDEX) return api_fail(PAD_ERR_INVALID_ARG, "scaling=%d", s.scaling);
+  if (!positive(s.theta)) return api_fail(PAD_ERR_INVALID_ARG, "theta must be finite and > 0");
+  if (!std::isfinite(s.magnitude)) return api_fail(PAD_ERR_INVALID_ARG, "magnitude must be finite");
+  if (s.scaling != PAD_ROPE_NONE && !positive(s.factor)) return api_fail(PAD_ERR_INVALID_ARG, "factor must be finite and > 0");
+  if (s.scaling == PAD_ROPE_BASE && s.rotary_dim < 4) return api_fail(PAD_ERR_INVALID_ARG, "a scaled base needs a rotary_dim of 4 at least");
+  if (s.scaling == PAD_ROPE_TURNS || s.scaling == PAD_ROPE_INDEX) {
+    if (!positive(s.original_len)) return api_fail(PAD_ERR_INVALID_ARG, "original_len must be finite and > 0");
+    if (!(s.low < s.high) || !std::isfinite(s.low) || !std::isfinite(s.high)) return api_fail(PAD_ERR_INVALID_ARG, "low must be below high");
+    if (s.scaling == PAD_ROPE_INDEX && (!(s.low > 0) || !(s.theta > 1)))
+      return api_fail(PAD_ERR_INVALID_ARG, "a ramp over the index needs low > 0 and theta > 1");
+  }
+  double a = 0, b = 0;
+  if (s.scaling == PAD_ROPE_INDEX) {
+    auto index = [&](double n) { return R * std::log(s.original_len / (2 * pi * n)) / (2 * std::log(s.theta)); };
+    a = std::min(std::max(std::floor(index(s.high)), 0.0), R - 1);
+    b = std::min(std::max(std::ceil(index(s.low)), 0.0), R - 1);
+  }
+  const double theta = s.scaling == PAD_ROPE_BASE ? s.theta * std::pow(s.factor, R / (R - 2)) : s.theta;
+  pad_rope r{};
+  r.head_dim = s.head_dim;
+  r.rotary_dim = s.rotary_dim;
+  r.layout = s.layout;
+  r.magnitude = (float)s.magnitude;
+  for (int i = 0; i < s.rotary_dim / 2; ++i) {
+    double f = std::pow(theta, -2.0 * i / R), g = 1;
+    if (s.scaling == PAD_ROPE_LINEAR) g = 0;
+    if (s.scaling == PAD_ROPE_TURNS) g = (s.original_len * f / (2 * pi) - s.low) / (s.high - s.low);
+    if (s.scaling == PAD_ROPE_INDEX) g = 1 - (i - a) / std::max(b - a, 0.001);
+    g = std::min(std::max(g, 0.0), 1.0);
+    if (g < 1) f *= g + (1 - g) / s.factor;
+    // as a fraction of a turn: whole turns a token make no difference
+    const double turn = f / (2 * pi);
+    if (!std::isfinite(turn)) return api_fail(PAD_ERR_INVALID_ARG, "the frequency of pair %d is not finite", i);
+    const double part = std::ldexp(turn - std::floor(turn), 64);
+    r.turn[i] = part < 18446744073709551616.0 ? (uint64_t)part : 0;
+  }
+  *rope = r;
+  return PAD_OK;
+}
+
+pad_status pad_chunk_append_rope(const pad_chunk_t* c, const pad_rope* rope, const int32_t* position, const void* q,
+                                 int64_t q_stride, void* q_out, int64_t out_stride, const void* k_new, const void* v_new,
+                                 int64_t new_stride, void* k_pool, void* v_pool, uint8_t* k_scale, uint8_t* v_scale,
+                                 pad_stream_t stream) {
+  Range r("pad_chunk_append_rope");
+  pad_status st = check_launch(c, true);
+  if (st != PAD_OK) return st;
+  if (!rope) return api_fail(PAD_ERR_INVALID_ARG, "rope is NULL");
+  if (rope->head_dim != c->prob.head_dim || rope->rotary_dim < 2 || rope->rotary_dim > rope->head_dim || rope->rotary_dim % 2 != 0 ||
+      (rope->layout != PAD_ROPE_HALF && rope->layout != PAD_ROPE_INTERLEAVED))
+    return api_fail(PAD_ERR_INVALID_ARG, "rope is not of pad_rope_init for head_dim=%d", c->prob.head_dim);
+  const int64_t q_width = (int64_t)c->prob.h_q * c->prob.head_dim, new_width = (int64_t)c->prob.h_kv * c->prob.head_dim;
+  st = check_stride(q_stride, q_width, 8, "q");
+  if (st == PAD_OK) st = check_stride(out_stride, q_width, 8, "q_out");
+  if (st == PAD_OK) st = check_stride(new_stride, new_width, 8, "k_new");
+  if (st != PAD_OK) return st;
+  const int64_t n = c->L.n_tokens;
+  if (n == 0) return PAD_OK;
+  st = check_pools(c, k_pool, v_pool, k_scale, v_scale);
+  if (st != PAD_OK) return st;
+  if (!position || !aligned(position, 4)) return api_fail(PAD_ERR_INVALID_ARG, "position must be a 4-byte aligned tensor");
+  for (const void* t : {q, static_cast<const void*>(q_out), k_new, v_new})
+    if (!t || !aligned(t, 16)) return api_fail(PAD_ERR_INVALID_ARG, "q, q_out, k_new and v_new must be 16-byte aligned tensors");
+  if ((q_out != q || out_stride != q_stride) && overlap(q, q_stride, q_width, q_out, out_stride, q_width, n))
+    return api_fail(PAD_ERR_INVALID_ARG, "q_out overlaps q without being q");
+  if (overlap(k_new, new_stride, new_width, q_out, out_stride, q_width, n) || overlap(v_new, new_stride, new_width, q_out, out_stride, q_width, n))
+    return api_fail(PAD_ERR_INVALID_ARG, "q_out overlaps k_new or v_new");
+  const int sms = c->prob.num_sms > 0 ? c->prob.num_sms : api_num_sms();
+  cudaError_t e = launch_chunk_rope(params_of(c), c->prob.head_dim, c->kv_format, *rope, list<ChunkPages>(c, c->L.off_pages),
+                                    (int)c->L.pages.size(), c->L.most_in_page, n, sms, position, q, q_stride, q_out, out_stride,
+                                    k_new, v_new, new_stride, k_pool, v_pool, k_scale, v_scale, reinterpret_cast<cudaStream_t>(stream));
+  return e == cudaSuccess ? PAD_OK : cuda_fail(e, "chunk append with rotary positions launch");
+}
+
+pad_status pad_chunk_probs(const pad_chunk_t* c, int32_t vocab, int32_t logits_dtype, const void* logits, int64_t logits_stride,
+                           const float* params, const int32_t* tokens, const int32_t* history, int32_t history_width,
+                           const int32_t* history_len, const int32_t* bias_token, const float* bias_value, int32_t bias_width,
+                           const int32_t* bias_len, const int32_t* mask, int64_t mask_stride, int32_t p_dtype, void* p,
+                           int64_t p_stride, pad_stream_t stream) {
+  Range r("pad_chunk_probs");
+  pad_status st = check_launch(c, false);
+  if (st != PAD_OK) return st;
+  if (vocab < 1 || vocab > chunk_probs_max_vocab()) return api_fail(PAD_ERR_UNSUPPORTED, "vocab=%d outside [1, %d]", vocab, chunk_probs_max_vocab());
+  if ((logits_dtype != 0 && logits_dtype != 1) || (p_dtype != 0 && p_dtype != 1))
+    return api_fail(PAD_ERR_INVALID_ARG, "logits_dtype=%d, p_dtype=%d (0 = fp32, 1 = bf16)", logits_dtype, p_dtype);
+  st = check_stride(logits_stride, vocab, 1, "logits");
+  if (st == PAD_OK) st = check_stride(p_stride, vocab, 1, "p");
+  if (st == PAD_OK) st = check_stride(mask_stride, (vocab + 31) / 32, 1, "mask");
+  if (st != PAD_OK) return st;
+  if (history_width < 0 || bias_width < 0) return api_fail(PAD_ERR_INVALID_ARG, "negative width");
+  if (!history != !history_len) return api_fail(PAD_ERR_INVALID_ARG, "history and history_len come together");
+  if (!bias_token != !bias_value || !bias_token != !bias_len) return api_fail(PAD_ERR_INVALID_ARG, "bias_token, bias_value and bias_len come together");
+  if (c->L.n_tokens == 0) return PAD_OK;
+  if (!logits || !p) return api_fail(PAD_ERR_INVALID_ARG, "NULL tensor");
+  for (const void* t : {static_cast<const void*>(params), static_cast<const void*>(tokens), static_cast<const void*>(history),
+                        static_cast<const void*>(history_len), static_cast<const void*>(bias_token), static_cast<const void*>(bias_value),
+                        static_cast<const void*>(bias_len), static_cast<const void*>(mask)})
+    if (!aligned(t, 4)) return api_fail(PAD_ERR_INVALID_ARG, "a tensor is not aligned to its elements");
+  if (!aligned(logits, logits_dtype ? 2 : 4) || !aligned(p, p_dtype ? 2 : 4))
+    return api_fail(PAD_ERR_INVALID_ARG, "a tensor is not aligned to its elements");
+  ChunkProbs a{};
+  a.logits = logits;
+  a.p = p;
+  a.logits_stride = logits_stride;
+  a.p_stride = p_stride;
+  a.params = params;
+  a.tokens = tokens;
+  a.history = history;
+  a.history_len = history_len;
+  a.bias_token = bias_token;
+  a.bias_value = bias_value;
+  a.bias_len = bias_len;
+  a.mask = reinterpret_cast<const uint32_t*>(mask);
+  a.mask_stride = mask_stride;
+  a.history_width = history_width;
+  a.bias_width = bias_width;
+  a.vocab = vocab;
+  a.n_events = c->n_events;
+  a.longest = c->L.longest;
+  a.logits_bf16 = logits_dtype;
+  a.p_bf16 = p_dtype;
+  cudaError_t e = launch_chunk_probs(a, list<ChunkVerify>(c, c->L.off_verify), (int)c->L.n_tokens, reinterpret_cast<cudaStream_t>(stream));
+  return e == cudaSuccess ? PAD_OK : cuda_fail(e, "logits to probabilities launch");
 }
 
 pad_status pad_chunk_read(const pad_chunk_t* c, const void* k_pool, const void* v_pool, const uint8_t* k_scale,

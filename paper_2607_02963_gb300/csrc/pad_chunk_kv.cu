@@ -15,13 +15,12 @@
 // Bound by memory, one pass each; short ones by the launch.  32768 tokens of 4 heads x 128 written and read back
 // (two calls of 101 MB): 45 us, 4.5 TB/s; 32 branches x 5 tokens written and 9000 read: 12 us.
 #include <cuda_bf16.h>
-#include <cuda_fp16.h>
-#include <cuda_fp8.h>
 #include <algorithm>
 #include <cstdint>
 #include <type_traits>
 
 #include "pad_chunk.h"
+#include "pad_chunk_quant.cuh"
 
 namespace pad {
 
@@ -29,37 +28,6 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kReadTokens = 32;  // of a span
-
-// The 4-bit codes of eight values with scale byte `byte`.  x / s is x times the rounded 1 / s, 2^-22 off at most, rounded
-// to f16 on the way: x has eight significant bits and s four, so that x / s either is a number half way between two
-// codes (three significant bits), which f16 restores, or is 2^-8 of itself away from every one, further than f16 moves it.
-__device__ __forceinline__ uint32_t e2m1_codes(const uint32_t (&x)[4], uint32_t byte) {
-  const float s = (byte >> 3) ? __uint_as_float((byte + 896u) << 20) : (float)byte * 0x1p-17f;
-  const float inv = byte == 0u ? 0.f : 1.f / s;
-  float y[8];
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const __half2 h = __floats2half2_rn(__uint_as_float(x[j] << 16) * inv, __uint_as_float(x[j] & 0xffff0000u) * inv);
-    y[2 * j] = __low2float(h);
-    y[2 * j + 1] = __high2float(h);
-  }
-  uint32_t r;
-  asm("{\n .reg .b8 a, b, c, d;\n"
-      " cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n cvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n"
-      " cvt.rn.satfinite.e2m1x2.f32 c, %6, %5;\n cvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n"
-      " mov.b32 %0, {a, b, c, d};\n}\n"
-      : "=r"(r) : "f"(y[0]), "f"(y[1]), "f"(y[2]), "f"(y[3]), "f"(y[4]), "f"(y[5]), "f"(y[6]), "f"(y[7]));
-  return r;
-}
-// The scale byte of a group whose largest magnitude has this bf16 pattern: max / 6 (no tie is moved by that division's
-// rounding: the quotient of an eight-bit number by 3 that lies half way between two scales is exact) to the nearest.
-__device__ __forceinline__ uint32_t e2m1_scale(uint32_t m) {
-  if (m >= 0x7f80u) return 255u;
-  const float s = __fdiv_rn(__uint_as_float(m << 16), 6.f);
-  const uint32_t u = __float_as_uint(s);
-  const uint32_t b = s < 0x1p-14f ? (uint32_t)rintf(s * 0x1p17f) : ((u + 0x7ffffu + ((u >> 20) & 1u)) >> 20) - 896u;
-  return min(b, 226u);
-}
 
 // 16 lanes of 8 bf16 values (8 at head_dim 64) hold a token and head: one 8-bit group, or a 4-bit one for two lanes.
 template <int D, int FMT>
@@ -98,47 +66,7 @@ __global__ void __launch_bounds__(kThreads) chunk_append_kernel(const __grid_con
       const int g = (i0 + u * kThreads) / L, tok = g / (2 * p.h_kv), r = g % (2 * p.h_kv), h = r >> 1;
       const bool on = g < groups;
       const int64_t slot = ((int64_t)page * p.h_kv + h) * p.page_size + w.slot + tok;
-      if (FMT == PAD_KV_BF16) {
-        if (on) *(reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>((r & 1) ? v_pool : k_pool) + slot * D) + c) = x[u];
-        continue;
-      }
-      // the largest magnitude as a bf16 pattern: integer order is theirs, NaN and infinity on top
-      uint32_t m = 0u;
-      const uint32_t xs[4] = {x[u].x, x[u].y, x[u].z, x[u].w};
-#pragma unroll
-      for (int j = 0; j < 4; ++j) m = max(m, max(xs[j] & 0x7fffu, (xs[j] >> 16) & 0x7fffu));
-#pragma unroll
-      for (int o = FMT == PAD_KV_FP4 ? 1 : L / 2; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
-      if (FMT == PAD_KV_FP4) {
-        const uint32_t byte = e2m1_scale(m);
-        if (on) {
-          static_cast<uint32_t*>((r & 1) ? v_pool : k_pool)[slot * (D / 8) + c] = byte == 255u ? 0u : e2m1_codes(xs, byte);
-          if (!(c & 1)) ((r & 1) ? v_scale : k_scale)[slot * (D / 16) + (c >> 1)] = (uint8_t)byte;
-        }
-        continue;
-      }
-      // max = f * 2^(e - 127) with f in [1, 2): max <= 448 * 2^k = 1.75 * 2^(k + 8).  (A subnormal's k
-      // is below the range in any case.)
-      const int e = (int)(m >> 7);
-      const int k = min(max(e - 127 - 8 + ((m & 0x7fu) > 0x60u ? 1 : 0), -120), 7);
-      const bool bad = m >= 0x7f80u;
-      const float inv = __uint_as_float((uint32_t)(127 - k) << 23);  // 2^-k
-      uint32_t code[2];
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        uint32_t two[2];
-#pragma unroll
-        for (int q = 0; q < 2; ++q) {
-          const uint32_t v = xs[2 * j + q];
-          const float2 f = make_float2(__uint_as_float(v << 16) * inv, __uint_as_float(v & 0xffff0000u) * inv);
-          two[q] = bad ? 0u : __nv_cvt_float2_to_fp8x2(f, __NV_SATFINITE, __NV_E4M3);  // (codes are finite, always)
-        }
-        code[j] = two[0] | (two[1] << 16);
-      }
-      if (on) {
-        *(reinterpret_cast<uint2*>(static_cast<uint8_t*>((r & 1) ? v_pool : k_pool) + slot * D) + c) = make_uint2(code[0], code[1]);
-        if (c == 0) ((r & 1) ? v_scale : k_scale)[slot] = (uint8_t)(bad ? 255 : m == 0u ? 0 : k + 127);
-      }
+      store_group<D, FMT>(x[u], c, on, slot, (r & 1) ? v_pool : k_pool, (r & 1) ? v_scale : k_scale);
     }
   }
 }

@@ -1,9 +1,9 @@
 """Speculative steps of event branches: drafted tokens of every branch are written into the paged cache, attended
 together, verified against the target's probabilities, and the branches advance by what was kept.
 
-``BranchCache`` holds what a program keeps for one attention layer (pools in bf16 or 8 bits, page table, page
-bookkeeping, lengths); a step is ``plan`` -> ``append`` -> ``attend`` -> ``verify`` -> ``commit``, each one call of the
-C ABI.  A model of many layers shares one plan and page table among its layers' pools.
+``BranchCache`` holds what a program keeps for one attention layer (pools in bf16, 8 or 4 bits, page table, page
+bookkeeping, lengths); a step is ``plan`` -> ``append`` (or ``append_rope``) -> ``attend`` -> ``probs`` -> ``verify`` ->
+``commit``, each one call of the C ABI.  A model of many layers shares one plan and page table among its layers' pools.
 
     python -m paper_2607_02963_gb300.speculative        (a GPU; synthetic tensors, no model)
 
@@ -25,12 +25,13 @@ class BranchCache:
         self.problem = B.make_problem(h_q, h_kv, head_dim, page_size, out_dtype=out_dtype)
         self.kv_format, self.device = kv_format, torch.device(device)
         self.prefix_len, self.event_video = prefix_len, event_video
-        shape = (n_pages, h_kv, page_size, head_dim)
-        kind = torch.uint8 if kv_format == B.KV_FP8 else torch.bfloat16
-        self.k_pool, self.v_pool = (torch.zeros(shape, dtype=kind, device=self.device) for _ in range(2))
+        shape, kind = (n_pages, h_kv, page_size), torch.bfloat16 if kv_format == B.KV_BF16 else torch.uint8
+        row = head_dim // 2 if kv_format == B.KV_FP4 else head_dim
+        self.k_pool, self.v_pool = (torch.zeros(shape + (row,), dtype=kind, device=self.device) for _ in range(2))
         self.k_scale = self.v_scale = None
-        if kv_format == B.KV_FP8:
-            self.k_scale, self.v_scale = (torch.zeros(shape[:3], dtype=torch.uint8, device=self.device) for _ in range(2))
+        if kv_format != B.KV_BF16:
+            scales = shape + ((head_dim // 16,) if kv_format == B.KV_FP4 else ())
+            self.k_scale, self.v_scale = (torch.zeros(scales, dtype=torch.uint8, device=self.device) for _ in range(2))
         self.page_table = torch.full((n_events, max_pages), -1, dtype=torch.int32, device=self.device)
         self.pages = B.CacheState(n_pages)
         self.event_len = np.zeros(n_events, dtype=np.int32)
@@ -50,6 +51,12 @@ class BranchCache:
     def append(self, plan, k_new, v_new):
         B.pad_chunk_append(plan, k_new, v_new, self.k_pool, self.v_pool, self.k_scale, self.v_scale)
 
+    def append_rope(self, plan, rope, position, q, k_new, v_new, q_out=None):
+        """append with rotary positions; returns the turned queries (``q_out``, which may be q)."""
+        q_out = torch.empty_like(q, memory_format=torch.contiguous_format) if q_out is None else q_out
+        B.pad_chunk_append_rope(plan, rope, position, q, q_out, k_new, v_new, self.k_pool, self.v_pool, self.k_scale, self.v_scale)
+        return q_out
+
     def attend(self, plan, q, k_prefix=None, v_prefix=None, out=None, lse=None):
         if out is None:
             kind = torch.bfloat16 if self.problem.out_dtype == 1 else torch.float32
@@ -63,6 +70,12 @@ class BranchCache:
         k, v = (torch.empty(shape, dtype=torch.bfloat16, device=self.device) for _ in range(2))
         B.pad_chunk_read(plan, self.k_pool, self.v_pool, k, v, self.k_scale, self.v_scale)
         return k, v
+
+    def probs(self, plan, logits, **context):
+        """The probabilities that ``verify`` reads, from the model's logits (pad_chunk_probs's arguments by name)."""
+        p = torch.empty(logits.shape, dtype=logits.dtype, device=self.device)
+        B.pad_chunk_probs(plan, logits, p, **context)
+        return p
 
     def verify(self, plan, p, q, draft, u_accept, u_pick):
         """(accepted, token) of every branch, on the device."""
