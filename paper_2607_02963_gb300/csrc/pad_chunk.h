@@ -101,6 +101,7 @@ cudaError_t launch_chunk_mma(const ChunkParams& p, int head_dim, bool fp8, int r
 // The same over 4-bit pages; rows8: groups of eight rows, 1 to 4.
 cudaError_t launch_chunk_mma4(const ChunkParams& p, int head_dim, int rows8, bool early, const ChunkItem* items, int n_items,
                               cudaStream_t s);
+int chunk_mma4_ctas(int head_dim, int rows8);  // that an SM takes
 // split: one slot of 128 / group tokens per CTA, its tiles taken in turn by two halves; else two slots.
 // prefix_tokens: tokens of k_prefix up to the last one that an item reads, 0 without prefix items.
 cudaError_t launch_chunk_tc(const ChunkParams& p, int head_dim, bool fp8, bool split, int64_t prefix_tokens,

@@ -135,7 +135,9 @@ void split_by(Segment& s, int64_t len, int64_t unit) {
 // SM), and key ranges are cut so that there are some eight CTAs for each SM, no shorter than
 // kMinSplit keys.  (16 x 1 token over 333k cached tokens, 28/4 heads: 121 us in bf16 and 91 in 8 bits; with four CTAs
 // for each SM 127 and 98, with sixteen 133 and 110.  128 or 512 keys make no difference beyond a short call's noise.)
-// 4-bit pages: tiles of eight rows, up to four; a branch of more rows in pieces of about as many tokens.
+// 4-bit pages: tiles of eight rows, up to four; a branch of more rows in pieces of about as many tokens.  The ranges there
+// are the shortest that make no more CTAs than fit the GPU at once: a CTA's start and end cost as much as two of
+// its blocks, and a few CTAs beyond one wave as much as the wave.
 void cut_mma(std::vector<Segment>& segs, int paged, const pad_problem& prob, bool fp4, int sms, int& rows, int& tpt) {
   const int G = prob.h_q / prob.h_kv;
   int longest = 1;
@@ -150,10 +152,26 @@ void cut_mma(std::vector<Segment>& segs, int paged, const pad_problem& prob, boo
     tpt = 16 * rows / G;
   }
   double work = 0;
+  int64_t least = 0, longest_keys = 0;  // CTAs if nothing is cut
   for (const Segment& s : segs)
-    if (!s.tc && s.paged == paged) work += (double)((s.ntok + tpt - 1) / tpt) * s.keys * prob.h_kv;
-  const double per = work / (8.0 * sms);
-  const int64_t len = std::max<int64_t>(kMinSplit, ((int64_t)(per / kSplitUnit) + 1) * kSplitUnit);
+    if (!s.tc && s.paged == paged) {
+      const int64_t n = (int64_t)((s.ntok + tpt - 1) / tpt) * prob.h_kv;
+      work += (double)n * s.keys;
+      least += n;
+      longest_keys = std::max<int64_t>(longest_keys, s.keys);
+    }
+  double per = work / (8.0 * sms);
+  const int64_t slots = fp4 ? (int64_t)chunk_mma4_ctas(prob.head_dim, rows) * sms : 0;
+  if (least <= slots) per = work / (double)slots;
+  int64_t len = std::max<int64_t>(kMinSplit, ((int64_t)(per / kSplitUnit) + 1) * kSplitUnit);
+  auto ctas = [&]() {
+    int64_t n = 0;
+    for (const Segment& s : segs)
+      if (!s.tc && s.paged == paged) n += (int64_t)((s.ntok + tpt - 1) / tpt) * prob.h_kv * ((s.keys + len - 1) / len);
+    return n;
+  };
+  if (least <= slots)
+    while (len < longest_keys && ctas() > slots) len += std::max<int64_t>(1, len / (16 * kSplitUnit)) * kSplitUnit;
   for (Segment& s : segs)
     if (!s.tc && s.paged == paged) split_by(s, len, kSplitUnit);
 }

@@ -40,17 +40,15 @@ constexpr float kNegInf = -__builtin_huge_valf();
 constexpr float kLn2 = 0.69314718055994531f;
 constexpr float kUp = 15.f;       // weights are held as 2^15 times themselves
 
-// A warp's stages.
+// A warp's stages: the codes and scales of a block as they lie in the pages.
 template <int D, int NT>
 struct Ring {
   static constexpr int kRow = D / 2;                        // bytes of a key's codes,
   static constexpr int kScales = D / 16;                    // and of its scales
-  static constexpr int kPitchV = D == 128 ? 80 : 48;        // (keys two apart start on other banks)
   static constexpr int kV = kBlk * kRow;
-  static constexpr int kSK = kV + kBlk * kPitchV;
+  static constexpr int kSK = 2 * kV;
   static constexpr int kSV = kSK + kBlk * kScales;
-  static constexpr int kMask = kSV + kBlk * kScales;        // which keys are there
-  static constexpr int kStage = kMask + 16;
+  static constexpr int kStage = kSV + kBlk * kScales;
   static constexpr int kStages = 3;
   static constexpr int kWarpBytes = kStages * kStage;
 };
@@ -61,12 +59,15 @@ constexpr int smem_bytes() {
   constexpr int join = kWarps * 8 * NT * (D + 2) * 4;
   return ring > join ? ring : join;
 }
-template <int NT>
-constexpr int ctas_per_sm() { return NT == 1 ? 4 : NT == 2 ? 3 : 2; }
+template <int D, int NT>
+constexpr int ctas_per_sm() { return D == 128 ? (NT == 1 ? 4 : NT == 2 ? 3 : 2) : (NT <= 2 ? 4 : 3); }
 
 __device__ __forceinline__ void cp16(uint32_t dst, const void* src, uint32_t n) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
 }
+// The key of a 16-key group that row r of S^T stands for: two keys apart lie on the same banks, and the lanes that read
+// K rows together differ in g, those that read V rows together in t.
+__device__ __forceinline__ int key_of(int r) { return r ^ ((r >> 1) & 1); }
 __device__ __forceinline__ void mma_f16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
   asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
@@ -81,6 +82,10 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
   const __half2 h = __floats2half2_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&h);
 }
+// Of the keys of a block that are there, the first `keys`.
+__device__ __forceinline__ uint32_t seen(uint32_t there, int keys) {
+  return there & (keys >= kBlk ? 0xffffffffu : keys <= 0 ? 0u : (1u << keys) - 1u);
+}
 // A scale byte as f16 in both halves, and two of them.
 __device__ __forceinline__ uint32_t scale2(uint32_t byte) { return byte * 0x800080u; }
 __device__ __forceinline__ uint32_t scale_pair(uint32_t lo, uint32_t hi) { return (lo << 7) | (hi << 23); }
@@ -92,7 +97,7 @@ __device__ __forceinline__ int swap(int row) {
 }
 
 template <int D, int NT>
-__global__ void __launch_bounds__(kThreads, ctas_per_sm<NT>()) chunk_mma4_kernel(const __grid_constant__ ChunkParams p,
+__global__ void __launch_bounds__(kThreads, (ctas_per_sm<D, NT>())) chunk_mma4_kernel(const __grid_constant__ ChunkParams p,
                                                                                  const ChunkItem* __restrict__ items) {
   using R = Ring<D, NT>;
   constexpr int kRows = 8 * NT, W = D / 32, MT = D / 16;  // words of a lane's K, 16-column tiles of O
@@ -110,51 +115,46 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm<NT>()) chunk_mma4_kernel
   const int n_blocks = it.key1 > it.key0 ? (it.key1 - it.key0 + kBlk - 1) / kBlk : 0;
   const int mine = n_blocks > warp ? (n_blocks - warp + kWarps - 1) / kWarps : 0;
   const int32_t* table = p.page_table + it.src * p.max_pages;
-  const uint32_t per_page = (uint32_t)(p.h_kv * p.page_size);     // rows of a page
-  const int64_t row0 = (int64_t)h * p.page_size;
+  // (rows of a pool are counted in 32 bits; the launcher sees to it)
+  const uint32_t per_page = (uint32_t)(p.h_kv * p.page_size), row0 = (uint32_t)(h * p.page_size);
+  const uint32_t some = p.n_pages > 0 ? 16u : 0u;  // (keys that are not there come as whatever row 0 holds)
+  constexpr int CH = R::kRow / 16, RPI = 32 / CH, kIter = kBlk / RPI;   // 16-byte pieces of a row, rows of an instruction
+  constexpr int kPer = 16 / R::kScales, kLanes = kBlk / kPer;           // keys whose scales make 16 bytes (they share a page)
+  const uint8_t* kb = static_cast<const uint8_t*>(p.k_pool) + 16 * (lane % CH);
+  const uint8_t* vb = static_cast<const uint8_t*>(p.v_pool) + 16 * (lane % CH);
+  const uint8_t* sb = lane < kLanes ? p.k_scale : p.v_scale;
+  const uint32_t to = ring_at + 16 * lane, sto = ring_at + (lane < kLanes ? R::kSK : R::kSV) + 16 * (lane % kLanes);
 
   // page of this lane's key of the warp's i-th block
   auto page_of = [&](int i) -> int {
     const int key = it.key0 + (warp + kWarps * i) * kBlk + lane;
-    return i < mine && key < it.key1 ? __ldcg(table + (key >> p.page_shift)) : 0;
+    return i < mine && key < it.key1 ? __ldcg(table + (key >> p.page_shift)) : -1;
   };
-  auto issue = [&](int i, int page, int stage) {
-    if (i >= mine) return;
-    const uint32_t st = ring_at + stage * R::kStage;
-    const int k0 = it.key0 + (warp + kWarps * i) * kBlk, key = k0 + lane;
-    bool ok = key < it.key1;
-    if (ok && (unsigned)page >= (unsigned)p.n_pages) {
-      ok = false;
-      pad_set_error(p.header, p.gen, PAD_ERR_DEVICE_BOUNDS, (int)it.src, key >> p.page_shift, page);
-    }
-    const uint32_t there = __ballot_sync(0xffffffffu, ok);
-    // the lane's key: row of the pools
-    const int64_t mine_at = ok ? row0 + (int64_t)page * per_page + (key & (p.page_size - 1)) : 0;
-    constexpr int CH = R::kRow / 16, RPI = 32 / CH, kIter = kBlk / RPI;
-    const int r0 = lane / CH, c = lane % CH;
+  // Fetches the block; returns which of its keys are there.
+  auto issue = [&](int i, int page, int stage) -> uint32_t {
+    if (i >= mine) return 0u;
+    const int key = it.key0 + (warp + kWarps * i) * kBlk + lane;
+    const bool ok = (unsigned)page < (unsigned)p.n_pages;
+    if (!ok && key < it.key1) pad_set_error(p.header, p.gen, PAD_ERR_DEVICE_BOUNDS, (int)it.src, key >> p.page_shift, page);
+    const uint32_t row = ok ? row0 + (uint32_t)page * per_page + (uint32_t)(key & (p.page_size - 1)) : 0u;
+    const uint32_t at = stage * R::kStage;
 #pragma unroll
     for (int j = 0; j < kIter; ++j) {
-      const int row = j * RPI + r0;
-      const uint32_t on = (there >> row) & 1u;
-      const int64_t off = __shfl_sync(0xffffffffu, mine_at, row) * R::kRow + 16 * c;
-      cp16(st + row * R::kRow + 16 * c, static_cast<const uint8_t*>(p.k_pool) + off, on * 16u);
-      cp16(st + R::kV + row * R::kPitchV + 16 * c, static_cast<const uint8_t*>(p.v_pool) + off, on * 16u);
+      const uint64_t off = (uint64_t)__shfl_sync(0xffffffffu, row, j * RPI + lane / CH) * R::kRow;
+      cp16(to + at + 512 * j, kb + off, some);
+      cp16(to + at + R::kV + 512 * j, vb + off, some);
     }
-    // scales: 16 bytes hold those of a few keys, which share a page; what lies past the last of them stays out
-    constexpr int per = 16 / R::kScales, kLanes = kBlk / per;
-    const int first = (lane % kLanes) * per;
-    const int64_t at = __shfl_sync(0xffffffffu, mine_at, first) * R::kScales;
-    const uint32_t bytes = (uint32_t)__popc((there >> first) & ((1u << per) - 1u)) * R::kScales;
-    if (lane < 2 * kLanes)
-      cp16(st + (lane < kLanes ? R::kSK : R::kSV) + 16 * (lane % kLanes), (lane < kLanes ? p.k_scale : p.v_scale) + at, bytes);
-    if (lane == 0) *reinterpret_cast<uint32_t*>(ring + stage * R::kStage + R::kMask) = there;
+    const uint64_t off = (uint64_t)__shfl_sync(0xffffffffu, row, (lane % kLanes) * kPer) * R::kScales;
+    if (lane < 2 * kLanes) cp16(sto + at, sb + off, some);
+    return __ballot_sync(0xffffffffu, ok);
   };
 
+  uint32_t keys_in[R::kStages];  // of the blocks under way, the next one's first
   int page = page_of(0);
 #pragma unroll
   for (int i = 0; i < R::kStages - 1; ++i) {
     const int next = page_of(i + 1);
-    issue(i, page, i);
+    keys_in[i] = issue(i, page, i);
     asm volatile("cp.async.commit_group;" ::: "memory");
     page = next;
   }
@@ -184,7 +184,7 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm<NT>()) chunk_mma4_kernel
     // whatever the scale)
     const int e = min(max((int)(top >> 7) - 127 - 14, -120), 113);
     const float down = __uint_as_float((uint32_t)(127 - e) << 23);
-    const float back = p.scale_log2 * __uint_as_float((uint32_t)(127 + e) << 23);
+    const float back = fmaxf(p.scale_log2 * __uint_as_float((uint32_t)(127 + e) << 23), 1e-45f);  // (0 would make a NaN of -inf)
 #pragma unroll
     for (int j = 0; j < W; ++j) {
       const uint32_t xs[4] = {x[j].x, x[j].y, x[j].z, x[j].w};
@@ -214,89 +214,114 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm<NT>()) chunk_mma4_kernel
   }
 
   int s_use = 0, s_fill = R::kStages - 1;  // the stages of this block and of the one being fetched
+  const int kg = key_of(g);
 #pragma unroll 1
   for (int i = 0; i < mine; ++i) {
     {
       const int next = page_of(i + R::kStages);
-      issue(i + R::kStages - 1, page, s_fill);
+      keys_in[R::kStages - 1] = issue(i + R::kStages - 1, page, s_fill);
       asm volatile("cp.async.commit_group;" ::: "memory");
       page = next;
       s_fill = s_fill == R::kStages - 1 ? 0 : s_fill + 1;
     }
     asm volatile("cp.async.wait_group %0;" ::"n"(R::kStages - 1) : "memory");
     __syncwarp();
-    const uint8_t* st = ring + s_use * R::kStage;
+    uint8_t* st = ring + s_use * R::kStage;
     s_use = s_use == R::kStages - 1 ? 0 : s_use + 1;
-    const uint32_t there = *reinterpret_cast<const uint32_t*>(st + R::kMask);
+    const uint32_t there = keys_in[0];
+#pragma unroll
+    for (int j = 0; j + 1 < R::kStages; ++j) keys_in[j] = keys_in[j + 1];
     const int k0 = it.key0 + (warp + kWarps * i) * kBlk;
 
-    // S^T: keys 16 m + g (and + 8) of the block, rows 8 n + 2 t4 (and + 1)
-    float s[NT][2][4];
+    // S^T: keys 16 m + key_of(g) (and + 8) of the block, rows 8 n + 2 t4 (and + 1)
+    // (NT 1: two sums each, of every other step, so that four chains of products are under way)
+    constexpr int CHAINS = NT == 1 ? 2 : 1;
+    float s[NT][2][4], s2[CHAINS][NT][2][4];
+    uint32_t kw[2][2][W], ks[2][2][W / 2];
 #pragma unroll
     for (int m = 0; m < 2; ++m) {
 #pragma unroll
-      for (int n = 0; n < NT; ++n)
+      for (int c = 0; c < CHAINS; ++c)
 #pragma unroll
-        for (int u = 0; u < 4; ++u) s[n][m][u] = 0.f;
-      uint32_t w[2][W], sc[2][W / 2];
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int u = 0; u < 4; ++u) s2[c][n][m][u] = 0.f;
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
-        const int key = 16 * m + 8 * u + g;
+        const int key = 16 * m + 8 * u + kg;
         const uint8_t* a = st + key * R::kRow + 4 * W * t4;
         const uint8_t* b = st + R::kSK + key * R::kScales + (W / 2) * t4;
         if constexpr (W == 4) {
           const uint4 v = *reinterpret_cast<const uint4*>(a);
-          w[u][0] = v.x, w[u][1] = v.y, w[u][2] = v.z, w[u][3] = v.w;
+          kw[m][u][0] = v.x, kw[m][u][1] = v.y, kw[m][u][2] = v.z, kw[m][u][3] = v.w;
           const uint32_t two = *reinterpret_cast<const uint16_t*>(b);
-          sc[u][0] = scale2(two & 255u), sc[u][1] = scale2(two >> 8);
+          ks[m][u][0] = scale2(two & 255u), ks[m][u][1] = scale2(two >> 8);
         } else {
           const uint2 v = *reinterpret_cast<const uint2*>(a);
-          w[u][0] = v.x, w[u][1] = v.y;
-          sc[u][0] = scale2(*b);
+          kw[m][u][0] = v.x, kw[m][u][1] = v.y;
+          ks[m][u][0] = scale2(*b);
         }
       }
+    }
 #pragma unroll
-      for (int j = 0; j < W; ++j) {
+    for (int j = 0; j < W; ++j)
+#pragma unroll
+      for (int m = 0; m < 2; ++m) {
         uint32_t x[2][4];
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-          f16_of_e2m1(w[u][j], x[u]);
+          f16_of_e2m1(kw[m][u][j], x[u]);
 #pragma unroll
-          for (int q = 0; q < 4; ++q) x[u][q] = f16_times(x[u][q], sc[u][j / 2]);
+          for (int q = 0; q < 4; ++q) x[u][q] = f16_times(x[u][q], ks[m][u][j / 2]);
         }
 #pragma unroll
         for (int q = 0; q < 2; ++q) {
           const uint32_t a[4] = {x[0][2 * q], x[1][2 * q], x[0][2 * q + 1], x[1][2 * q + 1]};
 #pragma unroll
-          for (int n = 0; n < NT; ++n) mma_f16(s[n][m], a, qf[n][2 * j + q][0], qf[n][2 * j + q][1]);
+          for (int n = 0; n < NT; ++n) mma_f16(s2[q % CHAINS][n][m], a, qf[n][2 * j + q][0], qf[n][2 * j + q][1]);
         }
       }
-    }
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int m = 0; m < 2; ++m)
+#pragma unroll
+        for (int u = 0; u < 4; ++u) s[n][m][u] = CHAINS == 2 ? s2[0][n][m][u] + s2[CHAINS - 1][n][m][u] : s2[0][n][m][u];
 
-    // a block that every row sees in full needs no mask
-    const bool full = there == 0xffffffffu && k0 + kBlk <= lim_all;
-    uint32_t hides[NT][2];  // keys of the block that each row does not see
+    // A block that some row does not see in full: hidden scores are replaced.  A weight of 0 times a scale that is not finite is
+    // not 0: in such a block those scales become 0, as those of keys that are not there, and the rows that see
+    // them get their NaN at the end of it.
+    uint32_t nan_keys = 0u;  // of the lane's column group
+    if (there != 0xffffffffu || k0 + kBlk > lim_all) {
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const uint32_t sees = seen(there, lim[n][u] - k0);
+#pragma unroll
+          for (int m = 0; m < 2; ++m)
+#pragma unroll
+            for (int v = 0; v < 2; ++v)
+              if (!((sees >> (16 * m + 8 * v + kg)) & 1u)) s[n][m][2 * v + u] = kNegInf;
+        }
+      const bool in = (there >> lane) & 1u;
+#pragma unroll
+      for (int j = 0; j < R::kScales; ++j) {
+        uint8_t* b = st + R::kSV + R::kScales * lane + j;
+        const bool odd = in && *b > 226u;
+        const uint32_t which = __ballot_sync(0xffffffffu, odd);
+        if ((W == 4 ? g : g >> 1) == j) nan_keys = which;
+        if (!in || odd) *b = 0;
+      }
+      __syncwarp();
+    }
     bool grow = false;
     float top[NT][2];
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
-        hides[n][u] = 0u;
-        if (!full) {
-          const int keys = lim[n][u] - k0;
-          hides[n][u] = ~(there & (keys >= kBlk ? 0xffffffffu : keys <= 0 ? 0u : (1u << keys) - 1u));
-        }
-        top[n][u] = kNegInf;
-#pragma unroll
-        for (int m = 0; m < 2; ++m)
-#pragma unroll
-          for (int v = 0; v < 2; ++v) {
-            float& x = s[n][m][2 * v + u];
-            x *= qs[n][u];
-            if (!full && ((hides[n][u] >> (16 * m + 8 * v + g)) & 1u)) x = kNegInf;
-            top[n][u] = fmaxf(top[n][u], x);
-          }
+        top[n][u] = fmaxf(tc::max3f(s[n][0][u], s[n][0][2 + u], s[n][1][u]), s[n][1][2 + u]) * qs[n][u];
         grow |= top[n][u] > mx[n][u];
       }
     // (the maximum of few blocks is above all before them)
@@ -321,37 +346,26 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm<NT>()) chunk_mma4_kernel
     uint32_t pf[NT][2][2];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-      const float base[2] = {mx[n][0] == kNegInf ? 0.f : mx[n][0] - kUp, mx[n][1] == kNegInf ? 0.f : mx[n][1] - kUp};
+      const float up[2] = {mx[n][0] == kNegInf ? 0.f : kUp - mx[n][0], mx[n][1] == kNegInf ? 0.f : kUp - mx[n][1]};
 #pragma unroll
       for (int m = 0; m < 2; ++m)
 #pragma unroll
         for (int v = 0; v < 2; ++v) {
-          const float a = ex2(s[n][m][2 * v] - base[0]), b = ex2(s[n][m][2 * v + 1] - base[1]);
+          const float a = ex2(fmaf(s[n][m][2 * v], qs[n][0], up[0])), b = ex2(fmaf(s[n][m][2 * v + 1], qs[n][1], up[1]));
           l[n][0] += a;
           l[n][1] += b;
           pf[n][m][v] = transposed(pack_f16(a, b));
         }
     }
 
-    // O^T: columns D/8 g + 2 i (and + 1), rows as those of S^T.  A weight of 0 times a scale that is not finite is not 0:
-    // where a row does not see all of the block, such scales count as 0, and the rows that see them get their NaN after.
-    bool odd = false;
-    if (!full) {
-#pragma unroll
-      for (int j = 0; j < 2 * W / 4; ++j) {
-        const uint32_t x = *reinterpret_cast<const uint32_t*>(st + R::kSV + 4 * (lane + 32 * j));
-#pragma unroll
-        for (int b = 0; b < 4; ++b) odd |= ((x >> (8 * b)) & 255u) > 226u;
-      }
-      odd = __any_sync(0xffffffffu, odd);
-    }
+    // O^T: columns D/8 g + 2 i (and + 1), rows as those of S^T
 #pragma unroll
     for (int m = 0; m < 2; ++m) {
       uint32_t w[4][W / 2], b[4];
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
-        const int key = 16 * m + 8 * (u >> 1) + 2 * t4 + (u & 1);
-        const uint8_t* a = st + R::kV + key * R::kPitchV + 2 * W * g;
+        const int key = 16 * m + 8 * (u >> 1) + key_of(2 * t4 + (u & 1));
+        const uint8_t* a = st + R::kV + key * R::kRow + 2 * W * g;
         if constexpr (W == 4) {
           const uint2 v = *reinterpret_cast<const uint2*>(a);
           w[u][0] = v.x, w[u][1] = v.y;
@@ -359,7 +373,6 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm<NT>()) chunk_mma4_kernel
           w[u][0] = *reinterpret_cast<const uint32_t*>(a);
         }
         b[u] = st[R::kSV + key * R::kScales + (W == 4 ? g : g >> 1)];
-        if (odd && b[u] > 226u) b[u] = 0u;
       }
       const uint32_t lo = scale_pair(b[0], b[1]), hi = scale_pair(b[2], b[3]);
 #pragma unroll
@@ -377,19 +390,15 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm<NT>()) chunk_mma4_kernel
         }
       }
     }
-    if (odd) {
-#pragma unroll 1
-      for (int key = 0; key < kBlk; ++key) {
-        if (st[R::kSV + key * R::kScales + (W == 4 ? g : g >> 1)] <= 226u) continue;
+    if (__any_sync(0xffffffffu, nan_keys != 0u)) {
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
+      for (int n = 0; n < NT; ++n)
 #pragma unroll
-          for (int u = 0; u < 2; ++u)
-            if (!((hides[n][u] >> key) & 1u)) {
+        for (int u = 0; u < 2; ++u)
+          if (nan_keys & seen(there, lim[n][u] - k0)) {
 #pragma unroll
-              for (int c = 0; c < MT; ++c) o[n][c][u] = o[n][c][2 + u] = __uint_as_float(0x7fc00000u);
-            }
-      }
+            for (int c = 0; c < MT; ++c) o[n][c][u] = o[n][c][2 + u] = __uint_as_float(0x7fc00000u);
+          }
     }
     __syncwarp();
   }
@@ -468,11 +477,17 @@ cudaError_t launch(const ChunkParams& p, bool early, const ChunkItem* items, int
     if (e != cudaSuccess) return e;
     if (dev >= 0 && dev < 64) configured[dev] = true;
   }
-  if ((int64_t)n * p.h_kv > INT32_MAX) return cudaErrorInvalidValue;
+  if ((int64_t)n * p.h_kv > INT32_MAX || (int64_t)p.n_pages * p.h_kv * p.page_size > UINT32_MAX) return cudaErrorInvalidValue;
   return launch_early(early, chunk_mma4_kernel<D, NT>, dim3(n * p.h_kv), kThreads, smem_bytes<D, NT>(), s, p, items);
 }
 
 }  // namespace
+
+int chunk_mma4_ctas(int head_dim, int rows8) {
+  static constexpr int kCtas[2][4] = {{ctas_per_sm<64, 1>(), ctas_per_sm<64, 2>(), ctas_per_sm<64, 3>(), ctas_per_sm<64, 4>()},
+                                      {ctas_per_sm<128, 1>(), ctas_per_sm<128, 2>(), ctas_per_sm<128, 3>(), ctas_per_sm<128, 4>()}};
+  return kCtas[head_dim == 128][rows8 - 1];
+}
 
 cudaError_t launch_chunk_mma4(const ChunkParams& p, int head_dim, int rows8, bool early, const ChunkItem* items, int n_items,
                               cudaStream_t s) {

@@ -7,9 +7,9 @@
 // traffic.  Bound by those bytes; short ones by the chain of a CTA's steps.
 //
 // How often a token occurs in the context is counted in a plane of integers over the slice: additions of whole numbers,
-// whose order does not matter.  Going through the context again, whoever takes a token's count out of the plane first
-// applies it, so that each token is changed once, by its whole count.  Biases use the plane to find tokens that occur
-// once (added at once) and those that occur again (their first entry adds all, in order).
+// whose order does not matter; the pass for the maximum reads the counts beside the logits and changes each token once,
+// by its whole count.  Biases use the plane to find tokens that occur once (added at once) and those that occur again
+// (their first entry adds all, in order).
 // Sums are in fp32: a thread's terms, the warps', the slices', each in a fixed order.
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
@@ -29,6 +29,7 @@ constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
 constexpr int kMaxCtas = 16;       // of a row
 constexpr int kMaxSlice = 24576;   // entries of a CTA: 4 bytes each of logits and of counts
+constexpr int kSlack = 16;          // entries of the buffers beyond a slice
 constexpr float kNegInf = -__builtin_huge_valf();
 constexpr float kLog2e = 1.4426950408889634f;
 
@@ -66,25 +67,27 @@ __global__ void __launch_bounds__(kThreads) probs_kernel(const __grid_constant__
   const int lo = min(a.vocab, rank * slice), n = min(slice, a.vocab - lo);
   cl.barrier_arrive();  // (every CTA of the cluster runs before one writes into another's memory)
 
-  // The slice, entry i at x[shift + i]: shared memory is as far from a 16-byte boundary as the row's memory is.
+  // The slice, entry i at x[shift + i] with its count at the same place of the plane: shared memory is as far from a
+  // 16-byte boundary as the row's memory is.  What lies before and behind it in the same 16 bytes is -infinity.
   constexpr int VL = 16 / (int)sizeof(TL), VP = 16 / (int)sizeof(TP);
   const TL* src = static_cast<const TL*>(a.logits) + row * a.logits_stride + lo;
   const int shift = (int)((reinterpret_cast<uintptr_t>(src) / sizeof(TL)) % VL);
   float* x = reinterpret_cast<float*>(smem);
-  uint32_t* plane = reinterpret_cast<uint32_t*>(smem + (size_t)(slice + 8) * 4);
-  const int vecs = n > 0 ? (shift + n + VL - 1) / VL : 0;
+  uint32_t* plane = reinterpret_cast<uint32_t*>(smem + (size_t)(slice + kSlack) * 4);
+  const int fours = (shift + n + 3) / 4;
+  if (threadIdx.x < 8) {
+    if ((int)threadIdx.x < shift) x[threadIdx.x] = kNegInf;
+    x[shift + n + threadIdx.x] = kNegInf;
+  }
+  // whole pieces of 16 bytes [v0, v1), and what is left before and behind them
+  const int v0 = shift > 0 ? 1 : 0, v1 = max(v0, (shift + n) / VL);
+  const int head = min(n, v0 * VL - shift), tail = max(head, v1 * VL - shift);
   if constexpr (sizeof(TL) == 4) {
     const uint32_t at = tc::smem_u32(x);
-    for (int v = threadIdx.x; v < vecs; v += kThreads) {
-      const int i0 = v * VL - shift;
-      if (i0 >= 0 && i0 + VL <= n) {
-        cp16(at + 16 * v, src + i0);
-      } else {
-#pragma unroll
-        for (int u = 0; u < VL; ++u)
-          if (i0 + u >= 0 && i0 + u < n) cp4(at + 16 * v + 4 * u, src + i0 + u);
-      }
-    }
+#pragma unroll 4
+    for (int v = v0 + threadIdx.x; v < v1; v += kThreads) cp16(at + 16 * v, src + v * VL - shift);
+    if ((int)threadIdx.x < head) cp4(at + 4 * (shift + threadIdx.x), src + threadIdx.x);
+    if ((int)threadIdx.x < n - tail) cp4(at + 4 * (shift + tail + threadIdx.x), src + tail + threadIdx.x);
   }
   // which event and place in its chunk the row has
   for (int e = threadIdx.x; e < a.n_events; e += kThreads) {
@@ -93,29 +96,24 @@ __global__ void __launch_bounds__(kThreads) probs_kernel(const __grid_constant__
   }
   const bool counts = a.history != nullptr || a.tokens != nullptr, plane_used = counts || a.bias_token != nullptr;
   if (plane_used)
-    for (int i = threadIdx.x; i < slice / (WIDE ? 1 : 2); i += kThreads) plane[i] = 0u;
+    for (int i = threadIdx.x; i < (slice + kSlack) / (WIDE ? 4 : 8); i += kThreads) reinterpret_cast<uint4*>(plane)[i] = make_uint4(0u, 0u, 0u, 0u);
   if constexpr (sizeof(TL) == 2) {
     constexpr int U = 4;
-    for (int v0 = threadIdx.x; v0 < vecs; v0 += U * kThreads) {
+    for (int w = v0 + threadIdx.x; w < v1; w += U * kThreads) {
       uint4 r[U];
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int i0 = (v0 + u * kThreads) * VL - shift;
-        if (i0 >= 0 && i0 + VL <= n) r[u] = *reinterpret_cast<const uint4*>(src + i0);
-      }
+      for (int u = 0; u < U; ++u)
+        if (w + u * kThreads < v1) r[u] = *reinterpret_cast<const uint4*>(src + (w + u * kThreads) * VL - shift);
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const int v = v0 + u * kThreads, i0 = v * VL - shift;
-        if (i0 >= 0 && i0 + VL <= n) {
-          float4* d = reinterpret_cast<float4*>(x + v * VL);
-          d[0] = make_float4(__uint_as_float(r[u].x << 16), __uint_as_float(r[u].x & 0xffff0000u), __uint_as_float(r[u].y << 16), __uint_as_float(r[u].y & 0xffff0000u));
-          d[1] = make_float4(__uint_as_float(r[u].z << 16), __uint_as_float(r[u].z & 0xffff0000u), __uint_as_float(r[u].w << 16), __uint_as_float(r[u].w & 0xffff0000u));
-        } else {
-          for (int k = 0; k < VL; ++k)
-            if (i0 + k >= 0 && i0 + k < n) x[v * VL + k] = __bfloat162float(src[i0 + k]);
-        }
+        if (w + u * kThreads >= v1) break;
+        float4* d = reinterpret_cast<float4*>(x + (w + u * kThreads) * VL);
+        d[0] = make_float4(__uint_as_float(r[u].x << 16), __uint_as_float(r[u].x & 0xffff0000u), __uint_as_float(r[u].y << 16), __uint_as_float(r[u].y & 0xffff0000u));
+        d[1] = make_float4(__uint_as_float(r[u].z << 16), __uint_as_float(r[u].z & 0xffff0000u), __uint_as_float(r[u].w << 16), __uint_as_float(r[u].w & 0xffff0000u));
       }
     }
+    if ((int)threadIdx.x < head) x[shift + threadIdx.x] = __bfloat162float(src[threadIdx.x]);
+    if ((int)threadIdx.x < n - tail) x[shift + tail + threadIdx.x] = __bfloat162float(src[tail + threadIdx.x]);
   }
   __syncthreads();
   const int e = event;
@@ -127,65 +125,117 @@ __global__ void __launch_bounds__(kThreads) probs_kernel(const __grid_constant__
   const int32_t* history = a.history != nullptr ? a.history + (int64_t)e * a.history_width : nullptr;
   const int past = history != nullptr ? min(max(a.history_len[e], 0), a.history_width) : 0;
   const int chunk = a.tokens != nullptr ? row - mine.tok0 + 1 : 0;
-  auto token = [&](int i) { return i < past ? history[i] : a.tokens[mine.tok0 + (i - past)]; };
-  if (counts) {
-    for (int i = threadIdx.x; i < past + chunk; i += kThreads) {
-      const int64_t k = (int64_t)token(i) - lo;
-      if (k >= 0 && k < n) atomicAdd(plane + (WIDE ? k : k >> 1), WIDE ? 1u : 1u << (16 * (k & 1)));
+  // adds one for each of a list's tokens that lie in the slice
+  auto count = [&](const int32_t* list, int len) {
+    constexpr int U = 8;
+    for (int i0 = threadIdx.x; i0 < len; i0 += U * kThreads) {
+      int32_t t[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) t[u] = i0 + u * kThreads < len ? __ldg(list + i0 + u * kThreads) : -1;
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const uint32_t k = (uint32_t)t[u] - (uint32_t)lo;
+        if (t[u] >= 0 && k < (uint32_t)n) {
+          const uint32_t at = shift + k;
+          atomicAdd(plane + (WIDE ? at : at >> 1), WIDE ? 1u : 1u << (16 * (at & 1)));
+        }
+      }
     }
+  };
+  if (counts) {
+    count(history, past);
+    count(a.tokens + mine.tok0, chunk);
   }
   asm volatile("cp.async.wait_all;" ::: "memory");
   __syncthreads();
-  if (counts) {
-    for (int i = threadIdx.x; i < past + chunk; i += kThreads) {
-      const int64_t k = (int64_t)token(i) - lo;
-      if (k < 0 || k >= n) continue;
-      uint32_t c;
-      if (WIDE) c = atomicExch(plane + k, 0u);
-      else c = (atomicAnd(plane + (k >> 1), (k & 1) ? 0xffffu : 0xffff0000u) >> (16 * (k & 1))) & 0xffffu;
-      if (c == 0u) continue;
-      const float v = x[shift + k];
-      x[shift + k] = (v > 0.f ? __fdiv_rn(v, repetition) : v * repetition) - fmaf(frequency, (float)c, presence);
+  // the counts of the four entries from 4 v on
+  auto counts_of = [&](int v, uint32_t (&c)[4]) -> bool {
+    if (WIDE) {
+      const uint4 w = reinterpret_cast<const uint4*>(plane)[v];
+      c[0] = w.x, c[1] = w.y, c[2] = w.z, c[3] = w.w;
+    } else {
+      const uint2 w = reinterpret_cast<const uint2*>(plane)[v];
+      c[0] = w.x & 0xffffu, c[1] = w.x >> 16, c[2] = w.y & 0xffffu, c[3] = w.y >> 16;
     }
-    __syncthreads();
-  }
+    return (c[0] | c[1] | c[2] | c[3]) != 0u;
+  };
+  // (a product with the rounded 1 / r: entries that occur are few, but hardly a warp's pass is without one)
+  const float up = __fdiv_rn(1.f, repetition);
+  auto penalised = [&](float v, uint32_t c) {
+    const float y = v * (v > 0.f ? up : repetition) - fmaf(frequency, (float)c, presence);
+    return c == 0u ? v : y;
+  };
   if (a.bias_token != nullptr) {
+    if (counts) {
+      for (int v = threadIdx.x; v < fours; v += kThreads) {
+        uint32_t c[4];
+        if (!counts_of(v, c)) continue;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) x[4 * v + u] = penalised(x[4 * v + u], c[u]);
+        if (WIDE) reinterpret_cast<uint4*>(plane)[v] = make_uint4(0u, 0u, 0u, 0u);
+        else reinterpret_cast<uint2*>(plane)[v] = make_uint2(0u, 0u);
+      }
+      __syncthreads();
+    }
     const int64_t first = (int64_t)e * a.bias_width;
     const int32_t* tok = a.bias_token + first;
     const float* value = a.bias_value + first;
     const int len = min(max(a.bias_len[e], 0), a.bias_width);
-    for (int i = threadIdx.x; i < len; i += kThreads) {
-      const int64_t k = (int64_t)tok[i] - lo;
-      if (k >= 0 && k < n) atomicAdd(plane + (WIDE ? k : k >> 1), WIDE ? 1u : 1u << (16 * (k & 1)));
-    }
+    count(tok, len);
     __syncthreads();
     for (int i = threadIdx.x; i < len; i += kThreads) {
       const int32_t me = tok[i];
-      const int64_t k = (int64_t)me - lo;
-      if (k < 0 || k >= n) continue;
+      const uint32_t k = (uint32_t)me - (uint32_t)lo, at = shift + k;
+      if (me < 0 || k >= (uint32_t)n) continue;
       float sum = value[i];
-      if ((WIDE ? plane[k] : (plane[k >> 1] >> (16 * (k & 1))) & 0xffffu) > 1u) {
+      if ((WIDE ? plane[at] : (plane[at >> 1] >> (16 * (at & 1))) & 0xffffu) > 1u) {
         bool before = false;
         for (int j = 0; j < i && !before; ++j) before = tok[j] == me;
         if (before) continue;
         for (int j = i + 1; j < len; ++j)
           if (tok[j] == me) sum += value[j];
       }
-      x[shift + k] += sum;
+      x[at] += sum;
     }
     __syncthreads();
   }
-  if (a.mask != nullptr) {  // (slices start at whole words)
-    const uint32_t* word = a.mask + row * a.mask_stride + lo / 32;
-#pragma unroll 4
-    for (int i = threadIdx.x; i < n; i += kThreads)
-      if (!((word[i >> 5] >> lane) & 1u)) x[shift + i] = kNegInf;
-    __syncthreads();
+  // Penalties (where biases did not want them first) and the mask, and the slice's maximum.
+  const bool apply = counts && a.bias_token == nullptr;
+  const bool greedy = !(temperature > 0.f);
+  const uint32_t* words = a.mask != nullptr ? a.mask + row * a.mask_stride + lo / 32 : nullptr;  // (slices start at whole words)
+  const int n_words = (n + 31) / 32;
+  Part q{kNegInf, 0.f, 0x7fffffff, 0};
+#pragma unroll 2
+  for (int v = threadIdx.x; v < fours; v += kThreads) {
+    float4 f = reinterpret_cast<const float4*>(x)[v];
+    float y[4] = {f.x, f.y, f.z, f.w};
+    bool changed = false;
+    uint32_t c[4];
+    if (apply && counts_of(v, c)) {
+      changed = true;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) y[u] = penalised(y[u], c[u]);
+    }
+    if (words != nullptr) {
+      const int i0 = 4 * v - shift, w0 = i0 >> 5;  // (of a first place before the slice: -1)
+      const uint32_t bits = __funnelshift_r(w0 >= 0 ? __ldg(words + w0) : 0u, w0 + 1 < n_words ? __ldg(words + w0 + 1) : 0u, i0 & 31);
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        if (!((bits >> u) & 1u)) y[u] = kNegInf, changed = true;
+    }
+    if (changed) reinterpret_cast<float4*>(x)[v] = make_float4(y[0], y[1], y[2], y[3]);
+    if (greedy) {
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        if (y[u] > q.m) q.m = y[u], q.at = lo + 4 * v + u - shift;
+        q.nan |= y[u] != y[u];
+      }
+    } else {
+      q.m = fmaxf(tc::max3f(y[0], y[1], y[2]), fmaxf(y[3], q.m));
+    }
   }
 
-  // the slice's maximum and its first place, then (T > 0) the sum of 2^((x - m) log2(e) / T), which takes x's place
-  const bool greedy = !(temperature > 0.f);
-  const int end = shift + n;
+  // the maximum's first place, then (T > 0) the sum of 2^((x - m) log2(e) / T), which takes x's place
   auto block_join = [&](Part& q, bool sum) {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
@@ -205,21 +255,13 @@ __global__ void __launch_bounds__(kThreads) probs_kernel(const __grid_constant__
     __syncthreads();
     q = r;
   };
-  Part q{kNegInf, 0.f, 0x7fffffff, 0};
-  if (greedy) {
-    for (int i = shift + threadIdx.x; i < end; i += kThreads) {
-      const float v = x[i];
-      if (v > q.m) q.m = v, q.at = lo + i - shift;
-      q.nan |= v != v;
-    }
-  } else {
-    for (int i = shift + threadIdx.x; i < end; i += kThreads) q.m = fmaxf(q.m, x[i]);
-  }
   block_join(q, false);
   const float c = fminf(__fdiv_rn(kLog2e, temperature), 3.402823466e38f);  // (0 times it is 0 however small T)
   if (!greedy) {
     const float m = q.m == kNegInf ? 0.f : q.m;
-    for (int i = shift + threadIdx.x; i < end; i += kThreads) {
+    // (by places from the slice's start: the sum does not depend on where in memory the row begins)
+#pragma unroll 4
+    for (int i = shift + threadIdx.x; i < shift + n; i += kThreads) {
       const float v = tc::ex2((x[i] - m) * c);
       x[i] = v;
       q.l += v;
@@ -229,45 +271,49 @@ __global__ void __launch_bounds__(kThreads) probs_kernel(const __grid_constant__
   cl.barrier_wait();
   if ((int)threadIdx.x < ctas) *cl.map_shared_rank(&parts[rank], threadIdx.x) = q;
   cl.sync();  // (nobody reads or writes another CTA's memory after this)
-  Part all = parts[0];
-  for (int k = 1; k < ctas; ++k) join_max(all, parts[k]);
+  Part all{kNegInf, 0.f, 0x7fffffff, 0};
+  if (lane < ctas) all = parts[lane];
+  const float part_m = all.m;
+#pragma unroll
+  for (int o = kMaxCtas / 2; o > 0; o >>= 1)
+    join_max(all, {__shfl_xor_sync(0xffffffffu, all.m, o), 0.f, __shfl_xor_sync(0xffffffffu, all.at, o), __shfl_xor_sync(0xffffffffu, all.nan, o)});
+  // (lanes of the upper half repeat nothing: their parts are empty, and only the lower half is read)
   float scale = 0.f;
   if (!greedy) {
-    float l = 0.f;
-    for (int k = 0; k < ctas; ++k)
-      if (parts[k].l != 0.f) l += parts[k].l * (parts[k].m == kNegInf ? 1.f : tc::ex2((parts[k].m - all.m) * c));  // (a NaN counts)
+    float l = all.l == 0.f ? 0.f : all.l * (part_m == kNegInf ? 1.f : tc::ex2((part_m - all.m) * c));  // (a NaN counts)
+#pragma unroll
+    for (int o = kMaxCtas / 2; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
     scale = l == 0.f ? 0.f : __fdiv_rn(q.m == kNegInf ? 1.f : tc::ex2((q.m - all.m) * c), l);
   } else if (all.nan || all.m == kNegInf) {
     all.at = -1;
   }
+  scale = __shfl_sync(0xffffffffu, scale, 0);
+  all.at = __shfl_sync(0xffffffffu, all.at, 0);
   TP* dst = static_cast<TP*>(a.p) + row * a.p_stride + lo;
   auto value_at = [&](int i) { return greedy ? (lo + i == all.at ? 1.f : 0.f) : x[shift + i] * scale; };
   const int skew = (int)((reinterpret_cast<uintptr_t>(dst) / sizeof(TP)) % VP);
   if (((shift - skew) & 3) == 0) {
-    const int outs = n > 0 ? (skew + n + VP - 1) / VP : 0;
-    for (int v = threadIdx.x; v < outs; v += kThreads) {
+    const int o0 = skew > 0 ? 1 : 0, o1 = max(o0, (skew + n) / VP), front = min(n, o0 * VP - skew), back = max(front, o1 * VP - skew);
+#pragma unroll 2
+    for (int v = o0 + threadIdx.x; v < o1; v += kThreads) {
       const int i0 = v * VP - skew;
-      if (i0 >= 0 && i0 + VP <= n) {
-        float y[VP];
+      float y[VP];
 #pragma unroll
-        for (int u = 0; u < VP; u += 4) {
-          const float4 f = *reinterpret_cast<const float4*>(x + shift + i0 + u);
-          y[u] = f.x * scale, y[u + 1] = f.y * scale, y[u + 2] = f.z * scale, y[u + 3] = f.w * scale;
-        }
-        if (greedy) {
-#pragma unroll
-          for (int u = 0; u < VP; ++u) y[u] = lo + i0 + u == all.at ? 1.f : 0.f;
-        }
-        if constexpr (sizeof(TP) == 4)
-          __stcs(reinterpret_cast<float4*>(dst + i0), make_float4(y[0], y[1], y[2], y[3]));
-        else
-          __stcs(reinterpret_cast<uint4*>(dst + i0), make_uint4(tc::pack_bf16(y[0], y[1]), tc::pack_bf16(y[2], y[3]), tc::pack_bf16(y[4], y[5]), tc::pack_bf16(y[6], y[7])));
-      } else {
-#pragma unroll
-        for (int u = 0; u < VP; ++u)
-          if (i0 + u >= 0 && i0 + u < n) dst[i0 + u] = TP(value_at(i0 + u));
+      for (int u = 0; u < VP; u += 4) {
+        const float4 f = *reinterpret_cast<const float4*>(x + shift + i0 + u);
+        y[u] = f.x * scale, y[u + 1] = f.y * scale, y[u + 2] = f.z * scale, y[u + 3] = f.w * scale;
       }
+      if (greedy) {
+#pragma unroll
+        for (int u = 0; u < VP; ++u) y[u] = lo + i0 + u == all.at ? 1.f : 0.f;
+      }
+      if constexpr (sizeof(TP) == 4)
+        __stcs(reinterpret_cast<float4*>(dst + i0), make_float4(y[0], y[1], y[2], y[3]));
+      else
+        __stcs(reinterpret_cast<uint4*>(dst + i0), make_uint4(tc::pack_bf16(y[0], y[1]), tc::pack_bf16(y[2], y[3]), tc::pack_bf16(y[4], y[5]), tc::pack_bf16(y[6], y[7])));
     }
+    if ((int)threadIdx.x < front) dst[threadIdx.x] = TP(value_at(threadIdx.x));
+    if ((int)threadIdx.x < n - back) dst[back + threadIdx.x] = TP(value_at(back + threadIdx.x));
   } else {
     for (int i = threadIdx.x; i < n; i += kThreads) dst[i] = TP(value_at(i));
   }
@@ -281,7 +327,7 @@ cudaError_t launch(const ChunkProbs& a, const ChunkVerify* work, int rows, int c
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
   if (dev < 0 || dev >= 64 || !configured[dev]) {
-    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (kMaxSlice + 8) * 4 + kMaxSlice * (WIDE ? 4 : 2));
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (kMaxSlice + kSlack) * (WIDE ? 8 : 6));
     if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
     if (e != cudaSuccess) return e;
     if (dev >= 0 && dev < 64) configured[dev] = true;
@@ -290,7 +336,7 @@ cudaError_t launch(const ChunkProbs& a, const ChunkVerify* work, int rows, int c
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(rows * ctas));
   cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = (size_t)(slice + 8) * 4 + (plane ? (size_t)slice * (WIDE ? 4 : 2) : 0);
+  cfg.dynamicSmemBytes = (size_t)(slice + kSlack) * (plane ? (WIDE ? 8 : 6) : 4);
   cfg.stream = s;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
