@@ -680,7 +680,7 @@ pad_status pad_chunk_attn(const pad_chunk_t* chunk, const void* q, int64_t q_str
  *   mask         [N, mask_stride] int32 words, bit i % 32 of word i / 32 for token i; mask_stride at least
  *                ceil(vocab / 32), 0 = that; NULL: every token is allowed
  * All device memory.  Tokens outside [0, vocab) are passed over; lengths are kept within their rows.  Sums are in fp32 in a fixed
- * order: the same inputs give the same bits.  vocab at most 393216. */
+ * order: the same inputs give the same bits (the order depends on where a row begins within 16 bytes).  vocab at most 393152. */
 pad_status pad_chunk_probs(const pad_chunk_t* chunk, int32_t vocab, int32_t logits_dtype, const void* logits, int64_t logits_stride,
                            const float* params, const int32_t* tokens, const int32_t* history, int32_t history_width,
                            const int32_t* history_len, const int32_t* bias_token, const float* bias_value, int32_t bias_width,

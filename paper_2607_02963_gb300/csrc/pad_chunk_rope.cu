@@ -85,7 +85,7 @@ __device__ __forceinline__ uint4 turned(uint4 x, const float2 (&cs)[8], int n, i
 }
 
 template <int D, int FMT, int LAYOUT>
-__global__ void __launch_bounds__(kThreads) chunk_rope_kernel(const __grid_constant__ ChunkParams p,
+__global__ void __launch_bounds__(kThreads, 3) chunk_rope_kernel(const __grid_constant__ ChunkParams p,
                                                               const ChunkPages* __restrict__ work,
                                                               const __grid_constant__ RopeArgs a) {
   constexpr int L = D / 8, RPW = 32 / L;              // lanes of a head, heads of a warp at a time
@@ -104,17 +104,33 @@ __global__ void __launch_bounds__(kThreads) chunk_rope_kernel(const __grid_const
     if (w.page >= 0) *entry = page;
     if (!there) pad_set_error(p.header, p.gen, PAD_ERR_DEVICE_BOUNDS, w.event, w.column, page);
   }
+  // The token's heads in order: of q, of k, of v; a batch of U is on its way while the one before is turned, the first
+  // while the cosines and sines are formed.
+  constexpr int U = 4;
+  const int t = warp / a.warps_per_token, part = warp % a.warps_per_token;
+  const int heads = p.h_q + 2 * p.h_kv, step = RPW * a.warps_per_token;
+  const int64_t tok = w.tok + first + t;
+  const __nv_bfloat16* const q = a.q + tok * a.q_stride + 8 * c;
+  const __nv_bfloat16* const kn = a.k_new + tok * a.new_stride - (int64_t)p.h_q * D + 8 * c;
+  const __nv_bfloat16* const vn = a.v_new + tok * a.new_stride - (int64_t)(p.h_q + p.h_kv) * D + 8 * c;
+  uint4 next[U];
+  auto fetch = [&](int h0) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int h = h0 + sub + u * step;
+      if (h < heads && t < n) next[u] = __ldcs(reinterpret_cast<const uint4*>((h < p.h_q ? q : h < p.h_q + p.h_kv ? kn : vn) + h * D));
+    }
+  };
+  fetch(RPW * part);
   for (int i = threadIdx.x; i < n * H; i += kThreads) {
-    const int t = i / H, k = i % H;
-    const uint64_t turn = (uint64_t)(int64_t)a.position[w.tok + first + t] * a.rope.turn[k];
+    const int ti = i / H, k = i % H;
+    const uint64_t turn = (uint64_t)(int64_t)a.position[w.tok + first + ti] * a.rope.turn[k];
     float s, co;
     sincospif((float)(int32_t)(turn >> 32) * 0x1p-31f, &s, &co);
-    table[t][k] = make_float2(co * a.rope.magnitude, s * a.rope.magnitude);
+    table[ti][k] = make_float2(co * a.rope.magnitude, s * a.rope.magnitude);
   }
   __syncthreads();
-  const int t = warp / a.warps_per_token, part = warp % a.warps_per_token;
   if (t >= n) return;
-  const int64_t tok = w.tok + first + t;
   // this lane's cosines and sines, the sine's sign with it
   float2 cs[8];
   const int d0 = 8 * c, turns = min(max(R - d0, 0), 8);
@@ -139,39 +155,26 @@ __global__ void __launch_bounds__(kThreads) chunk_rope_kernel(const __grid_const
     }
     return turned<LAYOUT>(x, cs, turns, other, row, d0, R);
   };
-  const int step = RPW * a.warps_per_token;
-  constexpr int U = 4;  // heads of a lane under way together
-  const __nv_bfloat16* q = a.q + tok * a.q_stride + d0;
-  __nv_bfloat16* out = a.q_out + tok * a.out_stride + d0;
+  __nv_bfloat16* const out = a.q_out + tok * a.out_stride + d0;
+  const int64_t slot = w.slot + first + t;
 #pragma unroll 1
-  for (int h0 = RPW * part; h0 < p.h_q; h0 += U * step) {
+  for (int h0 = RPW * part; h0 < heads; h0 += U * step) {
     uint4 x[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int h = h0 + sub + u * step;
-      x[u] = make_uint4(0u, 0u, 0u, 0u);
-      if (h < p.h_q) x[u] = __ldcs(reinterpret_cast<const uint4*>(q + h * D));
-    }
+    for (int u = 0; u < U; ++u) x[u] = next[u];
+    fetch(h0 + U * step);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      if (h0 + u * step >= p.h_q) break;  // (whole warps)
-      const int h = h0 + sub + u * step;
+      if (h0 + u * step >= heads) break;  // (whole warps)
+      const int h = h0 + sub + u * step, kv = h - p.h_q;
       const uint4 o = turn(x[u]);
-      if (h < p.h_q) *reinterpret_cast<uint4*>(out + h * D) = o;
-    }
-  }
-  if (!there) return;
-  const int64_t slot = w.slot + first + t;
-  for (int kv = 0; kv < 2; ++kv) {
-    const __nv_bfloat16* src = (kv ? a.v_new : a.k_new) + tok * a.new_stride + d0;
-#pragma unroll 1
-    for (int h0 = RPW * part; h0 < p.h_kv; h0 += step) {
-      const int h = h0 + sub;
-      const bool on = h < p.h_kv;
-      uint4 x = make_uint4(0u, 0u, 0u, 0u);
-      if (on) x = __ldcs(reinterpret_cast<const uint4*>(src + h * D));
-      if (kv == 0) x = turn(x);
-      store_group<D, FMT>(x, c, on, ((int64_t)page * p.h_kv + h) * p.page_size + slot, kv ? a.v_pool : a.k_pool, kv ? a.v_scale : a.k_scale);
+      if (kv < 0) __stcs(reinterpret_cast<uint4*>(out + h * D), o);
+      if (there && h0 + u * step + RPW > p.h_q) {  // (some head of the warp's is the cache's)
+        const bool v = kv >= p.h_kv;
+        const int hk = max(v ? kv - p.h_kv : kv, 0);
+        const uint4 y = v ? x[u] : o;
+        store_group<D, FMT>(y, c, kv >= 0 && h < heads, ((int64_t)page * p.h_kv + hk) * p.page_size + slot, v ? a.v_pool : a.k_pool, v ? a.v_scale : a.k_scale);
+      }
     }
   }
 }

@@ -247,10 +247,10 @@ def test_probabilities(vocab, bf16):
 
 
 def test_the_largest_vocabulary_and_one_more():
-    r = Rows(1, [1, 2], 393216, 100, 10, 0.5)
+    r = Rows(1, [1, 2], 393152, 100, 10, 0.5)
     r.check(r.run())
     with pytest.raises(B.PadError, match="vocab"):
-        x = torch.zeros(3, 393217, device="cuda")
+        x = torch.zeros(3, 393153, device="cuda")
         B.pad_chunk_probs(r.plan, x, x)
 
 
@@ -320,7 +320,7 @@ def test_strides_alignments_and_in_place(bf16):
         mask = torch.zeros(5, 97, dtype=torch.int32, device="cuda")
         mask[:, 1:95] = r.mask()
         r.run(wide[:, a:a + 3001], out[:, b:b + 3001], mask=mask[:, 1:95])
-        assert torch.equal(out[:, b:b + 3001], want)
+        r.check(out[:, b:b + 3001])       # (terms are summed by 16-byte pieces, which begin elsewhere: equal within the bound alone)
         assert (out[:, :b] == 7).all() and (out[:, b + 3001:] == 7).all()
     if bf16[0] == bf16[1]:
         x = r.logits.cuda()
