@@ -497,6 +497,7 @@ class ChunkPlan:
         import torch
         hq, hk, d = problem.h_q, problem.h_kv, problem.head_dim
         self._q_shape, self._lse_shape = (self.n_tokens, hq, d), (self.n_tokens, hq)
+        self._row_shape, self._event_shape, self._params_shape = (self.n_tokens,), (n_events,), (n_events, 4)
         self._new_shape, self._read_shape = (self.n_tokens, hk, d), (self.n_cached, hk, d)
         self._scale_shape = (n_pages, hk, problem.page_size) + ((d // 16,) if kv_format == KV_FP4 else ())
         self._pool_shape = (n_pages, hk, problem.page_size, d // 2 if kv_format == KV_FP4 else d)
@@ -669,9 +670,10 @@ def pad_chunk_append_rope(plan: ChunkPlan, rope: Rope, position, q, q_out, k_new
     else:
         qp, qst = _rows(q, "q", qs, bf16)
         op, ost = _rows(q_out, "q_out", qs, bf16)
-    pp = _dev(position, "position", (plan.n_tokens,), plan._i32)
+    if not (position.shape == plan._row_shape and position.dtype is plan._i32 and position.is_contiguous() and position.is_cuda):
+        _dev(position, "position", plan._row_shape, plan._i32)
     kp, vp, ksc, vsc = plan._pools(k_pool, v_pool, k_scale, v_scale)
-    st = (_lib or lib()).pad_chunk_append_rope(plan._h, rope._ref, pp, qp, qst, op, ost, kn, vn, ks, kp, vp, ksc, vsc,
+    st = (_lib or lib()).pad_chunk_append_rope(plan._h, rope._ref, position.data_ptr(), qp, qst, op, ost, kn, vn, ks, kp, vp, ksc, vsc,
                                                _stream_handle(stream))
     if st:
         _check(st)
@@ -738,17 +740,31 @@ def pad_chunk_probs(plan: ChunkPlan, logits, p, params=None, history=None, histo
         pp, ps = _rows(p, "p", shape, pk)
     if lp == pp and (lk is not pk or ls != ps):
         raise ValueError("p: over logits, their types and strides must be the same")
-    hw = 0 if history is None else int(history.shape[-1])
-    bw = 0 if bias_token is None else int(bias_token.shape[-1])
-    hp, hl = _dev(history, "history", (ne, hw), i32), _dev(history_len, "history_len", (ne,), i32)
-    bt, bv = _dev(bias_token, "bias_token", (ne, bw), i32), _dev(bias_value, "bias_value", (ne, bw), f32)
-    bl = _dev(bias_len, "bias_len", (ne,), i32)
-    mp, ms = None, 0
+    hw = bw = ms = 0
+    pa = to = hp = hl = bt = bv = bl = mp = None
+    if params is not None:
+        if not (params.shape == plan._params_shape and params.dtype is f32 and params.is_contiguous() and params.is_cuda):
+            _dev(params, "params", plan._params_shape, f32)
+        pa = params.data_ptr()
+    if tokens is not None:
+        if not (tokens.shape == plan._row_shape and tokens.dtype is i32 and tokens.is_contiguous() and tokens.is_cuda):
+            _dev(tokens, "tokens", plan._row_shape, i32)
+        to = tokens.data_ptr()
+    if history is not None or history_len is not None:
+        hw = 0 if history is None else history.shape[-1]
+        if not (history is not None and history_len is not None and history.shape == (ne, hw) and history_len.shape == plan._event_shape
+                and history.dtype is i32 and history_len.dtype is i32 and history.is_contiguous() and history.is_cuda
+                and history_len.is_contiguous() and history_len.is_cuda):
+            _dev(history, "history", (ne, hw), i32), _dev(history_len, "history_len", plan._event_shape, i32)
+        hp, hl = _ptr(history), _ptr(history_len)
+    if bias_token is not None or bias_value is not None or bias_len is not None:
+        bw = 0 if bias_token is None else bias_token.shape[-1]
+        bt, bv = _dev(bias_token, "bias_token", (ne, bw), i32), _dev(bias_value, "bias_value", (ne, bw), f32)
+        bl = _dev(bias_len, "bias_len", plan._event_shape, i32)
     if mask is not None:
         mp, ms = _rows(mask, "mask", (n, -(-shape[1] // 32)), i32)
-    st = (_lib or lib()).pad_chunk_probs(plan._h, shape[1], int(lk is plan._bf16), lp, ls, _dev(params, "params", (ne, 4), f32),
-                                         _dev(tokens, "tokens", (n,), i32), hp, hw, hl, bt, bv, bw, bl, mp, ms,
-                                         int(pk is plan._bf16), pp, ps, _stream_handle(stream))
+    st = (_lib or lib()).pad_chunk_probs(plan._h, shape[1], 1 if lk is plan._bf16 else 0, lp, ls, pa, to, hp, hw, hl, bt, bv, bw, bl, mp, ms,
+                                         1 if pk is plan._bf16 else 0, pp, ps, _stream_handle(stream))
     if st:
         _check(st)
 

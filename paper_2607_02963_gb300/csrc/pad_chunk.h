@@ -98,7 +98,7 @@ cudaError_t launch_chunk_rope(const ChunkParams& p, int head_dim, int kv_format,
 // rows16: 16-row groups that the items' rows take, 1 or 2.  early: not the call's first kernel.
 cudaError_t launch_chunk_mma(const ChunkParams& p, int head_dim, bool fp8, int rows16, bool early, const ChunkItem* items,
                              int n_items, cudaStream_t s);
-// The same over 4-bit pages; rows8: groups of eight rows, 1 to 4.
+// The same over 4-bit pages; rows8: groups of eight rows, 1 to 3.
 cudaError_t launch_chunk_mma4(const ChunkParams& p, int head_dim, int rows8, bool early, const ChunkItem* items, int n_items,
                               cudaStream_t s);
 int chunk_mma4_ctas(int head_dim, int rows8);  // that an SM takes

@@ -31,9 +31,11 @@ constexpr int kMinSplit = 256;
 // Rows of a branch (tokens x group) up to which the warp-level kernel takes it: two 16-row groups.  13 branches
 // of 35 rows over a prefix of 8219 take 25.4 us with this limit, 29.7 with 48 or 64, where they go in pieces.
 constexpr int kMmaRows = 32;
-// The same over 4-bit pages, which the warp-level kernel takes in pieces of 32 rows that each widen the keys again; beyond
-// it they are widened once, to bf16 pages in the workspace, for the tcgen05 kernel.
-constexpr int kMma4Rows = 192;
+// The same over 4-bit pages, which the warp-level kernel takes in pieces of some 16 rows that each widen the keys again; beyond
+// it they are widened once, to bf16 pages in the workspace, for the tcgen05 kernel.  (us; 56, 112, 196 rows, 28/4 heads,
+// head_dim 128: 16 sequences of 2048 to 8192 keys, in pieces 60, 109, 170, widened 87, 91, 101; one of 30000, 31, 46, 72 and
+// 42, 43, 51.  14/2 heads, head_dim 64: 25, 37, 61 and 35, 36, 45; 21, 25, 31 and 27, 29, 29.)
+constexpr int kMma4Rows = 96;
 
 size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
@@ -135,7 +137,7 @@ void split_by(Segment& s, int64_t len, int64_t unit) {
 // SM), and key ranges are cut so that there are some eight CTAs for each SM, no shorter than
 // kMinSplit keys.  (16 x 1 token over 333k cached tokens, 28/4 heads: 121 us in bf16 and 91 in 8 bits; with four CTAs
 // for each SM 127 and 98, with sixteen 133 and 110.  128 or 512 keys make no difference beyond a short call's noise.)
-// 4-bit pages: tiles of eight rows, up to four; a branch of more rows in pieces of about as many tokens.  The ranges there
+// 4-bit pages: tiles of eight rows, up to three; a branch of more rows in pieces of about as many tokens.  The ranges there
 // are the shortest that make no more CTAs than fit the GPU at once: a CTA's start and end cost as much as two of
 // its blocks, and a few CTAs beyond one wave as much as the wave.
 void cut_mma(std::vector<Segment>& segs, int paged, const pad_problem& prob, bool fp4, int sms, int& rows, int& tpt) {
@@ -144,7 +146,9 @@ void cut_mma(std::vector<Segment>& segs, int paged, const pad_problem& prob, boo
   for (const Segment& s : segs)
     if (!s.tc && s.paged == paged) longest = std::max(longest, s.ntok);
   if (fp4) {
-    const int pieces = (longest + 32 / G - 1) / (32 / G);
+    // (one tile of up to 24 rows takes 29 us where two of 16 take 34, four of 14 take 60 where two of 28 take 65: 21 and
+    // 56 rows over 16 sequences as above)
+    const int most = longest * (int64_t)G <= 24 ? longest : 16 / G, pieces = (longest + most - 1) / most;
     tpt = (longest + pieces - 1) / pieces;
     rows = (tpt * G + 7) / 8;
   } else {

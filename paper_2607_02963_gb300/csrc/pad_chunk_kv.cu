@@ -29,6 +29,18 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kReadTokens = 32;  // of a span
 
+// Division by a count that the launch brings, as a product with 2^32 / d rounded up: the quotient, or one more where n d is
+// above 2^32.
+struct Divisor {
+  uint32_t d, inv;
+  __device__ explicit Divisor(int by) : d((uint32_t)by), inv(0xffffffffu / (uint32_t)by + 1u) {}
+  __device__ int operator()(int n) const {
+    if (d == 1u) return n;
+    const uint32_t q = __umulhi((uint32_t)n, inv);
+    return (int)(q * d > (uint32_t)n ? q - 1u : q);
+  }
+};
+
 // 16 lanes of 8 bf16 values (8 at head_dim 64) hold a token and head: one 8-bit group, or a 4-bit one for two lanes.
 template <int D, int FMT>
 __global__ void __launch_bounds__(kThreads) chunk_append_kernel(const __grid_constant__ ChunkParams p,
@@ -41,6 +53,7 @@ __global__ void __launch_bounds__(kThreads) chunk_append_kernel(const __grid_con
   const ChunkPages w = work[blockIdx.x];
   int32_t* entry = p.page_table + (int64_t)w.event * p.max_pages + w.column;
   const int page = w.page >= 0 ? w.page : __ldcg(entry);
+  const Divisor rows(2 * p.h_kv);
   const int groups = w.count * p.h_kv * 2, lanes = (groups * L + 31) / 32 * 32, c = threadIdx.x % L;
   constexpr int U = 4;  // groups of a thread under way together
 #pragma unroll 1
@@ -48,7 +61,7 @@ __global__ void __launch_bounds__(kThreads) chunk_append_kernel(const __grid_con
     uint4 x[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int g = (i0 + u * kThreads) / L, tok = g / (2 * p.h_kv), r = g % (2 * p.h_kv);
+      const int g = (i0 + u * kThreads) / L, tok = rows(g), r = g - tok * 2 * p.h_kv;
       x[u] = make_uint4(0u, 0u, 0u, 0u);
       if (g < groups) x[u] = __ldcs(reinterpret_cast<const uint4*>(((r & 1) ? v_new : k_new) + (w.tok + tok) * stride + (r >> 1) * D) + c);
     }
@@ -63,7 +76,7 @@ __global__ void __launch_bounds__(kThreads) chunk_append_kernel(const __grid_con
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       if (i0 + u * kThreads >= lanes) break;  // (whole warps)
-      const int g = (i0 + u * kThreads) / L, tok = g / (2 * p.h_kv), r = g % (2 * p.h_kv), h = r >> 1;
+      const int g = (i0 + u * kThreads) / L, tok = rows(g), r = g - tok * 2 * p.h_kv, h = r >> 1;
       const bool on = g < groups;
       const int64_t slot = ((int64_t)page * p.h_kv + h) * p.page_size + w.slot + tok;
       store_group<D, FMT>(x[u], c, on, slot, (r & 1) ? v_pool : k_pool, (r & 1) ? v_scale : k_scale);
@@ -103,6 +116,7 @@ __global__ void __launch_bounds__(kThreads) chunk_read_kernel(const __grid_const
   }
   __syncthreads();
   const int n = count * p.h_kv * L, c = threadIdx.x % L;
+  const Divisor heads(p.h_kv);
   constexpr int U = 4;  // rows of a thread under way together, K and V
 #pragma unroll 1
   for (int i0 = threadIdx.x; i0 < n; i0 += U * kThreads) {
@@ -111,7 +125,7 @@ __global__ void __launch_bounds__(kThreads) chunk_read_kernel(const __grid_const
     int64_t to[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int i = i0 + u * kThreads, g = i / L, h = g % p.h_kv, t = g / p.h_kv;
+      const int i = i0 + u * kThreads, g = i / L, t = heads(g), h = g - t * p.h_kv;
       if constexpr (kWiden)
         to[u] = i < n ? ((((int64_t)mine.page0 + ((pos + t) >> p.page_shift)) * p.h_kv + h) * p.page_size + ((pos + t) & (p.page_size - 1))) * D + 8 * c : -1;
       else

@@ -1,6 +1,6 @@
 // Attention of a step's chunk tokens over pages held in 4 bits, on the warp-level tensor-core path (mma.sync).
 //
-// o_t = sum_j softmax_j(scale q_t . k_j) v_j over the keys j that token t sees.  An item is a range of keys for up to 32
+// o_t = sum_j softmax_j(scale q_t . k_j) v_j over the keys j that token t sees.  An item is a range of keys for up to 24
 // rows (chunk tokens x the G query heads of a kv-head); a CTA of four warps takes an item and a kv-head, each warp every
 // fourth block of 32 keys with states of its own, joined through shared memory at the end.
 //
@@ -60,7 +60,7 @@ constexpr int smem_bytes() {
   return ring > join ? ring : join;
 }
 template <int D, int NT>
-constexpr int ctas_per_sm() { return D == 128 ? (NT == 1 ? 4 : NT == 2 ? 3 : 2) : (NT <= 2 ? 4 : 3); }
+constexpr int ctas_per_sm() { return D == 128 ? (NT == 1 ? 4 : NT == 2 ? 3 : 2) : (NT <= 2 ? 4 : 2); }
 
 __device__ __forceinline__ void cp16(uint32_t dst, const void* src, uint32_t n) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
@@ -484,15 +484,15 @@ cudaError_t launch(const ChunkParams& p, bool early, const ChunkItem* items, int
 }  // namespace
 
 int chunk_mma4_ctas(int head_dim, int rows8) {
-  static constexpr int kCtas[2][4] = {{ctas_per_sm<64, 1>(), ctas_per_sm<64, 2>(), ctas_per_sm<64, 3>(), ctas_per_sm<64, 4>()},
-                                      {ctas_per_sm<128, 1>(), ctas_per_sm<128, 2>(), ctas_per_sm<128, 3>(), ctas_per_sm<128, 4>()}};
+  static constexpr int kCtas[2][3] = {{ctas_per_sm<64, 1>(), ctas_per_sm<64, 2>(), ctas_per_sm<64, 3>()},
+                                      {ctas_per_sm<128, 1>(), ctas_per_sm<128, 2>(), ctas_per_sm<128, 3>()}};
   return kCtas[head_dim == 128][rows8 - 1];
 }
 
 cudaError_t launch_chunk_mma4(const ChunkParams& p, int head_dim, int rows8, bool early, const ChunkItem* items, int n_items,
                               cudaStream_t s) {
-  static constexpr decltype(&launch<128, 1>) kForms[2][4] = {{launch<64, 1>, launch<64, 2>, launch<64, 3>, launch<64, 4>},
-                                                             {launch<128, 1>, launch<128, 2>, launch<128, 3>, launch<128, 4>}};
+  static constexpr decltype(&launch<128, 1>) kForms[2][3] = {{launch<64, 1>, launch<64, 2>, launch<64, 3>},
+                                                             {launch<128, 1>, launch<128, 2>, launch<128, 3>}};
   return kForms[head_dim == 128][rows8 - 1](p, early, items, n_items, s);
 }
 

@@ -10,12 +10,14 @@
 
 namespace pad {
 
-// The 4-bit codes of eight values with scale byte `byte`.  x / s is x times the rounded 1 / s, 2^-22 off at most, rounded
+// The 4-bit codes of eight values with scale byte `byte`.  x / s is x times 1 / s, 2^-22 off at most, rounded
 // to f16 on the way: x has eight significant bits and s four, so that x / s either is a number half way between two
 // codes (three significant bits), which f16 restores, or is 2^-8 of itself away from every one, further than f16 moves it.
 __device__ __forceinline__ uint32_t e2m1_codes(const uint32_t (&x)[4], uint32_t byte) {
   const float s = (byte >> 3) ? __uint_as_float((byte + 896u) << 20) : (float)byte * 0x1p-17f;
-  const float inv = byte == 0u ? 0.f : 1.f / s;
+  float inv;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(s));
+  if (byte == 0u) inv = 0.f;
   float y[8];
 #pragma unroll
   for (int j = 0; j < 4; ++j) {

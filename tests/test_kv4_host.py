@@ -70,15 +70,14 @@ def test_long_chunks_bring_a_workspace_for_widened_pages(padlib):
     assert B.pad_chunk_workspace_size(_prob(), None, None, [0, 9], [300, 0], kv_format=B.KV_FP4) > 0
 
 
-@pytest.mark.parametrize("group,news", [(7, [1, 2, 3, 4, 5, 8, 9]), (16, [1, 2, 3]), (1, [1, 7, 32, 33]), (3, [11])])
+@pytest.mark.parametrize("group,news", [(7, [1, 2, 3, 4, 5, 8, 9]), (16, [1, 2, 3]), (1, [1, 7, 24, 25, 96]), (3, [8, 9, 11])])
 def test_items_cover_the_tokens(padlib, group, news):
-    """Pieces of 32 rows at most, about as long as one another."""
+    """One piece of up to 24 rows, pieces of up to 16 where there are more, about as long as one another."""
     for n in news:
         plan = B.pad_chunk_plan(_prob(h_q=group, h_kv=1), None, None, None, [100], [n], page_table=torch.zeros(1, 64, dtype=torch.int32),
                                 n_pages=64, kv_format=B.KV_FP4)
         i = plan.info()
-        per = 32 // group
-        pieces = -(-n // per)
+        pieces = 1 if n * group <= 24 else -(-n // (16 // group))
         assert i["tc_items"] == 0 and i["mma_items"] == -(-n // (-(-n // pieces))) * i["page_splits"]
 
 
