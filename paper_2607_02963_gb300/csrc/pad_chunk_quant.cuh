@@ -7,6 +7,7 @@
 #include <cstdint>
 
 #include "pad_chunk.h"
+#include "pad_tc_common.cuh"
 
 namespace pad {
 
@@ -18,10 +19,12 @@ __device__ __forceinline__ uint32_t e2m1_codes(const uint32_t (&x)[4], uint32_t 
   float inv;
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(s));
   if (byte == 0u) inv = 0.f;
+  const uint64_t inv2 = tc::f2pack(inv, inv);
   float y[8];
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
-    const __half2 h = __floats2half2_rn(__uint_as_float(x[j] << 16) * inv, __uint_as_float(x[j] & 0xffff0000u) * inv);
+    const uint64_t p = tc::fmul2(tc::f2pack(__uint_as_float(x[j] << 16), __uint_as_float(x[j] & 0xffff0000u)), inv2);
+    const __half2 h = __floats2half2_rn(tc::f2lo(p), tc::f2hi(p));
     y[2 * j] = __low2float(h);
     y[2 * j + 1] = __high2float(h);
   }
@@ -33,11 +36,12 @@ __device__ __forceinline__ uint32_t e2m1_codes(const uint32_t (&x)[4], uint32_t 
       : "=r"(r) : "f"(y[0]), "f"(y[1]), "f"(y[2]), "f"(y[3]), "f"(y[4]), "f"(y[5]), "f"(y[6]), "f"(y[7]));
   return r;
 }
-// The scale byte of a group whose largest magnitude has this bf16 pattern: max / 6 (no tie is moved by that division's
-// rounding: the quotient of an eight-bit number by 3 that lies half way between two scales is exact) to the nearest.
+// The scale byte of a group whose largest magnitude has this bf16 pattern: max / 6 to the nearest.  The product with 1 / 6,
+// which is 2^-25 of itself off as an fp32 number, is enough: a quotient that lies half way between two scales comes out exact
+// (2^-25 t is less than half a step of t, t < 2), and any other lies 2^-8 of itself from there (max has eight significant bits).
 __device__ __forceinline__ uint32_t e2m1_scale(uint32_t m) {
   if (m >= 0x7f80u) return 255u;
-  const float s = __fdiv_rn(__uint_as_float(m << 16), 6.f);
+  const float s = __uint_as_float(m << 16) * (1.f / 6.f);
   const uint32_t u = __float_as_uint(s);
   const uint32_t b = s < 0x1p-14f ? (uint32_t)rintf(s * 0x1p17f) : ((u + 0x7ffffu + ((u >> 20) & 1u)) >> 20) - 896u;
   return min(b, 226u);
@@ -53,10 +57,9 @@ __device__ __forceinline__ void store_group(uint4 x, int c, bool on, int64_t slo
     return;
   }
   // the largest magnitude as a bf16 pattern: integer order is theirs, NaN and infinity on top
-  uint32_t m = 0u;
   const uint32_t xs[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-  for (int j = 0; j < 4; ++j) m = max(m, max(xs[j] & 0x7fffu, (xs[j] >> 16) & 0x7fffu));
+  uint32_t m = __vmaxu2(__vmaxu2(xs[0] & 0x7fff7fffu, xs[1] & 0x7fff7fffu), __vmaxu2(xs[2] & 0x7fff7fffu, xs[3] & 0x7fff7fffu));
+  m = max(m & 0xffffu, m >> 16);
 #pragma unroll
   for (int o = FMT == PAD_KV_FP4 ? 1 : L / 2; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
   if (FMT == PAD_KV_FP4) {
