@@ -711,10 +711,14 @@ def pad_chunk_attn(plan: ChunkPlan, q, k_prefix, v_prefix, k_pool, v_pool, out, 
     kp, vp, ksc, vsc = plan._pools(k_pool, v_pool, k_scale, v_scale)
     kx, vx = None, None
     if k_prefix is not None:
-        if k_prefix.shape[0] < plan._prefix_tokens:
-            raise ValueError(f"k_prefix: {k_prefix.shape[0]} tokens, the plan reads {plan._prefix_tokens}")
-        kx = _dev(k_prefix, "k_prefix", (k_prefix.shape[0],) + plan._new_shape[1:], plan._bf16)
-        vx = _dev(v_prefix, "v_prefix", k_prefix.shape, plan._bf16)
+        shape, bf16 = k_prefix.shape, plan._bf16
+        if shape[0] < plan._prefix_tokens:
+            raise ValueError(f"k_prefix: {shape[0]} tokens, the plan reads {plan._prefix_tokens}")
+        if not (v_prefix is not None and shape[1:] == plan._new_shape[1:] and v_prefix.shape == shape and k_prefix.dtype is bf16
+                and v_prefix.dtype is bf16 and k_prefix.is_contiguous() and k_prefix.is_cuda and v_prefix.is_contiguous() and v_prefix.is_cuda):
+            _dev(k_prefix, "k_prefix", (shape[0],) + plan._new_shape[1:], bf16)
+            _dev(v_prefix, "v_prefix", shape, bf16)
+        kx, vx = k_prefix.data_ptr(), _ptr(v_prefix)
     st = (_lib or lib()).pad_chunk_attn(plan._h, qp, qs, kx, vx, kp, vp, ksc, vsc, out.data_ptr(), lp,
                                         _stream_handle(stream))
     if st:

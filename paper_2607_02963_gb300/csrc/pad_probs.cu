@@ -4,11 +4,13 @@
 // p = softmax(x / T) wants the row twice, for its maximum and sum and for the result.  A cluster takes a row, each CTA a
 // slice of it that stays in its threads' registers between the two: a row is read once and written once, whatever its
 // length, and what is done to it in between (penalties and biases at a few hundred places, the mask) costs no memory
-// traffic.  Bound by how long a CTA lives, 8 to 12 us, for its chain (event, context, slice, maximum, sum, the cluster's
-// meeting, the way out) and how many of them the GPU holds: 180 rows of 150001 in fp32, contexts of 2048 on average, 78 us,
-// 60 without contexts; 64 rows of 131072 in bf16 with a mask and biases 35 us; 5 rows of 32768 under 9 us, the host's call.
-// (Two passes without clusters, the second joining the slices of the first: 74 us, 33 and 12; the slice in shared memory
-// instead of registers 77, 35 and 9; the next wave's rows fetched to L2 ahead: no gain.)
+// traffic.  As many clusters as the GPU holds take rows in turn.  Bound by the chain that a row is to its CTAs, 10 to 14 us
+// (event, context, slice, maximum, sum, the cluster's meeting, the way out), and by the 36 rows that are under way
+// together: 180 rows of 150001 in fp32 take 71 us, contexts of 2048 tokens on average, 57 without contexts; 64 rows of 131072
+// in bf16 with a mask and biases 34 us; 5 rows of 32768 under 9 us, the host's call.
+// (A cluster launched for each row: 77 us, a third of the GPU waiting for a whole cluster's room.  Two passes without
+// clusters, the second joining the slices of the first: 74 us, 33 and 12.  The slice in shared memory instead of
+// registers: 77, 35 and 9.  The next row's slice fetched to L2 ahead, its event looked up ahead: no gain.)
 //
 // How often a token occurs in the context is counted in a plane of integers over the slice in shared memory: additions of
 // whole numbers, whose order does not matter.  The pass for the maximum reads the counts beside the logits, where a
@@ -59,7 +61,7 @@ __device__ __forceinline__ void join_max(Part& a, const Part& b) {
   a.nan |= b.nan;
 }
 
-// The entries of a vector changed by what the context, the biases and the mask say of them.  at: place in the planes, i: in the slice.
+// The entries of a vector changed by what the context, the biases and the mask say of them.  at: place in the planes.
 struct Change {
   const uint32_t* plane;
   const float* bias;
@@ -105,19 +107,24 @@ __device__ __forceinline__ void keep_allowed(float (&y)[E], const Change& h, int
 // WIDE: 32-bit counts.
 template <class TL, class TP, bool LONG, bool WIDE>
 __global__ void __launch_bounds__(Shape<LONG>::kThreads, LONG ? 1 : 2)
-    probs_kernel(const __grid_constant__ ChunkProbs a, const ChunkVerify* __restrict__ work, int slice, int staged) {
+    probs_kernel(const __grid_constant__ ChunkProbs a, const ChunkVerify* __restrict__ work, int rows, int slice, int staged) {
   using S = Shape<LONG>;
   constexpr int T = S::kThreads, E = sizeof(TL) == 2 || sizeof(TP) == 2 ? 8 : 4, K = S::kEach / E;  // entries of a vector, vectors of a thread
   extern __shared__ __align__(16) uint8_t smem[];
   __shared__ Part warp_part[S::kWarps];
-  __shared__ Part parts[kMaxCtas];
+  __shared__ Part both[2][kMaxCtas];  // of the row at hand and the one before
   __shared__ ChunkVerify mine;
   __shared__ int event;
   __shared__ uint32_t touched[S::kWarps];  // bit k: a context's token is in the warp's k-th vectors
   cg::cluster_group cl = cg::this_cluster();
   const int rank = (int)cl.block_rank(), ctas = (int)cl.num_blocks();
-  const int row = (int)blockIdx.x / ctas, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   cl.barrier_arrive();  // (every CTA of the cluster runs before one writes into another's memory)
+  const int stride = (int)gridDim.x / ctas;
+  const int first_row = (int)blockIdx.x / ctas;
+#pragma unroll 1
+  for (int row = first_row, turn = 0; row < rows; row += stride, turn ^= 1) {
+  Part* const parts = both[turn];
   // which event and place in its chunk the row has
   for (int e = threadIdx.x; e < a.n_events; e += T) {
     const ChunkVerify w = work[e];
@@ -204,7 +211,9 @@ __global__ void __launch_bounds__(Shape<LONG>::kThreads, LONG ? 1 : 2)
           if (t[u] >= 0 && at < width) {
             atomicAdd(plane + (WIDE ? at : at >> 1), WIDE ? 1u : 1u << (16 * (at & 1)));
             const uint32_t v = at / E;
-            atomicOr(touched + v % T / 32, 1u << (v / T));
+            const uint32_t bit = 1u << (v / T);
+            volatile uint32_t* const mark = touched + v % T / 32;
+            if (!(*mark & bit)) atomicOr(touched + v % T / 32, bit);  // (contexts repeat themselves: few get here)
           }
         }
       }
@@ -334,9 +343,9 @@ __global__ void __launch_bounds__(Shape<LONG>::kThreads, LONG ? 1 : 2)
     q.l = tc::f2lo(l[0]) + tc::f2hi(l[0]);
     block_join(true);
   }
-  cl.barrier_wait();
+  if (row == first_row) cl.barrier_wait();
   if ((int)threadIdx.x < ctas) *cl.map_shared_rank(&parts[rank], threadIdx.x) = q;
-  cl.sync();  // (nobody reads or writes another CTA's memory after this)
+  cl.sync();  // (another CTA writes to `parts` next two rows on, after it has met this one again)
   Part all{kNegInf, 0.f, 0x7fffffff, 0};
   if (lane < ctas) all = parts[lane];
   const float part_m = all.m;
@@ -412,25 +421,26 @@ __global__ void __launch_bounds__(Shape<LONG>::kThreads, LONG ? 1 : 2)
         if ((s == 0 ? v0 > 0 && v1 > 0 : ragged_end) && t >= 0 && t < hi) dst[t] = TP(z[s][u] * scale);
       }
   }
+  __syncthreads();  // (shared memory is the next row's)
+  }
 }
 
 template <class TL, class TP, bool LONG, bool WIDE>
 cudaError_t launch(const ChunkProbs& a, const ChunkVerify* work, int rows, int ctas, int slice, bool staged, cudaStream_t s) {
   auto* kernel = probs_kernel<TL, TP, LONG, WIDE>;
-  constexpr int most = Shape<LONG>::kSlice;
+  constexpr int longest = Shape<LONG>::kSlice;
   static bool configured[64] = {};
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
   if (dev < 0 || dev >= 64 || !configured[dev]) {
-    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(count_bytes(most, WIDE) + bias_bytes(most)));
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(count_bytes(longest, WIDE) + bias_bytes(longest)));
     if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
     if (e != cudaSuccess) return e;
     if (dev >= 0 && dev < 64) configured[dev] = true;
   }
   const size_t planes = (a.history != nullptr || a.tokens != nullptr ? count_bytes(slice, WIDE) : 0) + (a.bias_token != nullptr ? bias_bytes(slice) : 0);
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(rows * ctas));
   cfg.blockDim = dim3(Shape<LONG>::kThreads);
   cfg.dynamicSmemBytes = std::max(planes, staged ? stage_bytes(slice) : 0);
   cfg.stream = s;
@@ -440,7 +450,21 @@ cudaError_t launch(const ChunkProbs& a, const ChunkVerify* work, int rows, int c
   attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, kernel, a, work, slice, staged ? 1 : 0);
+  // as many clusters as the GPU holds, each taking rows in turn: with one for each row, the 16 or eight CTAs' room comes free
+  // piece by piece, and a third of the GPU waits for the rest of it
+  static thread_local size_t known_smem[64];
+  static thread_local int known_ctas[64], known[64];
+  const bool keep = dev >= 0 && dev < 64;
+  int most = keep && known[dev] > 0 && known_smem[dev] == cfg.dynamicSmemBytes && known_ctas[dev] == ctas ? known[dev] : 0;
+  if (most == 0) {
+    cfg.gridDim = dim3((unsigned)ctas);
+    e = cudaOccupancyMaxActiveClusters(&most, kernel, &cfg);
+    if (e != cudaSuccess) return e;
+    if (most < 1) return cudaErrorLaunchOutOfResources;
+    if (keep) known_smem[dev] = cfg.dynamicSmemBytes, known_ctas[dev] = ctas, known[dev] = most;
+  }
+  cfg.gridDim = dim3((unsigned)(std::min(rows, most) * ctas));
+  return cudaLaunchKernelEx(&cfg, kernel, a, work, rows, slice, staged ? 1 : 0);
 }
 
 template <class TL, class TP>
@@ -461,8 +485,8 @@ cudaError_t launch(const ChunkProbs& a, const ChunkVerify* work, int rows, int c
 int chunk_probs_max_vocab() { return kMaxCtas * Shape<true>::kSlice - 64; }
 
 cudaError_t launch_chunk_probs(const ChunkProbs& a, const ChunkVerify* work, int n_tokens, cudaStream_t s) {
-  // a row over as many CTAs as leave each 2048 entries, eight where they hold it (16 find room on the GPU less often:
-  // 180 rows of 150001 take 82 us with 16 CTAs of half as many threads)
+  // a row over as many CTAs as leave each 2048 entries, eight where they hold it (with 16 of half as many
+  // threads 180 rows of 150001 take 82 us, not 71)
   int ctas = 1;
   while (ctas < kMaxCtas && a.vocab > ctas * (ctas < 8 ? 2048 : Shape<false>::kSlice - 64)) ctas *= 2;
   const int slice = (a.vocab + 7 + 32 * ctas - 1) / (32 * ctas) * 32;  // (the first begins up to seven entries before the row)

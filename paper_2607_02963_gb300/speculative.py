@@ -101,30 +101,44 @@ def example(events=6, drafts=4, steps=5, prefix=2048, vocab=4096, kv_format=B.KV
     cache = BranchCache(h_q, h_kv, head_dim, events, n_pages=events * 16, max_pages=16, kv_format=kv_format,
                         prefix_len=[prefix], event_video=[0] * events)
     k_prefix, v_prefix = randn(prefix, h_kv, head_dim), randn(prefix, h_kv, head_dim)
+    rope = B.Rope(head_dim, theta=1.0e6)
+    # a branch's last token, what it has said so far, and how it is to say more: temperature, repetition, frequency, presence
+    last = torch.randint(0, vocab, (events,), generator=g, device="cuda", dtype=torch.int32)
+    said = torch.zeros(events, steps * (drafts + 1), dtype=torch.int32, device="cuda")
+    said_len = torch.zeros(events, dtype=torch.int32, device="cuda")
+    params = torch.tensor([[0.9, 1.1, 0.1, 0.1]], device="cuda").repeat(events, 1)
     kept = []
     for _ in range(steps):
         plan = cache.plan([drafts + 1] * events)
         n = plan.n_tokens
-        cache.append(plan, randn(n, h_kv, head_dim), randn(n, h_kv, head_dim))
-        out = cache.attend(plan, randn(n, h_q, head_dim), k_prefix, v_prefix)
+        start = torch.from_numpy(prefix + cache.event_len).cuda()
+        position = (start[:, None] + torch.arange(drafts + 1, device="cuda")).reshape(-1).int()
+        q = cache.append_rope(plan, rope, position, randn(n, h_q, head_dim), randn(n, h_kv, head_dim), randn(n, h_kv, head_dim))
+        out = cache.attend(plan, q, k_prefix, v_prefix)
         # stand-ins for the target's and the draft's distributions: the same logits, one with an error
         logits = 3.0 * torch.randn(n, vocab, generator=g, device="cuda")
-        p = torch.softmax(logits, -1)
         rows = torch.arange(n, device="cuda").view(events, drafts + 1)[:, :drafts].reshape(-1)
-        q = torch.softmax(logits[rows] + 0.5 * torch.randn(len(rows), vocab, generator=g, device="cuda"), -1)
-        draft = torch.multinomial(q, 1, generator=g)[:, 0].to(torch.int32)
-        accepted, _token = cache.verify(plan, p, q, draft, torch.rand(len(rows), generator=g, device="cuda"),
-                                        torch.rand(events, generator=g, device="cuda"))
+        dq = torch.softmax(logits[rows] + 0.5 * torch.randn(len(rows), vocab, generator=g, device="cuda"), -1)
+        draft = torch.multinomial(dq, 1, generator=g)[:, 0].to(torch.int32)
+        chunk = torch.cat([last[:, None], draft.view(events, drafts)], 1)
+        p = cache.probs(plan, logits, params=params, history=said, history_len=said_len, tokens=chunk.reshape(-1))
+        accepted, token = cache.verify(plan, p, dq, draft, torch.rand(len(rows), generator=g, device="cuda"),
+                                       torch.rand(events, generator=g, device="cuda"))
         B.pad_chunk_status(plan)
         if not bool(torch.isfinite(out).all()):
             raise RuntimeError("attention returned values that are not finite")
         cache.commit(plan, accepted)
+        for e, m in enumerate((accepted + 1).tolist()):   # the chunk's tokens up to the last accepted one are said
+            at = int(said_len[e])
+            said[e, at:at + m] = chunk[e, :m]
+        said_len += accepted + 1
+        last = token
         kept.append((accepted + 1).tolist())
     return kept, cache
 
 
 def main():
-    for name, fmt in (("bf16", B.KV_BF16), ("8 bits", B.KV_FP8)):
+    for name, fmt in (("bf16", B.KV_BF16), ("8 bits", B.KV_FP8), ("4 bits", B.KV_FP4)):
         kept, cache = example(kv_format=fmt)
         print(f"cache in {name}:")
         for i, row in enumerate(kept):

@@ -388,3 +388,63 @@ def test_a_step_captured_and_replayed(fmt):
         for x, w in zip((q_out, out, p, acc, tok, *pools), want[i]):
             assert torch.equal(x.view(torch.uint8), w.view(torch.uint8))
     B.pad_chunk_status(plan)
+
+
+@pytest.mark.parametrize("fmt", [B.KV_BF16, B.KV_FP8, B.KV_FP4])
+def test_steps_of_a_loop_against_the_oracle(fmt):
+    """Three steps of a loop (rotary append, attention, probabilities, verification, commit) on one cache, each held against the
+    oracle: the queries turned, attention over what the cache reads back as (that the cache holds the turned keys is tested
+    above), the probabilities, and the drafts that those keep."""
+    g = torch.Generator().manual_seed(11)
+    events, vocab, h_q, h_kv, d = 3, 700, 14, 2, 64
+    cache = BranchCache(h_q, h_kv, d, events, 60, 20, page_size=8, kv_format=fmt, out_dtype=0)
+    spec = dict(rotary_dim=48, theta=1e4, scaling="turns", factor=4.0, original_len=512.0)
+    rope = B.Rope(d, **spec)
+    news = [[5, 1, 9], [40, 3, 0], [2, 8, 4]]
+    for i, n_new in enumerate(news):
+        plan = cache.plan(n_new)
+        n, lens = plan.n_tokens, cache.event_len.copy()
+        ev = np.repeat(np.arange(events), n_new)
+        pos = np.concatenate([lens[e] + np.arange(m) for e, m in enumerate(n_new)]).astype(np.int32)
+        q, k, v = _randn(g, n, h_q, d), _randn(g, n, h_kv, d), _randn(g, n, h_kv, d)
+        q_out = cache.append_rope(plan, rope, torch.from_numpy(pos).cuda(), q.cuda(), k.cuda(), v.cuda())
+        want, tol, _ = _want(spec, d, q, pos, "half")
+        assert np.all(np.abs(q_out.double().cpu().numpy() - want) <= tol + 2.0 ** -8 * (np.abs(want) + tol))
+        kk, vv = (x.double().cpu().numpy() for x in cache.read(plan))
+        out = cache.attend(plan, q_out).double().cpu().numpy()
+        first = np.concatenate([[0], np.cumsum(lens + np.asarray(n_new))])
+        for e in range(events):
+            mine = slice(first[e], first[e + 1])
+            o, _, mag = oracle.chunk_attention(q_out[ev == e].double().cpu().numpy(), kk[mine], vv[mine], int(lens[e]) + 1, d ** -0.5)
+            assert np.all(np.abs(out[ev == e] - o) <= (2.0 ** -8 + 1e-4) * mag)
+        r = Rows(20 + i, n_new, vocab, 30, 5, 0.6)
+        r.plan = plan
+        p = r.run()
+        r.check(p)
+        nd = plan.n_drafts
+        drafted = np.concatenate([np.flatnonzero(ev == e)[:-1] for e in range(events)]).astype(int)
+        dq = torch.softmax(torch.log(p[drafted].clamp_min(1e-9)) + 0.4 * torch.randn(nd, vocab, generator=g).cuda(), 1)
+        draft = dq.argmax(1).int() if nd else torch.empty(0, dtype=torch.int32, device="cuda")
+        ua, up = torch.rand(nd, generator=g), torch.rand(events, generator=g)
+        accepted, token = cache.verify(plan, p, dq, draft, ua.cuda(), up.cuda())
+        B.pad_chunk_status(plan)
+        at = 0
+        for e, m in enumerate(n_new):
+            if m == 0:
+                assert int(token[e]) == -1
+                continue
+            rows = np.flatnonzero(ev == e)
+            want = oracle.draft_verify(p[rows].cpu().numpy(), dq[at:at + m - 1].cpu().numpy(), draft[at:at + m - 1].tolist(),
+                                       ua[at:at + m - 1].numpy(), float(up[e]))
+            assert (int(accepted[e]), int(token[e])) == want
+            at += m - 1
+        lens = np.where(np.asarray(n_new) > 0, lens + accepted.cpu().numpy() + 1, lens)
+        assert np.array_equal(cache.commit(plan, accepted), lens)
+
+
+@pytest.mark.parametrize("fmt", [B.KV_BF16, B.KV_FP4])
+def test_the_example_runs(fmt):
+    from paper_2607_02963_gb300 import speculative
+    kept, cache = speculative.example(events=3, drafts=3, steps=3, prefix=200, vocab=500, h_q=8, h_kv=2, kv_format=fmt)
+    assert len(kept) == 3 and all(1 <= m <= 4 for row in kept for m in row)
+    assert cache.event_len.tolist() == np.sum(kept, axis=0).tolist()
