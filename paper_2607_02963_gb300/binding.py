@@ -742,8 +742,6 @@ def pad_chunk_probs(plan: ChunkPlan, logits, p, params=None, history=None, histo
     else:
         lp, ls = _rows(logits, "logits", shape, lk)
         pp, ps = _rows(p, "p", shape, pk)
-    if lp == pp and (lk is not pk or ls != ps):
-        raise ValueError("p: over logits, their types and strides must be the same")
     hw = bw = ms = 0
     pa = to = hp = hl = bt = bv = bl = mp = None
     if params is not None:
@@ -755,16 +753,23 @@ def pad_chunk_probs(plan: ChunkPlan, logits, p, params=None, history=None, histo
             _dev(tokens, "tokens", plan._row_shape, i32)
         to = tokens.data_ptr()
     if history is not None or history_len is not None:
-        hw = 0 if history is None else history.shape[-1]
-        if not (history is not None and history_len is not None and history.shape == (ne, hw) and history_len.shape == plan._event_shape
+        if history is None or history_len is None:
+            raise ValueError("history and history_len come together")
+        hw = history.shape[-1]
+        if not (history.shape == (ne, hw) and history_len.shape == plan._event_shape
                 and history.dtype is i32 and history_len.dtype is i32 and history.is_contiguous() and history.is_cuda
                 and history_len.is_contiguous() and history_len.is_cuda):
             _dev(history, "history", (ne, hw), i32), _dev(history_len, "history_len", plan._event_shape, i32)
-        hp, hl = _ptr(history), _ptr(history_len)
+        if hw:
+            hp, hl = history.data_ptr(), history_len.data_ptr()
     if bias_token is not None or bias_value is not None or bias_len is not None:
-        bw = 0 if bias_token is None else bias_token.shape[-1]
+        if bias_token is None or bias_value is None or bias_len is None:
+            raise ValueError("bias_token, bias_value and bias_len come together")
+        bw = bias_token.shape[-1]
         bt, bv = _dev(bias_token, "bias_token", (ne, bw), i32), _dev(bias_value, "bias_value", (ne, bw), f32)
         bl = _dev(bias_len, "bias_len", plan._event_shape, i32)
+        if not bw:
+            bt = bv = bl = None
     if mask is not None:
         mp, ms = _rows(mask, "mask", (n, -(-shape[1] // 32)), i32)
     st = (_lib or lib()).pad_chunk_probs(plan._h, shape[1], 1 if lk is plan._bf16 else 0, lp, ls, pa, to, hp, hw, hl, bt, bv, bw, bl, mp, ms,

@@ -479,7 +479,7 @@ pad_status check_stride(int64_t& stride, int64_t packed, int64_t unit, const cha
   return PAD_OK;
 }
 
-// Whether `rows` rows of `width` elements at a and of `width_b` at b (bf16, strides in elements) share memory.
+// Whether `rows` rows of `width` elements at a and of `width_b` at b (of two bytes, strides in elements) share memory.
 bool overlap(const void* a, int64_t stride, int64_t width, const void* b, int64_t stride_b, int64_t width_b, int64_t rows) {
   const intptr_t x = reinterpret_cast<intptr_t>(a) / 2, y = reinterpret_cast<intptr_t>(b) / 2;
   if (x + (rows - 1) * stride + width <= y || y + (rows - 1) * stride_b + width_b <= x) return false;
@@ -527,6 +527,8 @@ pad_status pad_chunk_plan(const pad_problem* prob, int32_t kv_format, pad_cache_
       if (n_pages != 0 && n_pages != size) return api_fail(PAD_ERR_INVALID_ARG, "n_pages=%d, the cache has %d", n_pages, size);
       n_pages = size;
     }
+    if (kv_format == PAD_KV_FP4 && (int64_t)n_pages * prob->h_kv * prob->page_size > UINT32_MAX)
+      return api_fail(PAD_ERR_UNSUPPORTED, "a 4-bit pool of %d pages has more than 2^32 rows", n_pages);
     if (prefix_offset)
       for (int v = 0; v < n_videos; ++v)
         if (prefix_offset[v] < 0 || prefix_offset[v] > ((int64_t)1 << 40)) return api_fail(PAD_ERR_INVALID_ARG, "prefix_offset[%d]", v);
@@ -762,6 +764,10 @@ pad_status pad_chunk_probs(const pad_chunk_t* c, int32_t vocab, int32_t logits_d
     if (!aligned(t, 4)) return api_fail(PAD_ERR_INVALID_ARG, "a tensor is not aligned to its elements");
   if (!aligned(logits, logits_dtype ? 2 : 4) || !aligned(p, p_dtype ? 2 : 4))
     return api_fail(PAD_ERR_INVALID_ARG, "a tensor is not aligned to its elements");
+  const int64_t l2 = logits_dtype ? 1 : 2, p2 = p_dtype ? 1 : 2;
+  if ((p != logits || p_dtype != logits_dtype || p_stride != logits_stride) &&
+      overlap(logits, logits_stride * l2, vocab * l2, p, p_stride * p2, vocab * p2, c->L.n_tokens))
+    return api_fail(PAD_ERR_INVALID_ARG, "p overlaps logits without being logits");
   ChunkProbs a{};
   a.logits = logits;
   a.p = p;

@@ -13,7 +13,8 @@
 // nearest even.  Code times scale has six significant bits at most and is exact in bf16 and in f16 (up to 6 x 10240 = 61440).
 //
 // Bound by memory, one pass each; short ones by the launch.  32768 tokens of 4 heads x 128 written and read back
-// (two calls of 101 MB): 45 us, 4.5 TB/s; 32 branches x 5 tokens written and 9000 read: 12 us.
+// (two calls of 101 MB): 45 us, 4.5 TB/s; 32 branches x 5 tokens written and 9000 read: 12 us.  In 4 bits the same (two calls
+// of 86 MB) 43 us, 4 TB/s, where writing is bound by its instructions (140 for a warp's 256 values); 9000 read 12 us.
 #include <cuda_bf16.h>
 #include <algorithm>
 #include <cstdint>

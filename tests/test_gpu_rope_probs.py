@@ -254,6 +254,38 @@ def test_the_largest_vocabulary_and_one_more():
         B.pad_chunk_probs(r.plan, x, x)
 
 
+def test_probabilities_over_a_part_of_the_logits_are_refused():
+    r = Rows(1, [1, 2], 1000)
+    x = torch.zeros(7, 1000, device="cuda")
+    half = torch.zeros(3, 2000, device="cuda")
+    for logits, p in ((x[:3], x[1:4]), (x[0:6:2], x[:3]), (half[:, :1000], half[:, 999:1999]), (x[:3], x.view(torch.bfloat16)[:3, :1000])):
+        with pytest.raises(B.PadError, match="overlaps"):
+            B.pad_chunk_probs(r.plan, logits, p)
+    B.pad_chunk_probs(r.plan, half[:, :1000], half[:, 1000:])
+    assert ((half[:, 1000:] - 1e-3).abs() < 1e-8).all() and not half[:, :1000].any()
+
+
+@pytest.mark.parametrize("vocab", [393152, 165000, 330000])
+def test_long_rows_with_long_contexts_and_biases(vocab):
+    """32-bit counts and sums of biases beside one another in every form of the kernel."""
+    r = Rows(8, [1, 2], vocab, 70000, 3000, 0.9)
+    r.params[1, 0] = 0.0
+    r.check(r.run())
+
+
+def test_greedy_rows_that_begin_elsewhere():
+    r = Rows(9, [3, 2], 3001, 20, 20, 0.5)
+    r.params[:, 0] = 0.0
+    r.params[:, 1], r.params[:, 2:] = 1.0, 0.0
+    wide = torch.full((5, 3010), 99.0, device="cuda")
+    wide[:, 3:3004] = r.logits.cuda()
+    for kind, b in ((torch.float32, 1), (torch.float32, 3), (torch.bfloat16, 0), (torch.bfloat16, 7)):
+        out = torch.full((5, 3011), 7.0, dtype=kind, device="cuda")
+        r.run(wide[:, 3:3004], out[:, b:b + 3001])
+        r.check(out[:, b:b + 3001])
+        assert (out[:, :b] == 7).all() and (out[:, b + 3001:] == 7).all()
+
+
 def test_contexts_whose_counts_need_32_bits():
     r = Rows(2, [2, 1], 3000, 70000)
     r.history[0] = 5                                  # 70000 times the same token

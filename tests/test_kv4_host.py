@@ -81,6 +81,15 @@ def test_items_cover_the_tokens(padlib, group, news):
         assert i["tc_items"] == 0 and i["mma_items"] == -(-n // (-(-n // pieces))) * i["page_splits"]
 
 
+def test_pools_of_more_rows_than_32_bits_count_are_refused(padlib):
+    table = torch.zeros(1, 4, dtype=torch.int32)
+    def plan(n, fmt):
+        return B.pad_chunk_plan(_prob(page_size=64), None, None, None, [5], [1], page_table=table, n_pages=n, kv_format=fmt)
+    plan((1 << 24) - 1, B.KV_FP4), plan(1 << 24, B.KV_FP8)
+    with pytest.raises(B.PadError, match="2.32 rows"):
+        plan(1 << 24, B.KV_FP4)
+
+
 def test_formats_and_shapes_are_checked(padlib):
     with pytest.raises(B.PadError, match="kv_format=3"):
         B.pad_chunk_workspace_size(_prob(), None, None, [5], [1], kv_format=3)

@@ -119,6 +119,9 @@ def test_what_probs_refuses(padlib):
             call(p=bad)
     with pytest.raises(ValueError, match="mask"):
         call(mask=_zeros(n, 2, dtype=i32))
-    both = _zeros(2 * n, v, dtype=f32)
-    with pytest.raises(ValueError, match="over logits"):
-        call(logits=both[::2], p=both[:n])
+    for name in ("history", "history_len", "bias_token", "bias_value", "bias_len"):
+        with pytest.raises(ValueError, match="come together"):
+            call(**{name: t[name]})
+    with pytest.raises(B.PadError, match="host-only"):   # (a context and biases of width 0 are none)
+        call(history=t["history"][:, :0].contiguous(), history_len=t["history_len"], bias_token=t["bias_token"][:, :0].contiguous(),
+             bias_value=t["bias_value"][:, :0].contiguous(), bias_len=t["bias_len"])
