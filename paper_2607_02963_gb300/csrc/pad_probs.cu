@@ -10,7 +10,8 @@
 // in bf16 with a mask and biases 34 us; 5 rows of 32768 under 9 us, the host's call.
 // (A cluster launched for each row: 77 us, a third of the GPU waiting for a whole cluster's room.  Two passes without
 // clusters, the second joining the slices of the first: 74 us, 33 and 12.  The slice in shared memory instead of
-// registers: 77, 35 and 9.  The next row's slice fetched to L2 ahead, its event looked up ahead: no gain.)
+// registers: 77, 35 and 9.  The next row's slice fetched to L2 ahead, its event looked up ahead: no gain.  Rows of one event
+// one after the other, sharing what is counted: 70 where their length is a multiple of 16 bytes, 76 where it is not.)
 //
 // How often a token occurs in the context is counted in a plane of integers over the slice in shared memory: additions of
 // whole numbers, whose order does not matter.  The pass for the maximum reads the counts beside the logits, where a

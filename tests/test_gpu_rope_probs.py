@@ -246,6 +246,20 @@ def test_probabilities(vocab, bf16):
         assert torch.equal(p, r.run())
 
 
+@pytest.mark.parametrize("bf16", [(False, False), (True, True), (True, False), (False, True)])
+@pytest.mark.parametrize("news,vocab", [([90, 1, 0, 130], 20001), ([90, 60, 70], 20000), ([500, 0, 900], 501)])
+def test_many_rows_of_an_event(news, vocab, bf16):
+    """More rows than are under way together: a cluster takes several of an event's, one after the other."""
+    r = Rows(vocab, news, vocab, 200, 20, 0.5, bf16)
+    r.params[-1, 0] = 0.0
+    r.check(r.run())
+    out = torch.full((len(r.logits), vocab + 3), 7.0, dtype=r.kind, device="cuda")   # (rows that lie elsewhere on their way out)
+    r.run(p=out[:, 1:1 + vocab])
+    r.check(out[:, 1:1 + vocab])
+    r.bias = r.allowed = None
+    r.check(r.run())
+
+
 def test_the_largest_vocabulary_and_one_more():
     r = Rows(1, [1, 2], 393152, 100, 10, 0.5)
     r.check(r.run())
