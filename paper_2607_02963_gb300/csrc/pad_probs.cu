@@ -7,7 +7,7 @@
 // traffic.  As many clusters as the GPU holds take rows in turn.  Bound by the chain that a row is to its CTAs, 10 to 14 us
 // (event, context, slice, maximum, sum, the cluster's meeting, the way out), and by the 36 rows that are under way
 // together: 180 rows of 150001 in fp32 take 71 us, contexts of 2048 tokens on average, 57 without contexts; 64 rows of 131072
-// in bf16 with a mask and biases 34 us; 5 rows of 32768 under 9 us, the host's call.
+// in bf16 with a mask and biases 31 us; 5 rows of 32768 under 9 us, the host's call.
 // (A cluster launched for each row: 77 us, a third of the GPU waiting for a whole cluster's room.  Two passes without
 // clusters, the second joining the slices of the first: 74 us, 33 and 12.  The slice in shared memory instead of
 // registers: 77, 35 and 9.  The next row's slice fetched to L2 ahead, its event looked up ahead: no gain.  Rows of one event
@@ -37,12 +37,15 @@ constexpr int kSlack = 16;         // entries of the planes beyond a slice
 constexpr float kNegInf = -__builtin_huge_valf();
 constexpr float kLog2e = 1.4426950408889634f;
 
-// A CTA's threads hold its slice in registers, kEach entries each.
-template <bool LONG>
+// A CTA's threads hold its slice in registers, kEach entries each; E: entries of a vector, 8 where logits or results are in
+// 16 bits.  (64 rows of 131072 in bf16: 192 threads 31 us, 256 of 80 entries 35; 180 rows of 150001 in fp32: 78 and 72.)
+template <bool LONG, int E>
 struct Shape {
-  static constexpr int kThreads = 256, kEach = LONG ? 96 : 80, kWarps = kThreads / 32;
+  static constexpr int kThreads = !LONG && E == 8 ? 192 : 256, kEach = LONG ? 96 : E == 8 ? 104 : 80, kWarps = kThreads / 32;
   static constexpr int kSlice = kThreads * kEach / 32 * 32;
 };
+template <class TL, class TP>
+constexpr int vector_entries() { return sizeof(TL) == 2 || sizeof(TP) == 2 ? 8 : 4; }
 // Bytes of shared memory: counts (16 or 32 bits an entry), sums of biases and which entries have one or more than one,
 // results on their way out where p's rows are not as far from 16-byte boundaries as the logits'.
 __host__ __device__ inline size_t count_bytes(int slice, bool wide) { return (size_t)(slice + kSlack) * (wide ? 4 : 2); }
@@ -107,10 +110,11 @@ __device__ __forceinline__ void keep_allowed(float (&y)[E], const Change& h, int
 
 // WIDE: 32-bit counts.
 template <class TL, class TP, bool LONG, bool WIDE>
-__global__ void __launch_bounds__(Shape<LONG>::kThreads, LONG ? 1 : 2)
+__global__ void __launch_bounds__((Shape<LONG, vector_entries<TL, TP>()>::kThreads), LONG ? 1 : 2)
     probs_kernel(const __grid_constant__ ChunkProbs a, const ChunkVerify* __restrict__ work, int rows, int slice, int staged) {
-  using S = Shape<LONG>;
-  constexpr int T = S::kThreads, E = sizeof(TL) == 2 || sizeof(TP) == 2 ? 8 : 4, K = S::kEach / E;  // entries of a vector, vectors of a thread
+  constexpr int E = vector_entries<TL, TP>();
+  using S = Shape<LONG, E>;
+  constexpr int T = S::kThreads, K = S::kEach / E;  // entries of a vector, vectors of a thread
   extern __shared__ __align__(16) uint8_t smem[];
   __shared__ Part warp_part[S::kWarps];
   __shared__ Part both[2][kMaxCtas];  // of the row at hand and the one before
@@ -429,20 +433,20 @@ __global__ void __launch_bounds__(Shape<LONG>::kThreads, LONG ? 1 : 2)
 template <class TL, class TP, bool LONG, bool WIDE>
 cudaError_t launch(const ChunkProbs& a, const ChunkVerify* work, int rows, int ctas, int slice, bool staged, cudaStream_t s) {
   auto* kernel = probs_kernel<TL, TP, LONG, WIDE>;
-  constexpr int longest = Shape<LONG>::kSlice;
+  using S = Shape<LONG, vector_entries<TL, TP>()>;
   static bool configured[64] = {};
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
   if (dev < 0 || dev >= 64 || !configured[dev]) {
-    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(count_bytes(longest, WIDE) + bias_bytes(longest)));
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(count_bytes(S::kSlice, WIDE) + bias_bytes(S::kSlice)));
     if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
     if (e != cudaSuccess) return e;
     if (dev >= 0 && dev < 64) configured[dev] = true;
   }
   const size_t planes = (a.history != nullptr || a.tokens != nullptr ? count_bytes(slice, WIDE) : 0) + (a.bias_token != nullptr ? bias_bytes(slice) : 0);
   cudaLaunchConfig_t cfg = {};
-  cfg.blockDim = dim3(Shape<LONG>::kThreads);
+  cfg.blockDim = dim3(S::kThreads);
   cfg.dynamicSmemBytes = std::max(planes, staged ? stage_bytes(slice) : 0);
   cfg.stream = s;
   cudaLaunchAttribute attr[1];
@@ -476,20 +480,20 @@ cudaError_t launch(const ChunkProbs& a, const ChunkVerify* work, int rows, int c
   const bool staged = apart % unit != 0 || (rows > 1 && (a.p_stride - a.logits_stride) % unit != 0);
   // (a count is at most the context's length)
   const bool wide = (int64_t)a.history_width + a.longest > 65535;
-  if (slice <= Shape<false>::kSlice)
+  if (slice <= Shape<false, vector_entries<TL, TP>()>::kSlice)
     return wide ? launch<TL, TP, false, true>(a, work, rows, ctas, slice, staged, s) : launch<TL, TP, false, false>(a, work, rows, ctas, slice, staged, s);
   return wide ? launch<TL, TP, true, true>(a, work, rows, ctas, slice, staged, s) : launch<TL, TP, true, false>(a, work, rows, ctas, slice, staged, s);
 }
 
 }  // namespace
 
-int chunk_probs_max_vocab() { return kMaxCtas * Shape<true>::kSlice - 64; }
+int chunk_probs_max_vocab() { return kMaxCtas * Shape<true, 4>::kSlice - 64; }
 
 cudaError_t launch_chunk_probs(const ChunkProbs& a, const ChunkVerify* work, int n_tokens, cudaStream_t s) {
   // a row over as many CTAs as leave each 2048 entries, eight where they hold it (with 16 of half as many
   // threads 180 rows of 150001 take 82 us, not 71)
   int ctas = 1;
-  while (ctas < kMaxCtas && a.vocab > ctas * (ctas < 8 ? 2048 : Shape<false>::kSlice - 64)) ctas *= 2;
+  while (ctas < kMaxCtas && a.vocab > ctas * (ctas < 8 ? 2048 : Shape<false, 8>::kSlice - 64)) ctas *= 2;
   const int slice = (a.vocab + 7 + 32 * ctas - 1) / (32 * ctas) * 32;  // (the first begins up to seven entries before the row)
   if ((int64_t)n_tokens * ctas > INT32_MAX) return cudaErrorInvalidValue;
   if (a.logits_bf16)
