@@ -541,7 +541,8 @@ typedef struct pad_chunk_t pad_chunk_t;
 #define PAD_KV_FP4 4
 
 /* Bytes of device workspace pad_chunk_plan needs (host arrays, same meaning as there); 0 on
- * invalid arguments.  A caller that keeps one workspace for many steps takes the largest. */
+ * invalid arguments.  (PAD_KV_FP4: a branch with more than 96 new query rows, tokens x h_q / h_kv, brings the bytes of its cached
+ * tokens in bf16.)  A caller that keeps one workspace for many steps takes the largest. */
 size_t pad_chunk_workspace_size(const pad_problem* prob, int32_t kv_format, int32_t n_videos,
                                 const int32_t* prefix_len, int32_t n_events, const int32_t* event_video,
                                 const int32_t* event_len, const int32_t* n_new);
@@ -648,7 +649,7 @@ pad_status pad_chunk_append_rope(const pad_chunk_t* chunk, const pad_rope* rope,
                                  pad_stream_t stream);
 
 /* Copy the cached tokens of every event, positions 0 .. event_len + n_new - 1, event after event,
- * into k_out / v_out [n_cached, h_kv, head_dim] bf16 (exact in either format).  The tokens of a page id outside
+ * into k_out / v_out [n_cached, h_kv, head_dim] bf16 (exact in each format).  The tokens of a page id outside
  * the pool come out as zeros, and it is recorded (pad_chunk_status). */
 pad_status pad_chunk_read(const pad_chunk_t* chunk, const void* k_pool, const void* v_pool, const uint8_t* k_scale,
                           const uint8_t* v_scale, void* k_out, void* v_out, pad_stream_t stream);

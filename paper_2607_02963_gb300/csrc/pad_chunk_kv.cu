@@ -1,5 +1,5 @@
 // The private paged cache of the multi-token step: pad_chunk_append writes the new tokens of every
-// branch, in bf16 or as 8-bit groups, and pad_chunk_read copies cached tokens out as bf16.
+// branch, in bf16 or as 8-bit or 4-bit groups, and pad_chunk_read copies cached tokens out as bf16.
 //
 // An 8-bit group (the head_dim values of one token and kv-head): k is the smallest integer with
 // max|x| <= 448 * 2^k, kept in [-120, 7]; codes are e4m3 of x / 2^k to nearest even.  Both sides of
