@@ -303,7 +303,8 @@ __global__ void __launch_bounds__((Shape<LONG, vector_entries<TL, TP>()>::kThrea
     q.m = r.m, q.l = r.l;
   };
   block_join(false);
-  const float c = fminf(__fdiv_rn(kLog2e, temperature), 3.402823466e38f);  // (0 times it is 0 however small T)
+  // (0 times it is 0 however small T, -infinity times it -infinity however large)
+  const float c = fminf(fmaxf(__fdiv_rn(kLog2e, temperature), 0x1p-149f), 3.402823466e38f);
   if (greedy) {
     // the maximum's first place, and NaNs
     auto look = [&](float f, int token) {

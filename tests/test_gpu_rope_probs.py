@@ -342,6 +342,19 @@ def test_what_is_not_finite():
     assert p[7, int(r.logits[7].argmax())] == 1 and p[7].sum() == 1
 
 
+def test_an_infinite_temperature_makes_all_that_is_left_alike():
+    # (each p is 1 / n to 2^-20: exponents of 0, sums of ones)
+    r = Rows(8, [2, 2], 5003, 0, 0, 0.5)
+    r.logits[1, ::3] = -float("inf")
+    r.params[:, 0] = torch.tensor([float("inf"), 3e38])
+    r.params[:, 1], r.params[:, 2:] = 1.0, 0.0
+    p = r.run(tokens=None, history=None, history_len=None).double().cpu()
+    for row in range(4):
+        left = torch.from_numpy(r.allowed[row]) & (r.logits[row] != -float("inf"))
+        want = left.double() / left.sum().clamp_min(1)
+        assert ((p[row] - want).abs() <= 2.0 ** -20 * want).all()
+
+
 def test_tokens_outside_the_vocabulary_and_long_lengths_are_passed_over():
     r = Rows(5, [2], 1000, 20, 20)
     r.history[0, ::3], r.bias[0][0, ::4] = -1, 1000
