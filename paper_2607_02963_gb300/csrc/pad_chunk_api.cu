@@ -166,7 +166,8 @@ void cut_mma(std::vector<Segment>& segs, int paged, const pad_problem& prob, boo
     }
   double per = work / (8.0 * sms);
   const int64_t slots = fp4 ? (int64_t)chunk_mma4_ctas(prob.head_dim, rows) * sms : 0;
-  if (least <= slots) per = work / (double)slots;
+  const bool one_wave = fp4 && least <= slots;
+  if (one_wave) per = work / (double)slots;
   int64_t len = std::max<int64_t>(kMinSplit, ((int64_t)(per / kSplitUnit) + 1) * kSplitUnit);
   auto ctas = [&]() {
     int64_t n = 0;
@@ -174,7 +175,7 @@ void cut_mma(std::vector<Segment>& segs, int paged, const pad_problem& prob, boo
       if (!s.tc && s.paged == paged) n += (int64_t)((s.ntok + tpt - 1) / tpt) * prob.h_kv * ((s.keys + len - 1) / len);
     return n;
   };
-  if (least <= slots)
+  if (one_wave)
     while (len < longest_keys && ctas() > slots) len += std::max<int64_t>(1, len / (16 * kSplitUnit)) * kSplitUnit;
   for (Segment& s : segs)
     if (!s.tc && s.paged == paged) split_by(s, len, kSplitUnit);
