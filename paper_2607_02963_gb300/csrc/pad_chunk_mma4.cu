@@ -43,6 +43,9 @@ constexpr int kBlk = 32;          // keys of a block
 constexpr float kNegInf = -__builtin_huge_valf();
 constexpr float kLn2 = 0.69314718055994531f;
 constexpr float kUp = 15.f;       // weights are held as 2^15 times themselves
+// Scores (in powers of two) from which on one rounding of a score and of its row's maximum each, 2^-24 of them, may move a weight
+// by more than 2^(1/8): 2^15 times it would leave f16 from 2^23 on.
+constexpr float kFar = 0x1p20f;
 
 // A warp's stages: the codes and scales of a block as they lie in the pages.
 template <int D, int NT>
@@ -218,6 +221,7 @@ __global__ void __launch_bounds__(kThreads, (ctas_per_sm<D, NT>())) chunk_mma4_k
   }
 
   int s_use = 0, s_fill = R::kStages - 1;  // the stages of this block and of the one being fetched
+  bool far = false;                        // some row's maximum is beyond kFar (the same in all lanes)
   const int kg = key_of(g);
 #pragma unroll 1
   for (int i = 0; i < mine; ++i) {
@@ -330,6 +334,7 @@ __global__ void __launch_bounds__(kThreads, (ctas_per_sm<D, NT>())) chunk_mma4_k
       }
     // (the maximum of few blocks is above all before them)
     if (__any_sync(0xffffffffu, grow)) {
+      bool beyond = false;
 #pragma unroll
       for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -345,17 +350,33 @@ __global__ void __launch_bounds__(kThreads, (ctas_per_sm<D, NT>())) chunk_mma4_k
             o[n][c][2 + u] *= alpha;
           }
           mx[n][u] = m_new;
+          beyond |= m_new != kNegInf && fabsf(m_new) > kFar;
         }
+      far = __any_sync(0xffffffffu, beyond);
     }
     uint32_t pf[NT][2][2];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-      const float up[2] = {mx[n][0] == kNegInf ? 0.f : kUp - mx[n][0], mx[n][1] == kNegInf ? 0.f : kUp - mx[n][1]};
+      float up[2] = {mx[n][0] == kNegInf ? 0.f : kUp - mx[n][0], mx[n][1] == kNegInf ? 0.f : kUp - mx[n][1]};
+      float by[2] = {qs[n][0], qs[n][1]};
+      if (far) {
+        // scores rounded as their maximum was, whose difference from it is then never above 0
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const float m0 = mx[n][u] == kNegInf ? 0.f : mx[n][u];
+#pragma unroll
+          for (int m = 0; m < 2; ++m)
+#pragma unroll
+            for (int v = 0; v < 2; ++v) s[n][m][2 * v + u] = __fsub_rn(__fmul_rn(s[n][m][2 * v + u], by[u]), m0);
+          by[u] = 1.f;
+          up[u] = kUp;
+        }
+      }
 #pragma unroll
       for (int m = 0; m < 2; ++m)
 #pragma unroll
         for (int v = 0; v < 2; ++v) {
-          const float a = ex2(fmaf(s[n][m][2 * v], qs[n][0], up[0])), b = ex2(fmaf(s[n][m][2 * v + 1], qs[n][1], up[1]));
+          const float a = ex2(fmaf(s[n][m][2 * v], by[0], up[0])), b = ex2(fmaf(s[n][m][2 * v + 1], by[1], up[1]));
           l[n][0] += a;
           l[n][1] += b;
           pf[n][m][v] = transposed(pack_f16(a, b));
