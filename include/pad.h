@@ -631,7 +631,7 @@ typedef struct {
 typedef struct {
   int32_t head_dim, rotary_dim, layout;
   float magnitude;
-  uint64_t turn[64];         /* f_i / 2 pi in units of 2^-64: the product with a position, without its upper bits, is the
+  uint64_t turn[64];         /* f_i / 2 pi in units of 2^-64, to within one: the product with a position, without its upper bits, is the
                               * pair's angle as a fraction of a turn, however far the position */
 } pad_rope;
 /* Fill `rope` from `spec` (host). */
@@ -641,7 +641,7 @@ pad_status pad_rope_init(const pad_rope_spec* spec, pad_rope* rope);
  * quantised where the cache is), v_new is written as it is, and q is turned into q_out.
  *   position   [N] int32 device, of each new token, any value
  *   q, q_out   [N, h_q, head_dim] bf16; q_out may be q itself (same stride), and must not overlap q, k_new or v_new otherwise
- * Angles are exact to 2^-24 of a turn at any position.  Strides are in elements, multiples of 8, 0 = packed.  A page id
+ * Angles are exact to 2^-24 of a turn at any position (frequencies of up to 2^30 turns a token).  Strides are in elements, multiples of 8, 0 = packed.  A page id
  * outside the pool keeps its keys and values out and is recorded; their queries are turned all the same. */
 pad_status pad_chunk_append_rope(const pad_chunk_t* chunk, const pad_rope* rope, const int32_t* position, const void* q,
                                  int64_t q_stride, void* q_out, int64_t q_out_stride, const void* k_new, const void* v_new,

@@ -10,6 +10,7 @@
 #include <nvtx3/nvToolsExt.h>
 
 #include "pad_chunk.h"
+#include "pad_wide.h"
 
 static_assert(sizeof(pad_chunk_info) == 64, "prefix_tokens takes what was padding: the struct keeps its size");
 
@@ -659,7 +660,7 @@ pad_status pad_chunk_append(const pad_chunk_t* c, const void* k_new, const void*
 pad_status pad_rope_init(const pad_rope_spec* spec, pad_rope* rope) {
   if (!spec || !rope) return api_fail(PAD_ERR_INVALID_ARG, "NULL argument");
   const pad_rope_spec& s = *spec;
-  const double R = s.rotary_dim, pi = 3.14159265358979323846;
+  const double R = s.rotary_dim;
   auto positive = [](double x) { return x > 0 && std::isfinite(x); };
   if (s.head_dim != 64 && s.head_dim != 128) return api_fail(PAD_ERR_UNSUPPORTED, "head_dim=%d (supported: 64, 128)", s.head_dim);
   if (s.rotary_dim < 2 || s.rotary_dim > s.head_dim || s.rotary_dim % 2 != 0)
@@ -677,29 +678,31 @@ pad_status pad_rope_init(const pad_rope_spec* spec, pad_rope* rope) {
       return api_fail(PAD_ERR_INVALID_ARG, "a ramp over the index needs low > 0 and theta > 1");
   }
   double a = 0, b = 0;
+  const Wide log_theta = wide_log(s.theta);
   if (s.scaling == PAD_ROPE_INDEX) {
-    auto index = [&](double n) { return R * std::log(s.original_len / (2 * pi * n)) / (2 * std::log(s.theta)); };
-    a = std::min(std::max(std::floor(index(s.high)), 0.0), R - 1);
-    b = std::min(std::max(std::ceil(index(s.low)), 0.0), R - 1);
+    auto index = [&](double n) { return wide_log(Wide(s.original_len) / (wide_two_pi() * n)) * R / (log_theta * 2); };
+    a = std::min(std::max(wide_floor(index(s.high)).hi, 0.0), R - 1);
+    b = std::min(std::max(-wide_floor(-index(s.low)).hi, 0.0), R - 1);
   }
-  const double theta = s.scaling == PAD_ROPE_BASE ? s.theta * std::pow(s.factor, R / (R - 2)) : s.theta;
+  const Wide log_base = s.scaling == PAD_ROPE_BASE ? log_theta + wide_log(s.factor) * R / (R - 2) : log_theta;
   pad_rope r{};
   r.head_dim = s.head_dim;
   r.rotary_dim = s.rotary_dim;
   r.layout = s.layout;
   r.magnitude = (float)s.magnitude;
   for (int i = 0; i < s.rotary_dim / 2; ++i) {
-    double f = std::pow(theta, -2.0 * i / R), g = 1;
+    Wide f = wide_exp(log_base * (-2.0 * i) / R), g = 1;
     if (s.scaling == PAD_ROPE_LINEAR) g = 0;
-    if (s.scaling == PAD_ROPE_TURNS) g = (s.original_len * f / (2 * pi) - s.low) / (s.high - s.low);
-    if (s.scaling == PAD_ROPE_INDEX) g = 1 - (i - a) / std::max(b - a, 0.001);
-    g = std::min(std::max(g, 0.0), 1.0);
-    if (g < 1) f *= g + (1 - g) / s.factor;
-    // as a fraction of a turn: whole turns a token make no difference
-    const double turn = f / (2 * pi);
-    if (!std::isfinite(turn)) return api_fail(PAD_ERR_INVALID_ARG, "the frequency of pair %d is not finite", i);
-    const double part = std::ldexp(turn - std::floor(turn), 64);
-    r.turn[i] = part < 18446744073709551616.0 ? (uint64_t)part : 0;
+    if (s.scaling == PAD_ROPE_TURNS) g = (f * s.original_len / wide_two_pi() - s.low) / wide_sum(s.high, -s.low);
+    if (s.scaling == PAD_ROPE_INDEX) g = Wide(1) - Wide(i - a) / std::max(b - a, 0.001);
+    if (g < 0) g = 0;
+    if (g < 1) f = f * (g + (Wide(1) - g) / s.factor);
+    // as a fraction of a turn, 64 bits of it: whole turns a token make no difference
+    const Wide turn = f / wide_two_pi();
+    if (!std::isfinite(turn.hi)) return api_fail(PAD_ERR_INVALID_ARG, "the frequency of pair %d is not finite", i);
+    const Wide part = turn - wide_floor(turn);
+    const double hi = std::ldexp(part.hi, 64), whole = std::floor(hi), rest = std::nearbyint(hi - whole + std::ldexp(part.lo, 64));
+    r.turn[i] = (whole < 0x1p64 ? (uint64_t)whole : 0) + (uint64_t)(int64_t)rest;
   }
   *rope = r;
   return PAD_OK;
