@@ -619,7 +619,7 @@ typedef struct {
   double factor;             /* > 0 */
   double original_len;       /* > 0 */
   double low, high;          /* low < high (PAD_ROPE_INDEX: 0 < low < high) */
-  double magnitude;          /* finite; 1 for none */
+  double magnitude;          /* finite in 32 bits; 1 for none */
 } pad_rope_spec;
 #define PAD_ROPE_HALF 0
 #define PAD_ROPE_INTERLEAVED 1

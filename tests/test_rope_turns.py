@@ -53,3 +53,10 @@ def test_each_turn_is_within_a_unit(padlib, spec, rotary):
     for i, (g, want) in enumerate(zip(got, exact_turns(rotary, **spec))):
         off = abs(Decimal(g) - want % 1 * 2 ** 64)
         assert min(off, 2 ** 64 - off) <= 1, f"pair {i}: {float(off)} units"
+
+
+def test_a_magnitude_beyond_32_bits_is_refused(padlib):
+    B.Rope(128, magnitude=3.4e38)
+    for bad in (3.5e38, -1e300):
+        with pytest.raises(B.PadError, match="magnitude"):
+            B.Rope(128, magnitude=bad)
