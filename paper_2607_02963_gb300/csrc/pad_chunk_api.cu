@@ -1,6 +1,7 @@
 // C ABI of the multi-token step (pad_chunk_*, pad_draft_verify): argument checks, page allocation, the
 // work lists and their launches.
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 #include <cstring>
 #include <exception>
@@ -668,7 +669,7 @@ pad_status pad_rope_init(const pad_rope_spec* spec, pad_rope* rope) {
   if (s.layout != PAD_ROPE_HALF && s.layout != PAD_ROPE_INTERLEAVED) return api_fail(PAD_ERR_INVALID_ARG, "layout=%d", s.layout);
   if (s.scaling < PAD_ROPE_NONE || s.scaling > PAD_ROPE_INDEX) return api_fail(PAD_ERR_INVALID_ARG, "scaling=%d", s.scaling);
   if (!positive(s.theta)) return api_fail(PAD_ERR_INVALID_ARG, "theta must be finite and > 0");
-  if (!(std::fabs(s.magnitude) <= 3.402823466e38)) return api_fail(PAD_ERR_INVALID_ARG, "magnitude must be finite in 32 bits");
+  if (!(std::fabs(s.magnitude) <= FLT_MAX)) return api_fail(PAD_ERR_INVALID_ARG, "magnitude must be finite in 32 bits");
   if (s.scaling != PAD_ROPE_NONE && !positive(s.factor)) return api_fail(PAD_ERR_INVALID_ARG, "factor must be finite and > 0");
   if (s.scaling == PAD_ROPE_BASE && s.rotary_dim < 4) return api_fail(PAD_ERR_INVALID_ARG, "a scaled base needs a rotary_dim of 4 at least");
   if (s.scaling == PAD_ROPE_TURNS || s.scaling == PAD_ROPE_INDEX) {

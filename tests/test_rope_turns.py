@@ -3,6 +3,7 @@ one unit of the exact one for frequencies of up to 2^30 turns a token (half a un
 what it is formed with)."""
 from decimal import ROUND_CEILING, ROUND_FLOOR, Decimal, getcontext
 
+import numpy as np
 import pytest
 
 from paper_2607_02963_gb300 import binding as B
@@ -56,7 +57,7 @@ def test_each_turn_is_within_a_unit(padlib, spec, rotary):
 
 
 def test_a_magnitude_beyond_32_bits_is_refused(padlib):
-    B.Rope(128, magnitude=3.4e38)
+    B.Rope(128, magnitude=float(np.finfo(np.float32).max))
     for bad in (3.5e38, -1e300):
         with pytest.raises(B.PadError, match="magnitude"):
             B.Rope(128, magnitude=bad)
