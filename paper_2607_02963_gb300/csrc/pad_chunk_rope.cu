@@ -50,7 +50,7 @@ __device__ __forceinline__ float lo_of(uint32_t v) { return __uint_as_float(v <<
 __device__ __forceinline__ float hi_of(uint32_t v) { return __uint_as_float(v & 0xffff0000u); }
 
 // The lane's eight values turned.  cs: cosine and signed sine that go with each (kInterleaved: of the pairs); n: how many of
-// the eight are turned (kHalf: 0 or 8); other: the lane (of the warp) or the row in shared memory with the pairs' other members.
+// the eight are turned, an even number (kHalf: 0 or 8); other: the lane (of the warp) or the row in shared memory with the pairs' other members.
 template <int LAYOUT>
 __device__ __forceinline__ uint4 turned(uint4 x, const float2 (&cs)[8], int n, int other, const uint16_t* row, int d0, int rotary) {
   uint32_t v[4] = {x.x, x.y, x.z, x.w};
@@ -78,8 +78,7 @@ __device__ __forceinline__ uint4 turned(uint4 x, const float2 (&cs)[8], int n, i
         o[u] = a * cs[2 * j + u].x + b * cs[2 * j + u].y;
       }
       const uint32_t w = rounded2(o[0], o[1]);
-      if (2 * j + 1 < n) v[j] = w;
-      else if (2 * j < n) v[j] = (w & 0xffffu) | (v[j] & 0xffff0000u);
+      if (2 * j < n) v[j] = w;
     }
   }
   return make_uint4(v[0], v[1], v[2], v[3]);
