@@ -532,8 +532,9 @@ pad_status pad_prefill_status(pad_stream_t stream);
  * as NaN throughout (its codes are 0); bytes 227 to 254 do not occur.  Code times scale has six significant bits at
  * most: it is exact in bf16, and attention multiplies it as it is.
  * In attention over 4-bit pages a weight is off by 2^-11 of itself at most, or by 2^-40 of the largest of its row's piece of
- * keys where that is more (weights below 2^-29 of it); sequences with many new query rows are widened to bf16 pages in the
- * workspace first, where the bf16 cache's 2^-8 holds.
+ * keys where that is more (weights below 2^-29 of it).  Branches with more than 96 new query rows (tokens x h_q / h_kv), and all
+ * under PAD_FLAG_PREFIX_TC (none under PAD_FLAG_PREFIX_MMA), are widened to bf16 pages in the workspace first; there, as over the bf16 prefix, it is the bf16
+ * cache's 2^-8.
  * --------------------------------------------------------------------------- */
 typedef struct pad_chunk_t pad_chunk_t;
 #define PAD_KV_BF16 0
@@ -659,16 +660,18 @@ pad_status pad_chunk_read(const pad_chunk_t* chunk, const void* k_pool, const vo
  * prefix; lse may be NULL.  q_stride: elements
  * from one token of q to the next, a multiple of 8, 0 = h_q * head_dim.  A page id outside the pool
  * hides its tokens and is recorded; a row that then sees nothing gets 0 and an lse of -infinity.  What
- * lies in cache slots past a branch's last token is never used in arithmetic. */
+ * lies in cache slots past a branch's last token is never used in arithmetic.  Scores are held in fp32; the tcgen05 kernel wants
+ * them (scale q.k) below 2^29 in magnitude, the warp-level one finite. */
 pad_status pad_chunk_attn(const pad_chunk_t* chunk, const void* q, int64_t q_stride, const void* k_prefix,
                           const void* v_prefix, const void* k_pool, const void* v_pool, const uint8_t* k_scale,
                           const uint8_t* v_scale, void* out, float* lse, pad_stream_t stream);
 
 /* Logits turned into the probabilities that pad_draft_verify reads.  Row t of event e:
  *   x = logit; c = how often the token occurs in the event's history and in its chunk's tokens up to and including t's;
- *   where c > 0, x = x / r if x > 0, else x * r, and then x = x - (frequency * c + presence);
+ *   where c > 0, x = x * (1 / r) if x > 0, 1 / r rounded to fp32 first, else x * r, and then x = x - (frequency * c + presence);
  *   x = x + the event's biases of that token; a token whose mask bit is 0 is left out, whatever its logit is;
- *   p = softmax(x / T) over what is left; with T not above 0 one-hot at the first largest x; zeros where nothing is left
+ *   p = softmax(x / T) over what is left (differences times log2(e) / T, rounded to fp32 first); with T not above 0 one-hot at
+ *   the first largest x; zeros where nothing is left
  *   (every token masked, or at -infinity).  A NaN or +infinity among what is left makes a row with T > 0 NaN; with T not above 0
  *   a NaN makes it zeros.
  *   logits       [N, vocab] fp32 or bf16 (logits_dtype 0 or 1), row stride logits_stride elements (0 = vocab)

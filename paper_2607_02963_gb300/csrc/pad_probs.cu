@@ -7,7 +7,9 @@
 // traffic.  As many clusters as the GPU holds take rows in turn.  Bound by the chain that a row is to its CTAs, 10 to 14 us
 // (event, context, slice, maximum, sum, the cluster's meeting, the way out), and by the 36 rows that are under way
 // together: 180 rows of 150001 in fp32 take 71 us, contexts of 2048 tokens on average, 57 without contexts; 64 rows of 131072
-// in bf16 with a mask and biases 31 us; 5 rows of 32768 under 9 us, the host's call.
+// in bf16 with a mask and biases 31 us; 5 rows of 32768 under 9 us, the host's call.  Where biases come with contexts, their
+// planes take six bytes an entry of shared memory and bound the CTAs of an SM beside the registers: to two at 131072 entries, to
+// one at 150001 (64 rows of it in bf16: 27 us without biases, 69 with 100 of them and a mask).
 // (A cluster launched for each row: 77 us, a third of the GPU waiting for a whole cluster's room.  Two passes without
 // clusters, the second joining the slices of the first: 74 us, 33 and 12.  The slice in shared memory instead of
 // registers: 77, 35 and 9.  The next row's slice fetched to L2 ahead, its event looked up ahead: no gain.  Rows of one event
@@ -38,7 +40,9 @@ constexpr float kNegInf = -__builtin_huge_valf();
 constexpr float kLog2e = 1.4426950408889634f;
 
 // A CTA's threads hold its slice in registers, kEach entries each; E: entries of a vector, 8 where logits or results are in
-// 16 bits.  (64 rows of 131072 in bf16: 192 threads 31 us, 256 of 80 entries 35; 180 rows of 150001 in fp32: 78 and 72.)
+// 16 bits.  (us, 192 threads of 104 entries and 256 of 80.  64 rows of 131072: bf16 24.9 and 29.4, with biases and a mask 31.1 and
+// 35.2; bf16 to fp32 31.0 and 36.1, 37.1 and 41.4; fp32 to bf16 24.7 and 24.1, 33.2 and 32.6.  180 rows of 150001: 61.7 and 76.2,
+// 77.8 and 95.5, 60.3 and 60.2; in fp32 78 and 72.)
 template <bool LONG, int E>
 struct Shape {
   static constexpr int kThreads = !LONG && E == 8 ? 192 : 256, kEach = LONG ? 96 : E == 8 ? 104 : 80, kWarps = kThreads / 32;
@@ -491,8 +495,8 @@ cudaError_t launch(const ChunkProbs& a, const ChunkVerify* work, int rows, int c
 int chunk_probs_max_vocab() { return kMaxCtas * Shape<true, 4>::kSlice - 64; }
 
 cudaError_t launch_chunk_probs(const ChunkProbs& a, const ChunkVerify* work, int n_tokens, cudaStream_t s) {
-  // a row over as many CTAs as leave each 2048 entries, eight where they hold it (with 16 of half as many
-  // threads 180 rows of 150001 take 82 us, not 71)
+  // a row over as many CTAs as leave each 2048 entries, eight where they hold it in 16 bits, up to 159232 entries (with 16 of half
+  // as many threads 180 rows of 150001 take 82 us, not 71)
   int ctas = 1;
   while (ctas < kMaxCtas && a.vocab > ctas * (ctas < 8 ? 2048 : Shape<false, 8>::kSlice - 64)) ctas *= 2;
   const int slice = (a.vocab + 7 + 32 * ctas - 1) / (32 * ctas) * 32;  // (the first begins up to seven entries before the row)
