@@ -23,8 +23,9 @@ def exact_turns(rotary, theta, scaling="none", factor=1.0, original_len=0.0, low
             x = rotary * (length / (2 * PI * n)).ln() / (2 * t.ln())
             return min(max(x.to_integral_value(way), Decimal(0)), Decimal(rotary - 1))
         a, b = index(hi, ROUND_FLOOR), index(lo, ROUND_CEILING)
+    log = t.ln()
     for i in range(rotary // 2):
-        f = (t.ln() * -2 * i / rotary).exp()
+        f = (log * -2 * i / rotary).exp()
         g = Decimal(1)
         if scaling == "linear":
             g = Decimal(0)
